@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdf11.so")
 SOURCES = ["df11_host.cpp", "df11_tables.cpp", "df11_decode.hip", "df11_gemm.hip", "df11_gemv.hip",
-           "df11_hlut_host.cpp", "df11_hlut.hip"]
+           "df11_hlut_host.cpp", "df11_hlut.hip", "df11_logits.hip", "df11_lora.hip"]
 
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
