@@ -1,6 +1,26 @@
 // Operators on rows of logits: log probabilities of given tokens with rank,
 // entropy and top alternatives, distillation from a teacher's top log
-// probabilities, and the gradients of both.  One workgroup per row.
+// probabilities, and the gradients of both.
+//
+// All of them are bound by reading the logits (and writing the gradient): a
+// row is cut into parts of 8192 values, a workgroup takes one part and holds it
+// in registers (32 values a lane, all loads issued at once), so the logits are
+// read once however many statistics are wanted.  One wave per row then joins
+// the parts:
+//   - the maximum first, then sum exp2((z - max) log2e / tau) with that maximum
+//     fixed, per wave; waves and parts are joined by scaling with the
+//     exponential of the difference of their maxima;
+//   - sum e x beside sum e gives the entropy without a second pass;
+//   - the alternatives: of the 256 lanes' maxima (they are there already) a
+//     value with at least `top` lanes at or above it is found by bisection over
+//     the ordered bits; no value below it can be among the `top` largest, and
+//     only few are above (about 1.3 top for values in any order).  They go to
+//     the workspace unordered; the join orders the few that are left, by value
+//     and index, which are distinct, so the order they arrived in is gone;
+//   - where more than the workspace's room are above (equal values, ordered
+//     ones), the part is trimmed exactly, over all its values and then over the
+//     indices of the equal ones.
+// Rows that start at any address are read with unaligned 16-byte loads.
 #include "df11_ops_common.h"
 
 namespace {
@@ -8,106 +28,487 @@ namespace {
 using namespace df11ops;
 
 constexpr uint32_t kThreads = 256;
-constexpr int kWaves = kThreads / 64;
-constexpr uint32_t kPart = 8192;  // values of a row that one workgroup of a gradient takes
+constexpr uint32_t kWaves = kThreads / 64;
+constexpr uint32_t kPerLane = 32;
+constexpr uint32_t kPart = kThreads * kPerLane;  // values of a row in one workgroup
 
 // (v - m) / tau, of halves so that the difference of two finite values is finite
 __device__ float scaled(float v, float m, float two_over_tau) {
     return fmaf(v, 0.5f, -0.5f * m) * two_over_tau;
 }
 
+// Bits in the order of the values: unsigned comparison.  -0 is +0.
+__device__ uint32_t ordered(float v) {
+    const uint32_t u = __float_as_uint(v + 0.0f);
+    return u ^ (u & 0x80000000u ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ float from_ordered(uint32_t k) {
+    return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
+constexpr uint32_t kOrderedMasked = 0x007FFFFFu;  // of -inf
+
+// The next larger float; of -inf the lowest finite one.
+__device__ float above_of(float v) {
+    const uint32_t u = __float_as_uint(v + 0.0f);
+    return __uint_as_float(u & 0x80000000u ? u - 1 : u + 1);
+}
+
+// A lane's 32 values of a part: vector i of the lane holds the values from
+// part + (256 i + thread) * kVec.  What lies past the row is masked.
+template <class T>
+struct Held {
+    static constexpr uint32_t kVecs = kPerLane / T::kVec;
+    uint4 q[kVecs];
+
+    __device__ static uint32_t first(uint32_t part, uint32_t i) {
+        return part + (kThreads * i + threadIdx.x) * T::kVec;
+    }
+    __device__ void load(const typename T::raw *z, uint32_t part, uint32_t vocab) {
+        if (part + kPart <= vocab) {
+#pragma unroll
+            for (uint32_t i = 0; i < kVecs; ++i) q[i] = load16(z + first(part, i));
+            return;
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kVecs; ++i) {
+            const uint32_t j = first(part, i);
+            if (j + T::kVec <= vocab) {
+                q[i] = load16(z + j);
+            } else {
+                uint32_t w[4];
+                constexpr uint32_t both = T::kVec == 8 ? T::kMasked * 0x10001u : T::kMasked;
+                for (uint32_t e = 0; e < 4; ++e) w[e] = both;
+#pragma unroll
+                for (uint32_t e = 0; e < T::kVec; ++e)
+                    if (j + e < vocab) {
+                        if constexpr (T::kVec == 4) {
+                            w[e] = __float_as_uint(z[j + e]);
+                        } else {
+                            const uint32_t v = z[j + e];
+                            w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | v << 16
+                                             : (w[e / 2] & 0xFFFF0000u) | v;
+                        }
+                    }
+                q[i] = uint4{w[0], w[1], w[2], w[3]};
+            }
+        }
+    }
+    template <class F>
+    __device__ void each(F f) const {  // f(value, vector, element)
+#pragma unroll
+        for (uint32_t i = 0; i < kVecs; ++i)
+#pragma unroll
+            for (uint32_t e = 0; e < T::kVec; ++e) f(T::get(q[i], e), i, e);
+    }
+    __device__ float max() const {
+        float m = -INFINITY;
+        each([&](float v, uint32_t, uint32_t) { m = fmaxf(m, v); });
+        return m;
+    }
+};
+
+// What a part, or several, says about its row: maximum (at least the lowest
+// finite value, so that masked values give exp(-inf)), sum e, and a second sum:
+// e x in powers of two for the entropy, or e over the places a teacher does
+// not name.
+struct PartStat {
+    float m, s, t;
+    uint32_t above;
+};
+
+// e = exp2((v - m) c) for a wave's values with the wave's maximum m: f(v, e, x, i, j)
+// with x = (v - m) c up to the returned shift, which is the same for all.
+// One fused operation a value where m c is in range; its rounding is the shift.
+template <class T, class F>
+__device__ float each_exp(const Held<T> &h, float m, float two_over_tau, F f) {
+    const float c = 0.5f * two_over_tau * kLog2e, mc = m * c;
+    if (fabsf(mc) < 1e38f) {
+        h.each([&](float v, uint32_t i, uint32_t e) {
+            const float x = fmaf(v, c, -mc);
+            f(v, __builtin_amdgcn_exp2f(x), x, i, e);
+        });
+        return fmaf(m, c, -mc);  // m c is mc plus this: the true x is x minus it
+    }
+    h.each([&](float v, uint32_t i, uint32_t e) {
+        const float x = scaled(v, m, two_over_tau) * kLog2e;
+        f(v, __builtin_amdgcn_exp2f(x), x, i, e);
+    });
+    return 0.0f;
+}
+
+// Sums with maximum m scaled to the larger maximum M: the factor, and for the
+// sum of e x the shift of x.
+__device__ void rescale(const PartStat &p, float M, float two_over_tau, bool xsum, float *s,
+                        float *t) {
+    const float d = fmaxf(scaled(p.m, M, two_over_tau) * kLog2e, -300.0f);
+    const float f = d <= -300.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
+    *s += p.s * f;
+    *t += f * (xsum ? fmaf(d, p.s, p.t) : p.t);
+}
+
+// The waves' statistics as one, by every thread, after a barrier.
+__device__ PartStat join_waves(const PartStat *w, float two_over_tau, bool xsum) {
+    PartStat p{w[0].m, 0.0f, 0.0f, 0};
+    for (uint32_t i = 1; i < kWaves; ++i) p.m = fmaxf(p.m, w[i].m);
+    for (uint32_t i = 0; i < kWaves; ++i) {
+        rescale(w[i], p.m, two_over_tau, xsum, &p.s, &p.t);
+        p.above += w[i].above;
+    }
+    return p;
+}
+
+// The parts' statistics of a row as one, by a wave.
+__device__ PartStat join_parts(const PartStat *stat, uint32_t parts, float two_over_tau, bool xsum,
+                               uint64_t *above) {
+    const uint32_t lane = threadIdx.x & 63u;
+    PartStat mine{kLowest, 0.0f, 0.0f, 0};
+    uint64_t count = 0;
+    for (uint32_t i = lane; i < parts; i += 64) {  // one round up to 524,288 values
+        const PartStat p = stat[i];
+        const float M = fmaxf(mine.m, p.m);
+        PartStat both{M, 0.0f, 0.0f, 0};
+        rescale(mine, M, two_over_tau, xsum, &both.s, &both.t);
+        rescale(p, M, two_over_tau, xsum, &both.s, &both.t);
+        count += p.above;
+        mine = both;
+    }
+    PartStat row{wave_max(mine.m), 0.0f, 0.0f, 0};
+    float s = 0.0f, t = 0.0f;
+    rescale(mine, row.m, two_over_tau, xsum, &s, &t);
+    row.s = wave_sum(s);
+    row.t = wave_sum(t);
+    *above = static_cast<uint64_t>(wave_sum(static_cast<uint32_t>(count >> 16))) * 65536u +
+             wave_sum(static_cast<uint32_t>(count & 0xFFFFu));
+    return row;
+}
+
+// ------------------------------------------------------------ log probabilities
 struct LogprobArgs {
     const void *logits;
     const int64_t *tokens;
+    PartStat *stat;      // rows x parts
+    uint32_t *count;     // rows x parts: candidates
+    uint2 *candidate;    // rows x parts x room: ordered bits, index
     float *logprob, *entropy, *top_logprob, *stats;
     int64_t *rank, *top_index;
     uint64_t stride;
-    uint32_t vocab, top;
+    uint32_t vocab, parts, top, room;
     float two_over_tau;
 };
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void logprob_rows_kernel(LogprobArgs g) {
-    __shared__ float red[kWaves];
-    __shared__ float best_v[kThreads];
-    __shared__ uint32_t best_i[kThreads];
-    const uint64_t row = blockIdx.x;
+// Values above the threshold that a part may bring: twice what is wanted, and
+// some, so that equal neighbours (bf16 has 8 bits of mantissa) fit.
+__host__ __device__ constexpr uint32_t room_of(uint32_t top) { return top ? 2 * top + 64 : 0; }
+
+// How many of a workgroup's values satisfy f(value, index), by every thread.
+template <class T, class F>
+__device__ uint32_t wg_count(const Held<T> &h, uint32_t part, uint32_t *lds, F f) {
+    uint32_t n = 0;
+    h.each([&](float v, uint32_t i, uint32_t e) { n += f(v, h.first(part, i) + e) ? 1u : 0u; });
+    n = wave_sum(n);
+    __syncthreads();
+    if ((threadIdx.x & 63u) == 0) lds[threadIdx.x >> 6] = n;
+    __syncthreads();
+    n = 0;
+    for (uint32_t w = 0; w < kWaves; ++w) n += lds[w];
+    return n;
+}
+
+template <class T, bool kTop>
+__device__ void logprob_part(const LogprobArgs &g) {
+    __shared__ PartStat wave_stat[kWaves];
+    __shared__ uint32_t lane_key[kThreads];
+    __shared__ uint32_t found, counts[kWaves];
+    const uint32_t row_parts = g.parts;
+    const uint64_t row = blockIdx.x / row_parts;
+    const uint32_t part = (blockIdx.x % row_parts) * kPart;
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
+    Held<T> h;
+    h.load(z, part, g.vocab);
+
     const int64_t token = g.tokens ? g.tokens[row] : -1;
     const bool asked = token >= 0 && token < g.vocab;
-    const float zt = asked ? T::load(z[token]) : 0.0f;
-    // the lowest finite value and no -inf: masked values then give exp(-inf)
-    float m = -3.402823466e38f;
-    for (uint32_t j = threadIdx.x; j < g.vocab; j += kThreads) m = fmaxf(m, T::load(z[j]));
-    m = wg_max<kWaves>(m, red);
-    float s = 0.0f, t = 0.0f, above = 0.0f;
-    for (uint32_t j = threadIdx.x; j < g.vocab; j += kThreads) {
-        const float v = T::load(z[j]);
-        const float x = scaled(v, m, g.two_over_tau);
-        const float e = expf(x);
+    const uint32_t tok = asked ? static_cast<uint32_t>(token) : 0;
+    const float zt = asked ? T::load(z[tok]) : __builtin_nanf("");
+    const float more = asked ? above_of(zt) : zt;
+
+    const float lane_max = h.max();
+    const float m = fmaxf(wave_max(lane_max), kLowest);
+    float s = 0.0f, t = 0.0f;
+    uint32_t above = 0;
+    const auto add = [&](float v, float e, float x, uint32_t i, uint32_t) {
         s += e;
-        t += e * fmaxf(x, -200.0f);  // e is 0 below; no 0 * inf
-        above += v > zt || (v == zt && j < static_cast<uint64_t>(token)) ? 1.0f : 0.0f;
+        t = fmaf(e, fmaxf(x, -300.0f), t);  // no 0 * inf
+        // before the token equal values count, from it on larger ones
+        above += v >= (h.first(part, i) < tok ? zt : more) ? 1u : 0u;
+    };
+    const float shift = each_exp(h, m, g.two_over_tau, add);
+    // in the token's own vector equal ones from the token on were counted too
+    if (asked && tok >= part && tok - part < kPart && (tok - part) % T::kVec != 0 &&
+        (tok - part) / T::kVec % kThreads == threadIdx.x)
+        h.each([&](float v, uint32_t i, uint32_t e) {
+            const uint32_t j = h.first(part, i);
+            if (j < tok && tok < j + T::kVec && j + e >= tok && v == zt) --above;
+        });
+    s = wave_sum(s);
+    t = wave_sum(t);
+    above = wave_sum(above);
+    if ((threadIdx.x & 63u) == 0) {
+        const float f = __builtin_amdgcn_exp2f(-shift);
+        wave_stat[threadIdx.x >> 6] = PartStat{m, s * f, f * fmaf(-shift, s, t), above};
     }
-    s = wg_sum<kWaves>(s, red);
-    t = wg_sum<kWaves>(t, red);
-    above = wg_sum<kWaves>(above, red);  // below 2^24 by its parts' sizes up to that vocabulary
-    const bool broken = !(s >= 0.0f) || s == INFINITY;
-    const bool empty = s == 0.0f;
-    const float ln_s = logf(s);
-    const float nan = __builtin_nanf("");
-    if (threadIdx.x == 0) {
-        float lp = empty ? -INFINITY : scaled(zt, m, g.two_over_tau) - ln_s;
-        const float h = broken ? nan : empty ? 0.0f : ln_s - t / s;
+    if constexpr (kTop) {
+        if (threadIdx.x == 0) found = 0;
+        lane_key[threadIdx.x] = ordered(lane_max);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.two_over_tau, true);
+    if constexpr (!kTop) return;
+
+    // a value that at least `top` lanes reach: every wave finds the same one
+    uint32_t key[kWaves], high = 0, low = ~0u, there = 0;
+    for (uint32_t i = 0; i < kWaves; ++i) {
+        key[i] = lane_key[64 * i + (threadIdx.x & 63u)];
+        const bool some = key[i] > kOrderedMasked;
+        there += __popcll(__ballot(some));
+        high = max(high, key[i]);
+        low = min(low, some ? key[i] : ~0u);
+    }
+    uint32_t cut = kOrderedMasked + 1;
+    if (there >= g.top) {
+        high = wave_max(high);
+        cut = wave_min(low);
+        while (cut < high) {
+            const uint32_t mid = high - (high - cut) / 2;
+            uint32_t n = 0;
+            for (uint32_t i = 0; i < kWaves; ++i) n += __popcll(__ballot(key[i] >= mid));
+            if (n >= g.top) {
+                cut = mid;
+                if (n <= g.top + g.top / 4 + 2) break;
+            } else {
+                high = mid - 1;
+            }
+        }
+    }
+    uint2 *out = g.candidate + static_cast<uint64_t>(blockIdx.x) * g.room;
+    const float least = from_ordered(cut);
+    if (lane_max >= least)
+        h.each([&](float v, uint32_t i, uint32_t e) {
+            if (v >= least) {
+                const uint32_t slot = atomicAdd(&found, 1u);
+                if (slot < g.room) out[slot] = uint2{ordered(v), h.first(part, i) + e};
+            }
+        });
+    __syncthreads();
+    uint32_t n = found;
+    if (n > g.room) {  // equal values, or a few lanes with all the large ones
+        __syncthreads();
+        if (threadIdx.x == 0) found = 0;
+        uint32_t lo = cut, hi = 0xFF800000u;  // ordered bits of +inf
+        while (lo < hi) {
+            const uint32_t mid = hi - (hi - lo) / 2;
+            const float at = from_ordered(mid);
+            if (wg_count(h, part, counts, [&](float v, uint32_t) { return v >= at; }) >= g.top)
+                lo = mid;
+            else
+                hi = mid - 1;
+        }
+        const float last = from_ordered(lo);
+        const uint32_t larger = wg_count(h, part, counts, [&](float v, uint32_t) { return v > last; });
+        uint32_t from = part, to = part + kPart - 1;
+        while (from < to) {  // the index up to which equal ones fill the rest
+            const uint32_t mid = from + (to - from) / 2;
+            if (larger + wg_count(h, part, counts,
+                                  [&](float v, uint32_t j) { return v == last && j <= mid; }) >= g.top)
+                to = mid;
+            else
+                from = mid + 1;
+        }
+        __syncthreads();
+        h.each([&](float v, uint32_t i, uint32_t e) {
+            const uint32_t j = h.first(part, i) + e;
+            if (v > last || (v == last && j <= to)) {
+                const uint32_t slot = atomicAdd(&found, 1u);
+                if (slot < g.room) out[slot] = uint2{ordered(v), j};
+            }
+        });
+        __syncthreads();
+        n = min(found, g.room);
+    }
+    if (threadIdx.x == 0) g.count[blockIdx.x] = n;
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void logprob_part_kernel(LogprobArgs g) {
+    logprob_part<T, false>(g);
+}
+template <class T>
+__global__ __launch_bounds__(kThreads) void logprob_top_kernel(LogprobArgs g) {
+    logprob_part<T, true>(g);
+}
+
+constexpr uint32_t kJoin = 2048;  // candidates that the join holds at once
+
+// Keeps the `top` largest of the n candidates in key[], idx[] (LDS, one wave),
+// largest first and equal ones by index, and returns how many there are.  The
+// workgroup is one wave: a barrier orders its LDS accesses, no more.
+__device__ uint32_t keep_top(uint32_t *key, uint32_t *idx, uint32_t n, uint32_t top) {
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint64_t below = (1ull << lane) - 1;
+    // few enough to be ordered by counting
+    const uint32_t few = max(64u, top + top / 8);
+    if (n > few) {
+        uint32_t lo = ~0u, hi = 0;
+        for (uint32_t i = lane; i < n; i += 64) {
+            lo = min(lo, key[i]);
+            hi = max(hi, key[i]);
+        }
+        lo = wave_min(lo);
+        hi = wave_max(hi);
+        uint32_t got = n;
+        while (lo < hi && got > few) {
+            const uint32_t mid = hi - (hi - lo) / 2;
+            uint32_t c = 0;
+            for (uint32_t i = lane; i < n; i += 64) c += key[i] >= mid ? 1u : 0u;
+            c = wave_sum(c);
+            if (c >= top) {
+                lo = mid;
+                got = c;
+            } else {
+                hi = mid - 1;
+            }
+        }
+        uint32_t last = ~0u;  // the index up to which those equal to lo are kept
+        if (got > few) {
+            uint32_t from = 0, to = ~0u;
+            while (from < to) {
+                const uint32_t mid = from + (to - from) / 2;
+                uint32_t c = 0;
+                for (uint32_t i = lane; i < n; i += 64)
+                    c += key[i] > lo || (key[i] == lo && idx[i] <= mid) ? 1u : 0u;
+                if (wave_sum(c) >= top)
+                    to = mid;
+                else
+                    from = mid + 1;
+            }
+            last = to;
+        }
+        // to the front, in place: what is written lies at or before what was read
+        uint32_t kept = 0;
+        for (uint32_t i = 0; i < n; i += 64) {
+            const bool in = i + lane < n;
+            const uint32_t k = in ? key[i + lane] : 0, j = in ? idx[i + lane] : 0;
+            const bool keep = in && (k > lo || (k == lo && j <= last));
+            const uint64_t all = __ballot(keep);
+            __syncthreads();
+            if (keep) {
+                const uint32_t at = kept + __popcll(all & below);
+                key[at] = k;
+                idx[at] = j;
+            }
+            __syncthreads();
+            kept += __popcll(all);
+        }
+        n = kept;
+    }
+    // a candidate's place is the number of larger ones; at most 3 a lane
+    constexpr uint32_t kMost = (DF11_MAX_TOP + DF11_MAX_TOP / 8 + 63) / 64;
+    uint32_t k[kMost], j[kMost], place[kMost];
+#pragma unroll
+    for (uint32_t e = 0; e < kMost; ++e) {
+        const uint32_t i = 64 * e + lane;
+        k[e] = i < n ? key[i] : 0;
+        j[e] = i < n ? idx[i] : ~0u;
+        place[e] = 0;
+    }
+    for (uint32_t i = 0; i < n; ++i) {
+        const uint32_t ki = key[i], ji = idx[i];
+#pragma unroll
+        for (uint32_t e = 0; e < kMost; ++e)
+            place[e] += ki > k[e] || (ki == k[e] && ji < j[e]) ? 1u : 0u;
+    }
+    __syncthreads();
+#pragma unroll
+    for (uint32_t e = 0; e < kMost; ++e)
+        if (64 * e + lane < n && place[e] < top) {
+            key[place[e]] = k[e];
+            idx[place[e]] = j[e];
+        }
+    __syncthreads();
+    return min(n, top);
+}
+
+// One wave per row.
+template <class T>
+__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs g) {
+    __shared__ uint32_t key[kJoin], idx[kJoin], filled[64];
+    const uint64_t row = blockIdx.x;
+    const uint32_t lane = threadIdx.x;
+    const int64_t token = g.tokens ? g.tokens[row] : -1;
+    const bool asked = token >= 0 && token < g.vocab;
+    const float zt = asked ? T::load((static_cast<const typename T::raw *>(g.logits) + row * g.stride)[token]) : 0.0f;
+    uint64_t above;
+    const PartStat p = join_parts(g.stat + row * g.parts, g.parts, g.two_over_tau, true, &above);
+    const bool broken = !(p.s >= 0.0f) || p.s == INFINITY;
+    const bool empty = p.s == 0.0f;
+    const float ln_s = logf(p.s), nan = __builtin_nanf("");
+    if (lane == 0) {
+        float lp = empty ? -INFINITY : scaled(zt, p.m, g.two_over_tau) - ln_s;
+        const float h = broken ? nan : empty ? 0.0f : ln_s - kLn2 * (p.t / p.s);
         if (token < 0) lp = 0.0f;
         if ((token >= 0 && !asked) || broken) lp = nan;
         if (g.logprob) g.logprob[row] = lp;
         if (g.rank) g.rank[row] = asked && !broken ? static_cast<int64_t>(above) : -1;
         if (g.entropy) g.entropy[row] = h;
-        if (g.stats) {
-            g.stats[4 * row] = m;
-            g.stats[4 * row + 1] = ln_s;
-            g.stats[4 * row + 2] = h;
-            g.stats[4 * row + 3] = lp;
-        }
+        if (g.stats) *reinterpret_cast<float4 *>(g.stats + 4 * row) = float4{p.m, ln_s, h, lp};
     }
-    // one alternative a pass: the largest after the last one
-    float last_v = INFINITY;
-    uint32_t last_i = 0;
-    for (uint32_t k = 0; k < g.top; ++k) {
-        float v = -INFINITY;
-        uint32_t i = ~0u;
-        for (uint32_t j = threadIdx.x; j < g.vocab; j += kThreads) {
-            const float w = T::load(z[j]);
-            const bool after = k == 0 || w < last_v || (w == last_v && j > last_i);
-            if (after && w > v) {
-                v = w;
-                i = j;
-            }
-        }
-        best_v[threadIdx.x] = v;
-        best_i[threadIdx.x] = i;
+    if (!g.top) return;
+    // the parts' candidates lie `room` apart: lanes run over all the slots, a
+    // batch of loads at a time, and take those that are filled
+    constexpr uint32_t kBatch = 16;
+    const uint64_t below = (1ull << lane) - 1;
+    uint32_t n = 0;
+    for (uint32_t q0 = 0; q0 < g.parts; q0 += 64) {
+        const uint32_t here = min(64u, g.parts - q0);
+        const uint64_t first = row * g.parts + q0;
         __syncthreads();
-        for (uint32_t d = kThreads / 2; d; d >>= 1) {
-            if (threadIdx.x < d) {
-                const float w = best_v[threadIdx.x + d];
-                const uint32_t j = best_i[threadIdx.x + d];
-                if (w > best_v[threadIdx.x] || (w == best_v[threadIdx.x] && j < best_i[threadIdx.x])) {
-                    best_v[threadIdx.x] = w;
-                    best_i[threadIdx.x] = j;
+        if (lane < here) filled[lane] = min(g.count[first + lane], g.room);
+        __syncthreads();
+        const uint2 *from = g.candidate + first * g.room;
+        uint32_t q = lane / g.room, r = lane % g.room;
+        for (uint32_t f = lane; f - lane < here * g.room; f += 64 * kBatch) {
+            uint2 v[kBatch];
+            bool in[kBatch];
+#pragma unroll
+            for (uint32_t e = 0; e < kBatch; ++e) {
+                in[e] = q < here && r < filled[q < here ? q : 0];
+                if (in[e]) v[e] = from[f + 64 * e];
+                r += 64;
+                if (r >= g.room) {  // room > 64
+                    r -= g.room;
+                    ++q;
                 }
+            }
+            if (n + 64 * kBatch > kJoin) n = keep_top(key, idx, n, g.top);
+#pragma unroll
+            for (uint32_t e = 0; e < kBatch; ++e) {
+                const uint64_t all = __ballot(in[e]);
+                if (in[e]) {
+                    const uint32_t at = n + __popcll(all & below);
+                    key[at] = v[e].x;
+                    idx[at] = v[e].y;
+                }
+                n += __popcll(all);
             }
             __syncthreads();
         }
-        last_v = best_v[0];
-        last_i = best_i[0];
-        const bool none = last_i == ~0u;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            g.top_logprob[row * g.top + k] =
-                broken ? nan : none ? -INFINITY : scaled(last_v, m, g.two_over_tau) - ln_s;
-            g.top_index[row * g.top + k] = broken || none ? -1 : static_cast<int64_t>(last_i);
-        }
+    }
+    n = keep_top(key, idx, n, g.top);
+    for (uint32_t k = lane; k < g.top; k += 64) {
+        const bool some = k < n;
+        g.top_logprob[row * g.top + k] =
+            broken ? nan : some ? scaled(from_ordered(key[k]), p.m, g.two_over_tau) - ln_s : -INFINITY;
+        g.top_index[row * g.top + k] = broken || !some ? -1 : static_cast<int64_t>(idx[k]);
     }
 }
 
@@ -121,141 +522,219 @@ struct LogprobGradArgs {
     float two_over_tau;
 };
 
+// Writes f(value, index) for the values of a part.
+template <class T, class F>
+__device__ void store_part(const Held<T> &h, typename T::raw *out, uint32_t part, uint32_t vocab, F f) {
+#pragma unroll
+    for (uint32_t i = 0; i < Held<T>::kVecs; ++i) {
+        const uint32_t j = Held<T>::first(part, i);
+        typename T::raw r[T::kVec];
+#pragma unroll
+        for (uint32_t e = 0; e < T::kVec; ++e) r[e] = T::store(f(T::get(h.q[i], e), j + e));
+        if (j + T::kVec <= vocab) {
+            store16(out + j, __builtin_bit_cast(uint4, r));
+        } else {
+#pragma unroll
+            for (uint32_t e = 0; e < T::kVec; ++e)
+                if (j + e < vocab) out[j + e] = r[e];
+        }
+    }
+}
+
+// grad = p (A + B y), y = log2 p: the formula with its factors drawn together.
+// The token's value, the only other one, is written by the lane that holds it.
 template <class T>
 __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs g) {
     const uint64_t row = blockIdx.x / g.parts;
-    const uint32_t from = (blockIdx.x % g.parts) * kPart;
-    const uint32_t to = min(g.vocab, from + kPart);
-    const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
+    const uint32_t part = (blockIdx.x % g.parts) * kPart;
+    Held<T> h;
+    h.load(static_cast<const typename T::raw *>(g.logits) + row * g.stride, part, g.vocab);
     auto *out = static_cast<typename T::raw *>(g.grad) + row * g.grad_stride;
     const int64_t token = g.tokens ? g.tokens[row] : -1;
-    const float m = g.stats[4 * row], ln_s = g.stats[4 * row + 1], h = g.stats[4 * row + 2];
+    const float4 st = *reinterpret_cast<const float4 *>(g.stats + 4 * row);
+    const float m = st.x, ln_s = st.y, entropy = st.z;
+    const float over_tau = 0.5f * g.two_over_tau;
     float gl = g.grad_logprob && token >= 0 ? g.grad_logprob[row] : 0.0f;
     if (token >= static_cast<int64_t>(g.vocab)) gl = __builtin_nanf("");
     const float ge = g.grad_entropy ? g.grad_entropy[row] : 0.0f;
     const bool empty = ln_s == -INFINITY;
-    for (uint32_t j = from + threadIdx.x; j < to; j += kThreads) {
-        const float lp = scaled(T::load(z[j]), m, g.two_over_tau) - ln_s;
-        const float p = expf(lp);
-        float d = -p * (gl + ge * (fmaxf(lp, -200.0f) + h));
-        if (token == static_cast<int64_t>(j)) d += gl;
-        out[j] = T::store(empty ? 0.0f : d * (0.5f * g.two_over_tau));
-    }
+    const float A = -over_tau * fmaf(ge, entropy, gl), B = -over_tau * ge * kLn2;
+    const float hit = over_tau * gl, log2_s = ln_s * kLog2e;
+    const uint32_t tok = token >= 0 && token < g.vocab ? static_cast<uint32_t>(token) : ~0u;
+    store_part(h, out, part, g.vocab, [&](float v, uint32_t j) {
+        const float y = fmaf(scaled(v, m, g.two_over_tau), kLog2e, -log2_s);
+        const float d = __builtin_amdgcn_exp2f(y) * fmaf(B, fmaxf(y, -300.0f), A);
+        return empty ? 0.0f : j == tok ? d + hit : d;
+    });
 }
 
+// ---------------------------------------------------------------- distillation
 struct DistillArgs {
     const void *logits;
     void *grad;
     const int64_t *index;
     const float *teacher, *weight;
+    PartStat *stat;
     float *loss, *stats;
     uint64_t stride, grad_stride;
-    uint32_t vocab, top, tail, parts;
+    uint32_t vocab, parts, top, tail;
     float two_over_tau;
 };
 
-// The teacher's entries of a row in LDS: place (~0 where there is none) and
-// probability.  Returns whether an entry is bad.
-template <class A>
-__device__ bool load_teacher(const A &g, uint64_t row, uint32_t *place, float *prob) {
-    bool bad = false;
+// Whether the teacher's entry is there, and whether it is out of range.
+__device__ bool named(int64_t place) { return place >= 0; }
+__device__ bool bad_entry(int64_t place, float logprob, uint32_t vocab) {
+    return place >= 0 && (place >= static_cast<int64_t>(vocab) || !(logprob < INFINITY));
+}
+
+// sum e and the sum over the places that the teacher does not name: these are
+// a bit for each value of the part in LDS (1 KB), a lane reads its vector's.
+// The second sum is kept beside the first, not taken from it by subtraction:
+// where the named places have nearly all the probability nothing would be left.
+template <class T>
+__global__ __launch_bounds__(kThreads) void distill_part_kernel(DistillArgs g) {
+    __shared__ PartStat wave_stat[kWaves];
+    __shared__ uint32_t bits[kPart / 32];
+    const uint64_t row = blockIdx.x / g.parts;
+    const uint32_t part = (blockIdx.x % g.parts) * kPart;
+    Held<T> h;
+    h.load(static_cast<const typename T::raw *>(g.logits) + row * g.stride, part, g.vocab);
+    static_assert(kPart / 32 == kThreads, "a word a thread");
+    bits[threadIdx.x] = 0;
+    __syncthreads();
     for (uint32_t k = threadIdx.x; k < g.top; k += kThreads) {
         const int64_t i = g.index[row * g.top + k];
-        const float lp = g.teacher[row * g.top + k];
-        if (i >= 0 && (i >= static_cast<int64_t>(g.vocab) || !(lp < INFINITY))) bad = true;
-        place[k] = i < 0 ? ~0u : static_cast<uint32_t>(i);
-        prob[k] = i < 0 ? 0.0f : expf(lp);
+        if (i >= part && i < int64_t{part} + kPart)
+            atomicOr(&bits[(i - part) >> 5], 1u << ((i - part) & 31));
     }
-    return __syncthreads_or(bad);
+    __syncthreads();
+    const float m = fmaxf(wave_max(h.max()), kLowest);
+    float s = 0.0f, t = 0.0f;
+    uint32_t mask = 0;
+    const auto add = [&](float, float e, float, uint32_t i, uint32_t k) {
+        if (k == 0) {
+            const uint32_t at = h.first(0, i);
+            mask = bits[at >> 5] >> (at & 31u);
+        }
+        s += e;
+        t += mask >> k & 1u ? 0.0f : e;
+    };
+    const float shift = each_exp(h, m, g.two_over_tau, add);
+    s = wave_sum(s);
+    t = wave_sum(t);
+    if ((threadIdx.x & 63u) == 0) {
+        const float f = __builtin_amdgcn_exp2f(-shift);
+        wave_stat[threadIdx.x >> 6] = PartStat{m, s * f, t * f, 0};
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.two_over_tau, false);
 }
 
+// One wave per row: the loss from the parts and the student's values at the
+// named places, and what the gradient needs: m, ln S, the factor of q where no
+// place is named, and that of the teacher's probability (below 0: no gradient).
 template <class T>
-__global__ __launch_bounds__(kThreads) void distill_rows_kernel(DistillArgs g) {
-    __shared__ float red[kWaves];
-    __shared__ uint32_t place[DF11_MAX_TOP];
-    __shared__ float prob[DF11_MAX_TOP];
+__global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     const uint64_t row = blockIdx.x;
+    const uint32_t lane = threadIdx.x;
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
-    const bool bad = load_teacher(g, row, place, prob);
-    float m = -3.402823466e38f;
-    for (uint32_t j = threadIdx.x; j < g.vocab; j += kThreads) m = fmaxf(m, T::load(z[j]));
-    m = wg_max<kWaves>(m, red);
-    float s = 0.0f, rest = 0.0f;
-    for (uint32_t j = threadIdx.x; j < g.vocab; j += kThreads) {
-        const float e = expf(scaled(T::load(z[j]), m, g.two_over_tau));
-        bool named = false;
-        for (uint32_t k = 0; k < g.top; ++k) named |= place[k] == j;
-        s += e;
-        rest += named ? 0.0f : e;
+    constexpr uint32_t kMost = DF11_MAX_TOP / 64;
+    float lt[kMost], p[kMost], v[kMost];
+    bool some = false, bad = false;
+    float mass = 0.0f;
+#pragma unroll
+    for (uint32_t e = 0; e < kMost; ++e) {
+        const uint32_t k = 64 * e + lane;
+        const int64_t at = k < g.top ? g.index[row * g.top + k] : -1;
+        lt[e] = k < g.top ? g.teacher[row * g.top + k] : 0.0f;
+        some |= named(at);
+        bad |= bad_entry(at, lt[e], g.vocab);
+        p[e] = named(at) ? expf(lt[e]) : 0.0f;
+        v[e] = named(at) && at < g.vocab ? T::load(z[at]) : 0.0f;
+        mass += p[e];
     }
-    s = wg_sum<kWaves>(s, red);
-    rest = wg_sum<kWaves>(rest, red);
-    const float ln_s = logf(s);
-    float mass = 0.0f, some = 0.0f;
-    for (uint32_t k = threadIdx.x; k < g.top; k += kThreads) {
-        mass += prob[k];
-        some += place[k] != ~0u ? 1.0f : 0.0f;
-    }
-    mass = wg_sum<kWaves>(mass, red);
-    some = wg_sum<kWaves>(some, red);
+    some = __any(some);
+    bad = __any(bad);
+    mass = wave_sum(mass);
+    uint64_t none;
+    const PartStat st = join_parts(g.stat + row * g.parts, g.parts, g.two_over_tau, false, &none);
+    const float ln_s = logf(st.s);
     const float scale = g.tail ? 1.0f : 1.0f / mass, ln_mass = g.tail ? 0.0f : logf(mass);
     float loss = 0.0f;
-    if (!bad)
-        for (uint32_t k = threadIdx.x; k < g.top; k += kThreads)
-            if (prob[k] > 0.0f) {
-                const float lq = scaled(T::load(z[place[k]]), m, g.two_over_tau) - ln_s;
-                loss += prob[k] * scale * (g.teacher[row * g.top + k] - ln_mass - lq);
-            }
-    loss = wg_sum<kWaves>(loss, red);
-    if (threadIdx.x == 0) {
-        const float left = rest / s, r = fmaxf(0.0f, 1.0f - mass);
-        float other = 1.0f, inv_mass = scale;
-        if (g.tail) {
-            if (r > 0.0f) loss += r * (logf(r) - logf(left));
-            other = r > 0.0f ? (left > 0.0f ? 1.0f - r / left : 0.0f) : 1.0f;
-        }
-        if (s == 0.0f) {
-            inv_mass = -1.0f;
-            loss = INFINITY;
-        }
-        if (!(s >= 0.0f) || s == INFINITY) loss = other = __builtin_nanf("");
-        if (some == 0.0f || (!g.tail && mass == 0.0f)) {
-            loss = 0.0f;
-            inv_mass = -1.0f;
-        }
-        if (bad) loss = other = inv_mass = __builtin_nanf("");
-        g.loss[row] = loss;
-        g.stats[4 * row] = m;
-        g.stats[4 * row + 1] = ln_s;
-        g.stats[4 * row + 2] = other;
-        g.stats[4 * row + 3] = inv_mass;
+#pragma unroll
+    for (uint32_t e = 0; e < kMost; ++e)
+        if (p[e] > 0.0f)
+            loss += p[e] * scale * (lt[e] - ln_mass - (scaled(v[e], st.m, g.two_over_tau) - ln_s));
+    loss = wave_sum(loss);
+    if (lane) return;
+    const float left = st.t / st.s, r = fmaxf(0.0f, 1.0f - mass), nan = __builtin_nanf("");
+    float other = 1.0f, factor = scale;
+    if (g.tail && r > 0.0f) {
+        loss += r * (logf(r) - logf(left));
+        other = left > 0.0f ? 1.0f - r / left : 0.0f;
     }
+    if (st.s == 0.0f) {
+        factor = -1.0f;
+        loss = INFINITY;
+    }
+    if (!(st.s >= 0.0f) || st.s == INFINITY) loss = other = nan;
+    if (!some || (!g.tail && mass == 0.0f)) {
+        loss = 0.0f;
+        factor = -1.0f;
+    }
+    if (bad) loss = other = factor = nan;
+    g.loss[row] = loss;
+    *reinterpret_cast<float4 *>(g.stats + 4 * row) = float4{st.m, ln_s, other, factor};
 }
 
+// q times its factor everywhere, then the few named places of the part once
+// more, q minus the teacher's probability.  Their logits are read before the
+// first store, so that the gradient may replace the logits.
 template <class T>
 __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs g) {
-    __shared__ uint32_t place[DF11_MAX_TOP];
-    __shared__ float prob[DF11_MAX_TOP];
+    __shared__ uint32_t place[DF11_MAX_TOP], many;
     const uint64_t row = blockIdx.x / g.parts;
-    const uint32_t from = (blockIdx.x % g.parts) * kPart;
-    const uint32_t to = min(g.vocab, from + kPart);
+    const uint32_t part = (blockIdx.x % g.parts) * kPart;
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
     auto *out = static_cast<typename T::raw *>(g.grad) + row * g.grad_stride;
-    load_teacher(g, row, place, prob);
-    const float m = g.stats[4 * row], ln_s = g.stats[4 * row + 1];
-    const float other = g.stats[4 * row + 2], inv_mass = g.stats[4 * row + 3];
+    Held<T> h;
+    h.load(z, part, g.vocab);
+    const float4 st = *reinterpret_cast<const float4 *>(g.stats + 4 * row);
+    const float m = st.x, log2_s = st.y * kLog2e, other = st.z, factor = st.w;
     const float w = (g.weight ? g.weight[row] : 1.0f) * (0.5f * g.two_over_tau);
-    for (uint32_t j = from + threadIdx.x; j < to; j += kThreads) {
-        const float q = expf(scaled(T::load(z[j]), m, g.two_over_tau) - ln_s);
-        bool named = false;
-        float p = 0.0f;
-        for (uint32_t k = 0; k < g.top; ++k)
-            if (place[k] == j) {
-                named = true;
-                p += prob[k];
-            }
-        const float d = inv_mass != inv_mass ? inv_mass : named ? q - p * inv_mass : q * other;
-        out[j] = T::store(inv_mass < 0.0f ? 0.0f : d * w);
+    const bool none = factor < 0.0f;  // not for a NaN
+    const float every = factor != factor ? factor : other * w;
+
+    // a thread an entry; the places of this part go to LDS, so that an entry
+    // sees whether its place is named again
+    static_assert(DF11_MAX_TOP <= kThreads, "a thread an entry");
+    if (threadIdx.x == 0) many = 0;
+    __syncthreads();
+    const int64_t at = threadIdx.x < g.top ? g.index[row * g.top + threadIdx.x] : -1;
+    const bool mine = at >= part && at < min(int64_t{part} + kPart, int64_t{g.vocab});
+    if (mine) place[atomicAdd(&many, 1u)] = static_cast<uint32_t>(at);
+    __syncthreads();
+    float value = 0.0f, target = 0.0f;
+    if (mine) {
+        value = T::load(z[at]);
+        target = expf(g.teacher[row * g.top + threadIdx.x]);
+        uint32_t same = 0;
+        for (uint32_t k = 0; k < many; ++k) same += place[k] == at ? 1u : 0u;
+        if (same > 1) {  // all its entries, in their order: each of them writes the same
+            target = 0.0f;
+            for (uint32_t k = 0; k < g.top; ++k)
+                if (g.index[row * g.top + k] == at) target += expf(g.teacher[row * g.top + k]);
+        }
+    }
+    __syncthreads();
+    store_part(h, out, part, g.vocab, [&](float v, uint32_t) {
+        const float y = fmaf(scaled(v, m, g.two_over_tau), kLog2e, -log2_s);
+        return none ? 0.0f : __builtin_amdgcn_exp2f(y) * every;
+    });
+    __syncthreads();
+    if (mine && !none) {
+        const float y = fmaf(scaled(value, m, g.two_over_tau), kLog2e, -log2_s);
+        out[at] = T::store((__builtin_amdgcn_exp2f(y) - target * factor) * w);
     }
 }
 
@@ -288,6 +767,22 @@ int check_grad(const void *logits, const void *grad, uint32_t dtype, uint64_t ro
     return DF11_OK;
 }
 
+int check_workspace(const void *ws, uint64_t have, uint64_t need) {
+    if (have < need) return DF11_E_BUFFER_TOO_SMALL;
+    return need && (!ws || misaligned(ws, 16)) ? DF11_E_INVALID_ARG : DF11_OK;
+}
+
+// The workspace of `all` parts: their statistics, counts and candidates.
+struct Space {
+    uint64_t count, candidate, bytes;
+};
+Space logprob_space(uint64_t all, uint32_t top) {
+    Space s{sizeof(PartStat) * all, 0, 0};
+    s.candidate = s.count + (top ? (4 * all + 15) / 16 * 16 : 0);
+    s.bytes = s.candidate + sizeof(uint2) * room_of(top) * all;
+    return s;
+}
+
 #define DF11_BY_DTYPE(dtype, kernel, grid, block, stream, args)                            \
     do {                                                                                   \
         if ((dtype) == DF11_F32)                                                           \
@@ -308,7 +803,7 @@ int df11_logprobs_workspace_bytes(uint32_t dtype, uint64_t rows, uint32_t vocab,
     static const float some = 0.0f;
     const int rc = check_logits(&some, dtype, rows, vocab, vocab);
     if (rc) return rc;
-    *bytes = 0;
+    *bytes = logprob_space(rows * parts_of(vocab), top).bytes;
     return DF11_OK;
 }
 
@@ -328,11 +823,20 @@ int df11_logprobs(const void *logits, uint32_t dtype, uint64_t rows, uint32_t vo
         misaligned(logprob, 4) || misaligned(entropy, 4) || misaligned(top_logprob, 4) ||
         misaligned(stats, 16))
         return DF11_E_INVALID_ARG;
-    (void)workspace;
-    (void)workspace_bytes;
-    LogprobArgs g{logits, tokens, logprob, entropy, top_logprob, stats, rank, top_index,
-                  row_stride, vocab, top, 2.0f / temperature};
-    DF11_BY_DTYPE(dtype, logprob_rows_kernel, rows, kThreads, stream, g);
+    const uint32_t parts = parts_of(vocab);
+    const Space s = logprob_space(rows * parts, top);
+    if ((rc = check_workspace(workspace, workspace_bytes, s.bytes))) return rc;
+    char *ws = static_cast<char *>(workspace);
+    LogprobArgs g{logits, tokens, reinterpret_cast<PartStat *>(ws),
+                  reinterpret_cast<uint32_t *>(ws + s.count),
+                  reinterpret_cast<uint2 *>(ws + s.candidate), logprob, entropy, top_logprob, stats,
+                  rank, top_index, row_stride, vocab, parts, top, room_of(top), 2.0f / temperature};
+    if (top)
+        DF11_BY_DTYPE(dtype, logprob_top_kernel, rows * parts, kThreads, stream, g);
+    else
+        DF11_BY_DTYPE(dtype, logprob_part_kernel, rows * parts, kThreads, stream, g);
+    if ((rc = launched())) return rc;
+    DF11_BY_DTYPE(dtype, logprob_join_kernel, rows, 64, stream, g);
     return launched();
 }
 
@@ -362,7 +866,7 @@ int df11_distill_workspace_bytes(uint32_t dtype, uint64_t rows, uint32_t vocab, 
     static const float some = 0.0f;
     const int rc = check_logits(&some, dtype, rows, vocab, vocab);
     if (rc) return rc;
-    *bytes = 0;
+    *bytes = sizeof(PartStat) * rows * parts_of(vocab);
     return DF11_OK;
 }
 
@@ -381,13 +885,17 @@ int df11_distill(const void *logits, uint32_t dtype, uint64_t rows, uint32_t voc
     if (misaligned(teacher_index, 8) || misaligned(teacher_logprob, 4) || misaligned(weight, 4) ||
         misaligned(loss, 4) || misaligned(stats, 16))
         return DF11_E_INVALID_ARG;
-    (void)workspace;
-    (void)workspace_bytes;
-    DistillArgs g{logits, grad, teacher_index, teacher_logprob, weight, loss, stats, row_stride,
-                  grad_stride, vocab, top, tail, parts_of(vocab), 2.0f / temperature};
-    DF11_BY_DTYPE(dtype, distill_rows_kernel, rows, kThreads, stream, g);
+    const uint32_t parts = parts_of(vocab);
+    rc = check_workspace(workspace, workspace_bytes, sizeof(PartStat) * rows * parts);
+    if (rc) return rc;
+    DistillArgs g{logits, grad, teacher_index, teacher_logprob, weight,
+                  static_cast<PartStat *>(workspace), loss, stats, row_stride, grad_stride, vocab,
+                  parts, top, tail, 2.0f / temperature};
+    DF11_BY_DTYPE(dtype, distill_part_kernel, rows * parts, kThreads, stream, g);
+    if ((rc = launched())) return rc;
+    DF11_BY_DTYPE(dtype, distill_join_kernel, rows, 64, stream, g);
     if ((rc = launched()) || !grad) return rc;
-    DF11_BY_DTYPE(dtype, distill_grad_kernel, rows * g.parts, kThreads, stream, g);
+    DF11_BY_DTYPE(dtype, distill_grad_kernel, rows * parts, kThreads, stream, g);
     return launched();
 }
 
@@ -406,9 +914,9 @@ int df11_distill_backward(const void *logits, uint32_t dtype, uint64_t rows, uin
     if (misaligned(teacher_index, 8) || misaligned(teacher_logprob, 4) ||
         misaligned(grad_loss, 4) || misaligned(stats, 16))
         return DF11_E_INVALID_ARG;
-    DistillArgs g{logits, grad, teacher_index, teacher_logprob, grad_loss, nullptr,
-                  const_cast<float *>(stats), row_stride, grad_stride, vocab, top, tail,
-                  parts_of(vocab), 2.0f / temperature};
+    DistillArgs g{logits, grad, teacher_index, teacher_logprob, grad_loss, nullptr, nullptr,
+                  const_cast<float *>(stats), row_stride, grad_stride, vocab, parts_of(vocab), top,
+                  tail, 2.0f / temperature};
     DF11_BY_DTYPE(dtype, distill_grad_kernel, rows * g.parts, kThreads, stream, g);
     return launched();
 }
