@@ -5,8 +5,8 @@
 // All of them are bound by reading the logits (and writing the gradient): a
 // row is cut into parts of 8192 values, a workgroup takes one part and holds it
 // in registers (32 values a lane, all loads issued at once), so the logits are
-// read once however many statistics are wanted.  One wave per row then joins
-// the parts:
+// read once however many statistics are wanted.  A second kernel joins the parts
+// of a row:
 //   - the maximum first, then sum exp2((z - max) log2e / tau) with that maximum
 //     fixed, per wave; waves and parts are joined by scaling with the
 //     exponential of the difference of their maxima;
@@ -46,6 +46,12 @@ __device__ float from_ordered(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 constexpr uint32_t kOrderedMasked = 0x007FFFFFu;  // of -inf
+
+// How many lanes below this one have their bit set.
+__device__ uint32_t before(uint64_t all) {
+    return __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(all >> 32),
+                                     __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(all), 0u));
+}
 
 // The next larger float; of -inf the lowest finite one.
 __device__ float above_of(float v) {
@@ -200,11 +206,8 @@ struct LogprobArgs {
 // some, so that equal neighbours (bf16 has 8 bits of mantissa) fit.
 __host__ __device__ constexpr uint32_t room_of(uint32_t top) { return top ? 2 * top + 64 : 0; }
 
-// How many of a workgroup's values satisfy f(value, index), by every thread.
-template <class T, class F>
-__device__ uint32_t wg_count(const Held<T> &h, uint32_t part, uint32_t *lds, F f) {
-    uint32_t n = 0;
-    h.each([&](float v, uint32_t i, uint32_t e) { n += f(v, h.first(part, i) + e) ? 1u : 0u; });
+// A workgroup's sum of a count, by every thread.
+__device__ uint32_t wg_sum(uint32_t n, uint32_t *lds) {
     n = wave_sum(n);
     __syncthreads();
     if ((threadIdx.x & 63u) == 0) lds[threadIdx.x >> 6] = n;
@@ -214,11 +217,90 @@ __device__ uint32_t wg_count(const Held<T> &h, uint32_t part, uint32_t *lds, F f
     return n;
 }
 
+// Of 256 keys, one a lane in lane_key[], the largest that `top` of them reach,
+// or one that only some more do; 0 unmasked keys below `top`: the least of all
+// that are not masked.  Every wave finds the same, without a barrier.
+__device__ uint32_t reached_by(const uint32_t *lane_key, uint32_t top) {
+    uint32_t key[kWaves], high = 0, low = ~0u, there = 0;
+    for (uint32_t i = 0; i < kWaves; ++i) {
+        key[i] = lane_key[64 * i + (threadIdx.x & 63u)];
+        const bool some = key[i] > kOrderedMasked;
+        there += __popcll(__ballot(some));
+        high = max(high, key[i]);
+        low = min(low, some ? key[i] : ~0u);
+    }
+    if (there < top) return kOrderedMasked + 1;
+    high = wave_max(high);
+    uint32_t cut = wave_min(low);
+    while (cut < high) {
+        const uint32_t mid = high - (high - cut) / 2;
+        uint32_t n = 0;
+        for (uint32_t i = 0; i < kWaves; ++i) n += __popcll(__ballot(key[i] >= mid));
+        if (n >= top) {
+            cut = mid;
+            if (n <= top + top / 4 + 2) break;
+        } else {
+            high = mid - 1;
+        }
+    }
+    return cut;
+}
+
+// A part's `top` largest values, exactly, where more than fit reach `cut`: the
+// last of them by bisection over all values (not where `cut` is it already: equal
+// values), then the index up to which values equal to it are taken.  Reads the
+// part again: it is rare, and the registers it would need are not.
+template <class T>
+__device__ __attribute__((noinline)) void trim_part(const typename T::raw *z, uint32_t part,
+                                                    uint32_t vocab, uint32_t cut, uint32_t top,
+                                                    uint2 *out, uint32_t *lds) {
+    const uint32_t to = min(kPart, vocab - part);
+    z += part;
+    auto count = [&](auto f) {
+        uint32_t n = 0;
+#pragma unroll 8
+        for (uint32_t i = threadIdx.x; i < to; i += kThreads) n += f(T::load(z[i]), i) ? 1u : 0u;
+        return wg_sum(n, lds);
+    };
+    uint32_t lo = cut, hi = 0xFF800000u;  // ordered bits of +inf
+    float last = from_ordered(lo);
+    uint32_t larger = count([&](float v, uint32_t) { return v > last; });
+    while (lo < hi && larger >= top) {
+        const uint32_t mid = hi - (hi - lo) / 2;
+        const float at = from_ordered(mid);
+        if (count([&](float v, uint32_t) { return v >= at; }) >= top) {
+            lo = mid;
+            last = at;
+            larger = count([&](float v, uint32_t) { return v > last; });
+        } else {
+            hi = mid - 1;
+        }
+    }
+    uint32_t from = 0, until = kPart - 1;
+    while (from < until) {
+        const uint32_t mid = from + (until - from) / 2;
+        if (larger + count([&](float v, uint32_t i) { return v == last && i <= mid; }) >= top)
+            until = mid;
+        else
+            from = mid + 1;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) lds[0] = 0;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < to; i += kThreads) {
+        const float v = T::load(z[i]);
+        if (v > last || (v == last && i <= until)) {
+            const uint32_t slot = atomicAdd(&lds[0], 1u);
+            if (slot < top) out[slot] = uint2{ordered(v), part + i};
+        }
+    }
+}
+
 template <class T, bool kTop>
 __device__ void logprob_part(const LogprobArgs &g) {
     __shared__ PartStat wave_stat[kWaves];
-    __shared__ uint32_t lane_key[kThreads];
-    __shared__ uint32_t found, counts[kWaves];
+    __shared__ uint32_t lane_key[kTop ? kThreads : 1], counts[kWaves];
+    __shared__ uint2 list[kTop ? kWaves : 1][kTop ? room_of(DF11_MAX_TOP) : 1];
     const uint32_t row_parts = g.parts;
     const uint64_t row = blockIdx.x / row_parts;
     const uint32_t part = (blockIdx.x % row_parts) * kPart;
@@ -257,85 +339,39 @@ __device__ void logprob_part(const LogprobArgs &g) {
         const float f = __builtin_amdgcn_exp2f(-shift);
         wave_stat[threadIdx.x >> 6] = PartStat{m, s * f, f * fmaf(-shift, s, t), above};
     }
-    if constexpr (kTop) {
-        if (threadIdx.x == 0) found = 0;
-        lane_key[threadIdx.x] = ordered(lane_max);
-    }
+    if constexpr (kTop) lane_key[threadIdx.x] = ordered(lane_max);
     __syncthreads();
     if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.two_over_tau, true);
-    if constexpr (!kTop) return;
-
-    // a value that at least `top` lanes reach: every wave finds the same one
-    uint32_t key[kWaves], high = 0, low = ~0u, there = 0;
-    for (uint32_t i = 0; i < kWaves; ++i) {
-        key[i] = lane_key[64 * i + (threadIdx.x & 63u)];
-        const bool some = key[i] > kOrderedMasked;
-        there += __popcll(__ballot(some));
-        high = max(high, key[i]);
-        low = min(low, some ? key[i] : ~0u);
-    }
-    uint32_t cut = kOrderedMasked + 1;
-    if (there >= g.top) {
-        high = wave_max(high);
-        cut = wave_min(low);
-        while (cut < high) {
-            const uint32_t mid = high - (high - cut) / 2;
-            uint32_t n = 0;
-            for (uint32_t i = 0; i < kWaves; ++i) n += __popcll(__ballot(key[i] >= mid));
-            if (n >= g.top) {
-                cut = mid;
-                if (n <= g.top + g.top / 4 + 2) break;
-            } else {
-                high = mid - 1;
-            }
-        }
-    }
-    uint2 *out = g.candidate + static_cast<uint64_t>(blockIdx.x) * g.room;
-    const float least = from_ordered(cut);
-    if (lane_max >= least)
+    if constexpr (kTop) {
+        const uint32_t cut = reached_by(lane_key, g.top);
+        const float least = from_ordered(cut);
+        const uint32_t wave = threadIdx.x >> 6;
+        uint32_t n = 0;  // of this wave
         h.each([&](float v, uint32_t i, uint32_t e) {
-            if (v >= least) {
-                const uint32_t slot = atomicAdd(&found, 1u);
-                if (slot < g.room) out[slot] = uint2{ordered(v), h.first(part, i) + e};
+            const uint64_t all = __ballot(v >= least);
+            if (all) {
+                const uint32_t slot = n + before(all);
+                if (v >= least && slot < g.room)
+                    list[wave][slot] = uint2{ordered(v), h.first(part, i) + e};
+                n += __popcll(all);
             }
         });
-    __syncthreads();
-    uint32_t n = found;
-    if (n > g.room) {  // equal values, or a few lanes with all the large ones
+        if ((threadIdx.x & 63u) == 0) counts[wave] = n;
         __syncthreads();
-        if (threadIdx.x == 0) found = 0;
-        uint32_t lo = cut, hi = 0xFF800000u;  // ordered bits of +inf
-        while (lo < hi) {
-            const uint32_t mid = hi - (hi - lo) / 2;
-            const float at = from_ordered(mid);
-            if (wg_count(h, part, counts, [&](float v, uint32_t) { return v >= at; }) >= g.top)
-                lo = mid;
-            else
-                hi = mid - 1;
+        uint32_t at = 0, total = 0;
+        for (uint32_t w = 0; w < kWaves; ++w) {
+            at += w < wave ? counts[w] : 0;
+            total += counts[w];
         }
-        const float last = from_ordered(lo);
-        const uint32_t larger = wg_count(h, part, counts, [&](float v, uint32_t) { return v > last; });
-        uint32_t from = part, to = part + kPart - 1;
-        while (from < to) {  // the index up to which equal ones fill the rest
-            const uint32_t mid = from + (to - from) / 2;
-            if (larger + wg_count(h, part, counts,
-                                  [&](float v, uint32_t j) { return v == last && j <= mid; }) >= g.top)
-                to = mid;
-            else
-                from = mid + 1;
+        uint2 *out = g.candidate + static_cast<uint64_t>(blockIdx.x) * g.room;
+        if (total <= g.room) {
+            for (uint32_t i = threadIdx.x & 63u; i < n; i += 64) out[at + i] = list[wave][i];
+        } else {
+            trim_part<T>(z, part, g.vocab, cut, g.top, out, counts);
+            total = g.top;
         }
-        __syncthreads();
-        h.each([&](float v, uint32_t i, uint32_t e) {
-            const uint32_t j = h.first(part, i) + e;
-            if (v > last || (v == last && j <= to)) {
-                const uint32_t slot = atomicAdd(&found, 1u);
-                if (slot < g.room) out[slot] = uint2{ordered(v), j};
-            }
-        });
-        __syncthreads();
-        n = min(found, g.room);
+        if (threadIdx.x == 0) g.count[blockIdx.x] = total;
     }
-    if (threadIdx.x == 0) g.count[blockIdx.x] = n;
 }
 
 template <class T>
@@ -347,168 +383,154 @@ __global__ __launch_bounds__(kThreads) void logprob_top_kernel(LogprobArgs g) {
     logprob_part<T, true>(g);
 }
 
-constexpr uint32_t kJoin = 2048;  // candidates that the join holds at once
+constexpr uint32_t kSlots = 16;  // candidates that a lane of the join holds
+constexpr uint32_t kList = 512;  // that are ordered by counting
 
-// Keeps the `top` largest of the n candidates in key[], idx[] (LDS, one wave),
-// largest first and equal ones by index, and returns how many there are.  The
-// workgroup is one wave: a barrier orders its LDS accesses, no more.
-__device__ uint32_t keep_top(uint32_t *key, uint32_t *idx, uint32_t n, uint32_t top) {
-    const uint32_t lane = threadIdx.x & 63u;
-    const uint64_t below = (1ull << lane) - 1;
-    // few enough to be ordered by counting
-    const uint32_t few = max(64u, top + top / 8);
-    if (n > few) {
-        uint32_t lo = ~0u, hi = 0;
-        for (uint32_t i = lane; i < n; i += 64) {
-            lo = min(lo, key[i]);
-            hi = max(hi, key[i]);
-        }
-        lo = wave_min(lo);
-        hi = wave_max(hi);
-        uint32_t got = n;
-        while (lo < hi && got > few) {
-            const uint32_t mid = hi - (hi - lo) / 2;
-            uint32_t c = 0;
-            for (uint32_t i = lane; i < n; i += 64) c += key[i] >= mid ? 1u : 0u;
-            c = wave_sum(c);
-            if (c >= top) {
-                lo = mid;
-                got = c;
-            } else {
-                hi = mid - 1;
-            }
-        }
-        uint32_t last = ~0u;  // the index up to which those equal to lo are kept
-        if (got > few) {
-            uint32_t from = 0, to = ~0u;
-            while (from < to) {
-                const uint32_t mid = from + (to - from) / 2;
-                uint32_t c = 0;
-                for (uint32_t i = lane; i < n; i += 64)
-                    c += key[i] > lo || (key[i] == lo && idx[i] <= mid) ? 1u : 0u;
-                if (wave_sum(c) >= top)
-                    to = mid;
-                else
-                    from = mid + 1;
-            }
-            last = to;
-        }
-        // to the front, in place: what is written lies at or before what was read
-        uint32_t kept = 0;
-        for (uint32_t i = 0; i < n; i += 64) {
-            const bool in = i + lane < n;
-            const uint32_t k = in ? key[i + lane] : 0, j = in ? idx[i + lane] : 0;
-            const bool keep = in && (k > lo || (k == lo && j <= last));
-            const uint64_t all = __ballot(keep);
-            __syncthreads();
-            if (keep) {
-                const uint32_t at = kept + __popcll(all & below);
-                key[at] = k;
-                idx[at] = j;
-            }
-            __syncthreads();
-            kept += __popcll(all);
-        }
-        n = kept;
-    }
-    // a candidate's place is the number of larger ones; at most 3 a lane
-    constexpr uint32_t kMost = (DF11_MAX_TOP + DF11_MAX_TOP / 8 + 63) / 64;
-    uint32_t k[kMost], j[kMost], place[kMost];
-#pragma unroll
-    for (uint32_t e = 0; e < kMost; ++e) {
-        const uint32_t i = 64 * e + lane;
-        k[e] = i < n ? key[i] : 0;
-        j[e] = i < n ? idx[i] : ~0u;
-        place[e] = 0;
-    }
-    for (uint32_t i = 0; i < n; ++i) {
-        const uint32_t ki = key[i], ji = idx[i];
-#pragma unroll
-        for (uint32_t e = 0; e < kMost; ++e)
-            place[e] += ki > k[e] || (ki == k[e] && ji < j[e]) ? 1u : 0u;
-    }
-    __syncthreads();
-#pragma unroll
-    for (uint32_t e = 0; e < kMost; ++e)
-        if (64 * e + lane < n && place[e] < top) {
-            key[place[e]] = k[e];
-            idx[place[e]] = j[e];
-        }
-    __syncthreads();
-    return min(n, top);
-}
-
-// One wave per row.
+// One workgroup per row: the parts' statistics, and of their candidates the
+// `top` largest in order.  As in a part, a key that `top` lanes reach leaves
+// few (trimmed exactly where equal ones are too many); the place of each of
+// them is the number of larger ones, equal keys by their index.  Rows with more
+// slots than 4096 take rounds, with what was kept so far as further candidates.
 template <class T>
-__global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs g) {
-    __shared__ uint32_t key[kJoin], idx[kJoin], filled[64];
-    const uint64_t row = blockIdx.x;
-    const uint32_t lane = threadIdx.x;
-    const int64_t token = g.tokens ? g.tokens[row] : -1;
-    const bool asked = token >= 0 && token < g.vocab;
-    const float zt = asked ? T::load((static_cast<const typename T::raw *>(g.logits) + row * g.stride)[token]) : 0.0f;
-    uint64_t above;
-    const PartStat p = join_parts(g.stat + row * g.parts, g.parts, g.two_over_tau, true, &above);
-    const bool broken = !(p.s >= 0.0f) || p.s == INFINITY;
-    const bool empty = p.s == 0.0f;
-    const float ln_s = logf(p.s), nan = __builtin_nanf("");
-    if (lane == 0) {
-        float lp = empty ? -INFINITY : scaled(zt, p.m, g.two_over_tau) - ln_s;
-        const float h = broken ? nan : empty ? 0.0f : ln_s - kLn2 * (p.t / p.s);
-        if (token < 0) lp = 0.0f;
-        if ((token >= 0 && !asked) || broken) lp = nan;
-        if (g.logprob) g.logprob[row] = lp;
-        if (g.rank) g.rank[row] = asked && !broken ? static_cast<int64_t>(above) : -1;
-        if (g.entropy) g.entropy[row] = h;
-        if (g.stats) *reinterpret_cast<float4 *>(g.stats + 4 * row) = float4{p.m, ln_s, h, lp};
+__global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
+    __shared__ uint32_t lane_key[kThreads], counts[kWaves];
+    __shared__ uint32_t list_key[kList], list_idx[kList], place[kList];
+    __shared__ uint32_t best_key[DF11_MAX_TOP], best_idx[DF11_MAX_TOP];
+    __shared__ float row_m, row_ln_s, row_s;
+    const uint64_t row = blockIdx.x, first = row * g.parts;
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    uint32_t key[kSlots + 1], idx[kSlots + 1];
+    const uint32_t slots = g.parts * g.room;
+    const auto load = [&](uint32_t from) {
+#pragma unroll
+        for (uint32_t e = 0; e < kSlots; ++e) {
+            const uint32_t f = from + kThreads * e + threadIdx.x, q = f / max(g.room, 1u);
+            const bool some = f < slots && f - q * g.room < g.count[first + q];
+            const uint2 v = some ? g.candidate[first * g.room + f] : uint2{0u, ~0u};
+            key[e] = v.x;
+            idx[e] = v.y;
+        }
+    };
+    if (g.top) load(0);
+    if (wave == 0) {
+        const int64_t token = g.tokens ? g.tokens[row] : -1;
+        const bool asked = token >= 0 && token < g.vocab;
+        const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
+        const float zt = asked ? T::load(z[token]) : 0.0f;
+        uint64_t above;
+        const PartStat p = join_parts(g.stat + first, g.parts, g.two_over_tau, true, &above);
+        const bool broken = !(p.s >= 0.0f) || p.s == INFINITY;
+        const bool empty = p.s == 0.0f;
+        const float ln_s = logf(p.s), nan = __builtin_nanf("");
+        if (lane == 0) {
+            float lp = empty ? -INFINITY : scaled(zt, p.m, g.two_over_tau) - ln_s;
+            const float h = broken ? nan : empty ? 0.0f : ln_s - kLn2 * (p.t / p.s);
+            if (token < 0) lp = 0.0f;
+            if ((token >= 0 && !asked) || broken) lp = nan;
+            if (g.logprob) g.logprob[row] = lp;
+            if (g.rank) g.rank[row] = asked && !broken ? static_cast<int64_t>(above) : -1;
+            if (g.entropy) g.entropy[row] = h;
+            if (g.stats) *reinterpret_cast<float4 *>(g.stats + 4 * row) = float4{p.m, ln_s, h, lp};
+            row_m = p.m;
+            row_ln_s = ln_s;
+            row_s = broken ? -1.0f : p.s;
+        }
     }
     if (!g.top) return;
-    // the parts' candidates lie `room` apart: lanes run over all the slots, a
-    // batch of loads at a time, and take those that are filled
-    constexpr uint32_t kBatch = 16;
-    const uint64_t below = (1ull << lane) - 1;
-    uint32_t n = 0;
-    for (uint32_t q0 = 0; q0 < g.parts; q0 += 64) {
-        const uint32_t here = min(64u, g.parts - q0);
-        const uint64_t first = row * g.parts + q0;
-        __syncthreads();
-        if (lane < here) filled[lane] = min(g.count[first + lane], g.room);
-        __syncthreads();
-        const uint2 *from = g.candidate + first * g.room;
-        uint32_t q = lane / g.room, r = lane % g.room;
-        for (uint32_t f = lane; f - lane < here * g.room; f += 64 * kBatch) {
-            uint2 v[kBatch];
-            bool in[kBatch];
+
+    uint32_t kept = 0;
+    for (uint32_t from = 0;;) {
+        key[kSlots] = threadIdx.x < kept ? best_key[threadIdx.x] : 0;
+        idx[kSlots] = threadIdx.x < kept ? best_idx[threadIdx.x] : ~0u;
+        uint32_t most = 0;
 #pragma unroll
-            for (uint32_t e = 0; e < kBatch; ++e) {
-                in[e] = q < here && r < filled[q < here ? q : 0];
-                if (in[e]) v[e] = from[f + 64 * e];
-                r += 64;
-                if (r >= g.room) {  // room > 64
-                    r -= g.room;
-                    ++q;
+        for (uint32_t e = 0; e <= kSlots; ++e) most = max(most, key[e]);
+        lane_key[threadIdx.x] = most;
+        __syncthreads();
+        uint32_t cut = reached_by(lane_key, g.top), last = ~0u, n = 0;
+        const auto count = [&](auto f) {
+            uint32_t c = 0;
+#pragma unroll
+            for (uint32_t e = 0; e <= kSlots; ++e) c += f(key[e], idx[e]) ? 1u : 0u;
+            return wg_sum(c, counts);
+        };
+        n = count([&](uint32_t k, uint32_t) { return k >= cut; });
+        if (n > kList) {  // equal ones, or a few lanes with all the large ones
+            uint32_t hi = ~0u;
+            while (cut < hi) {
+                const uint32_t mid = hi - (hi - cut) / 2;
+                const uint32_t c = count([&](uint32_t k, uint32_t) { return k >= mid; });
+                if (c >= g.top) {
+                    cut = mid;
+                    n = c;
+                    if (c <= kList) break;
+                } else {
+                    hi = mid - 1;
                 }
             }
-            if (n + 64 * kBatch > kJoin) n = keep_top(key, idx, n, g.top);
-#pragma unroll
-            for (uint32_t e = 0; e < kBatch; ++e) {
-                const uint64_t all = __ballot(in[e]);
-                if (in[e]) {
-                    const uint32_t at = n + __popcll(all & below);
-                    key[at] = v[e].x;
-                    idx[at] = v[e].y;
+            uint32_t low = 0;
+            while (n > kList && low < last) {
+                const uint32_t mid = low + (last - low) / 2;
+                const uint32_t c = count(
+                    [&](uint32_t k, uint32_t i) { return k > cut || (k == cut && i <= mid); });
+                if (c >= g.top) {
+                    last = mid;
+                    n = c;
+                } else {
+                    low = mid + 1;
                 }
-                n += __popcll(all);
             }
-            __syncthreads();
         }
+        // to the list: each wave behind those below it
+        uint32_t mine = 0;
+#pragma unroll
+        for (uint32_t e = 0; e <= kSlots; ++e)
+            mine += __popcll(__ballot(key[e] > cut || (key[e] == cut && idx[e] <= last)));
+        __syncthreads();
+        if (lane == 0) counts[wave] = mine;
+        __syncthreads();
+        uint32_t at = 0;
+        for (uint32_t w = 0; w < wave; ++w) at += counts[w];
+#pragma unroll
+        for (uint32_t e = 0; e <= kSlots; ++e) {
+            const bool in = key[e] > cut || (key[e] == cut && idx[e] <= last);
+            const uint64_t all = __ballot(in);
+            if (in) {
+                list_key[at + before(all)] = key[e];
+                list_idx[at + before(all)] = idx[e];
+            }
+            at += __popcll(all);
+        }
+        for (uint32_t c = threadIdx.x; c < n; c += kThreads) place[c] = 0;
+        __syncthreads();
+        // each wave counts over a quarter of the list
+        const uint32_t lo = wave * n / kWaves, hi = (wave + 1) * n / kWaves;
+        for (uint32_t c = lane; c < n; c += 64) {
+            const uint32_t k = list_key[c], i = list_idx[c];
+            uint32_t larger = 0;
+#pragma unroll 4
+            for (uint32_t d = lo; d < hi; ++d)
+                larger += list_key[d] > k || (list_key[d] == k && list_idx[d] < i) ? 1u : 0u;
+            atomicAdd(&place[c], larger);
+        }
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < n; c += kThreads)
+            if (place[c] < g.top) {
+                best_key[place[c]] = list_key[c];
+                best_idx[place[c]] = list_idx[c];
+            }
+        __syncthreads();
+        kept = min(n, g.top);
+        from += kThreads * kSlots;
+        if (from >= slots) break;
+        load(from);
     }
-    n = keep_top(key, idx, n, g.top);
-    for (uint32_t k = lane; k < g.top; k += 64) {
-        const bool some = k < n;
-        g.top_logprob[row * g.top + k] =
-            broken ? nan : some ? scaled(from_ordered(key[k]), p.m, g.two_over_tau) - ln_s : -INFINITY;
-        g.top_index[row * g.top + k] = broken || !some ? -1 : static_cast<int64_t>(idx[k]);
+    const bool broken = row_s < 0.0f;
+    for (uint32_t k = threadIdx.x; k < g.top; k += kThreads) {
+        const bool some = k < kept;
+        const float lp = scaled(from_ordered(best_key[k]), row_m, g.two_over_tau) - row_ln_s;
+        g.top_logprob[row * g.top + k] = broken ? __builtin_nanf("") : some ? lp : -INFINITY;
+        g.top_index[row * g.top + k] = broken || !some ? -1 : static_cast<int64_t>(best_idx[k]);
     }
 }
 
@@ -836,7 +858,7 @@ int df11_logprobs(const void *logits, uint32_t dtype, uint64_t rows, uint32_t vo
     else
         DF11_BY_DTYPE(dtype, logprob_part_kernel, rows * parts, kThreads, stream, g);
     if ((rc = launched())) return rc;
-    DF11_BY_DTYPE(dtype, logprob_join_kernel, rows, 64, stream, g);
+    DF11_BY_DTYPE(dtype, logprob_join_kernel, rows, kThreads, stream, g);
     return launched();
 }
 
