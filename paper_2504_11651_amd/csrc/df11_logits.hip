@@ -31,6 +31,25 @@ constexpr uint32_t kThreads = 256;
 constexpr uint32_t kWaves = kThreads / 64;
 constexpr uint32_t kPerLane = 32;
 constexpr uint32_t kPart = kThreads * kPerLane;  // values of a row in one workgroup
+template <class T>
+constexpr int kOccupancy = T::kVec == 4 ? 6 : 8;  // waves on a SIMD
+template <class T>
+constexpr uint32_t kVecs = kPerLane / T::kVec;  // 16-byte loads of a lane
+
+// 1/tau and log2e/tau, in the forms that the kernels multiply by.
+struct Tau {
+    float two_over;  // 2/tau: differences of halves are multiplied by it
+    float c, rest;   // log2e/tau in two parts: one would be off by |x| 2^-25 in x, the
+                     // same way in every value, and so in the sum
+    double over;     // 1/tau
+    explicit Tau(float tau) : two_over(2.0f / tau), over(1.0 / tau) {
+        // the first part from below, so that the second is positive and a masked
+        // value stays -inf
+        c = static_cast<float>(M_LOG2E / tau);
+        if (c >= M_LOG2E / tau) c = std::nextafterf(c, 0.0f);
+        rest = static_cast<float>(M_LOG2E / tau - c);
+    }
+};
 
 // (v - m) / tau, of halves so that the difference of two finite values is finite
 __device__ float scaled(float v, float m, float two_over_tau) {
@@ -59,59 +78,91 @@ __device__ float above_of(float v) {
     return __uint_as_float(u & 0x80000000u ? u - 1 : u + 1);
 }
 
-// A lane's 32 values of a part: vector i of the lane holds the values from
+// A lane's values of a part: vector i of the lane holds the values from
 // part + (256 i + thread) * kVec.  What lies past the row is masked.
 template <class T>
 struct Held {
-    static constexpr uint32_t kVecs = kPerLane / T::kVec;
-    uint4 q[kVecs];
+    uint4 q[kVecs<T>];
 
     __device__ static uint32_t first(uint32_t part, uint32_t i) {
         return part + (kThreads * i + threadIdx.x) * T::kVec;
     }
-    __device__ void load(const typename T::raw *z, uint32_t part, uint32_t vocab) {
-        if (part + kPart <= vocab) {
+    __device__ void load(const typename T::raw *z, uint32_t part, uint32_t vocab, bool once) {
+        if (part + kPart <= vocab && once) {
+            keep_apart();
 #pragma unroll
-            for (uint32_t i = 0; i < kVecs; ++i) q[i] = load16(z + first(part, i));
+            for (uint32_t i = 0; i < kVecs<T>; ++i) q[i] = load16_once(z + first(part, i));
+            keep_apart();
             return;
         }
+        if (part + kPart <= vocab) {
 #pragma unroll
-        for (uint32_t i = 0; i < kVecs; ++i) {
-            const uint32_t j = first(part, i);
-            if (j + T::kVec <= vocab) {
-                q[i] = load16(z + j);
-            } else {
-                uint32_t w[4];
-                constexpr uint32_t both = T::kVec == 8 ? T::kMasked * 0x10001u : T::kMasked;
-                for (uint32_t e = 0; e < 4; ++e) w[e] = both;
+            for (uint32_t i = 0; i < kVecs<T>; ++i) q[i] = load16(z + first(part, i));
+            return;
+        }
+        // whole vectors first, all loads under way before the first is looked at;
+        // then the lane whose vector the row's end cuts takes single values
+        constexpr uint32_t both = T::kVec == 8 ? T::kMasked * 0x10001u : T::kMasked;
+        const uint4 masked{both, both, both, both};
+        if (vocab >= T::kVec) {
 #pragma unroll
-                for (uint32_t e = 0; e < T::kVec; ++e)
-                    if (j + e < vocab) {
-                        if constexpr (T::kVec == 4) {
-                            w[e] = __float_as_uint(z[j + e]);
-                        } else {
-                            const uint32_t v = z[j + e];
-                            w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | v << 16
-                                             : (w[e / 2] & 0xFFFF0000u) | v;
-                        }
-                    }
-                q[i] = uint4{w[0], w[1], w[2], w[3]};
+            for (uint32_t i = 0; i < kVecs<T>; ++i) {
+                const uint32_t j = first(part, i);
+                q[i] = load16(z + (j + T::kVec <= vocab ? j : 0));
             }
         }
+#pragma unroll
+        for (uint32_t i = 0; i < kVecs<T>; ++i) {
+            const uint32_t j = first(part, i);
+            if (j + T::kVec > vocab) {
+                q[i] = masked;
+                if (j < vocab) q[i] = cut_vector(z + j, vocab - j);
+            }
+        }
+    }
+    __device__ static uint4 cut_vector(const typename T::raw *z, uint32_t n) {
+        constexpr uint32_t kEach = 4 / sizeof(typename T::raw);
+        uint32_t w[4];
+        for (uint32_t k = 0; k < 4; ++k) {
+            w[k] = T::kVec == 8 ? T::kMasked * 0x10001u : T::kMasked;
+            for (uint32_t e = 0; e < kEach; ++e)
+                {
+                    const uint32_t i = k * kEach + e, v = T::bits(z[min(i, n - 1)]);
+                    const uint32_t at = 16 * e, mask = kEach == 2 ? 0xFFFFu : ~0u;
+                    w[k] = i < n ? (w[k] & ~(mask << at)) | v << at : w[k];
+                }
+        }
+        return uint4{w[0], w[1], w[2], w[3]};
+    }
+    // Keeps the compiler from holding the values cut out in one pass for the next:
+    // cutting them out again is cheaper than the registers.
+    __device__ void again() {
+#pragma unroll
+        for (uint32_t i = 0; i < kVecs<T>; ++i)
+            asm volatile("" : "+v"(q[i].x), "+v"(q[i].y), "+v"(q[i].z), "+v"(q[i].w));
     }
     template <class F>
     __device__ void each(F f) const {  // f(value, vector, element)
 #pragma unroll
-        for (uint32_t i = 0; i < kVecs; ++i)
+        for (uint32_t i = 0; i < kVecs<T>; ++i)
 #pragma unroll
             for (uint32_t e = 0; e < T::kVec; ++e) f(T::get(q[i], e), i, e);
     }
     __device__ float max() const {
-        float m = -INFINITY;
-        each([&](float v, uint32_t, uint32_t) { m = fmaxf(m, v); });
-        return m;
+        typename T::Max m;
+#pragma unroll
+        for (uint32_t i = 0; i < kVecs<T>; ++i) {
+            m.add(q[i].x, q[i].y);
+            m.add(q[i].z, q[i].w);
+        }
+        return m.value();
     }
 };
+
+// (v - m) / tau where a row's few results are made of it.
+__device__ double scaled64(float v, float m, const Tau &tau) {
+    return (static_cast<double>(v) - static_cast<double>(m)) * tau.over;
+}
 
 // What a part, or several, says about its row: maximum (at least the lowest
 // finite value, so that masked values give exp(-inf)), sum e, and a second sum:
@@ -122,25 +173,37 @@ struct PartStat {
     uint32_t above;
 };
 
-// e = exp2((v - m) c) for a wave's values with the wave's maximum m: f(v, e, x, i, j)
-// with x = (v - m) c up to the returned shift, which is the same for all.
-// One fused operation a value where m c is in range; its rounding is the shift.
-template <class T, class F>
-__device__ float each_exp(const Held<T> &h, float m, float two_over_tau, F f) {
-    const float c = 0.5f * two_over_tau * kLog2e, mc = m * c;
-    if (fabsf(mc) < 1e38f) {
-        h.each([&](float v, uint32_t i, uint32_t e) {
-            const float x = fmaf(v, c, -mc);
-            f(v, __builtin_amdgcn_exp2f(x), x, i, e);
-        });
-        return fmaf(m, c, -mc);  // m c is mc plus this: the true x is x minus it
+// x = (v - m) log2e / tau for the values of a wave with the wave's maximum m, up
+// to a shift that is the same for all of them: v c - m c, fused, with m c rounded.
+// Where m c leaves the range (masks of the lowest finite value, logits of 10^37)
+// the differences are taken first.
+struct Exponent {
+    float m, c, rest, mc, two_over_tau;
+    bool near;
+    // `most`: the wave's maximum, -inf where all is masked (then x is -inf)
+    __device__ Exponent(float most, const Tau &tau)
+        : m(fmaxf(most, kLowest)), c(tau.c), rest(tau.rest),
+          mc(most == -INFINITY ? 0.0f : m * c), two_over_tau(tau.two_over),
+          near(fabsf(mc) < 1e38f) {}
+    // what is to be taken from x: m (c + rest) is mc plus this
+    __device__ float shift() const {
+        return near && m != kLowest ? fmaf(m, rest, fmaf(m, c, -mc)) : 0.0f;
     }
-    h.each([&](float v, uint32_t i, uint32_t e) {
-        const float x = scaled(v, m, two_over_tau) * kLog2e;
-        f(v, __builtin_amdgcn_exp2f(x), x, i, e);
-    });
-    return 0.0f;
-}
+    template <class T>
+    __device__ void operator()(const uint4 &q, float *v, float *x) const {
+#pragma unroll
+        for (uint32_t k = 0; k < T::kVec; ++k) {
+            v[k] = T::get(q, k);
+            x[k] = fmaf(v[k], rest, fmaf(v[k], c, -mc));
+        }
+        if (!near) {
+            float far = two_over_tau;
+            asm volatile("" : "+v"(far));  // a branch, not a selection for every value
+#pragma unroll
+            for (uint32_t k = 0; k < T::kVec; ++k) x[k] = scaled(v[k], m, far) * kLog2e;
+        }
+    }
+};
 
 // Sums with maximum m scaled to the larger maximum M: the factor, and for the
 // sum of e x the shift of x.
@@ -199,7 +262,8 @@ struct LogprobArgs {
     int64_t *rank, *top_index;
     uint64_t stride;
     uint32_t vocab, parts, top, room;
-    float two_over_tau;
+    Tau tau;
+    bool once;
 };
 
 // Values above the threshold that a part may bring: twice what is wanted, and
@@ -251,14 +315,14 @@ __device__ uint32_t reached_by(const uint32_t *lane_key, uint32_t top) {
 // values), then the index up to which values equal to it are taken.  Reads the
 // part again: it is rare, and the registers it would need are not.
 template <class T>
-__device__ __attribute__((noinline)) void trim_part(const typename T::raw *z, uint32_t part,
+__device__ inline void trim_part(const typename T::raw *z, uint32_t part,
                                                     uint32_t vocab, uint32_t cut, uint32_t top,
                                                     uint2 *out, uint32_t *lds) {
     const uint32_t to = min(kPart, vocab - part);
     z += part;
     auto count = [&](auto f) {
         uint32_t n = 0;
-#pragma unroll 8
+#pragma unroll 4
         for (uint32_t i = threadIdx.x; i < to; i += kThreads) n += f(T::load(z[i]), i) ? 1u : 0u;
         return wg_sum(n, lds);
     };
@@ -287,6 +351,7 @@ __device__ __attribute__((noinline)) void trim_part(const typename T::raw *z, ui
     __syncthreads();
     if (threadIdx.x == 0) lds[0] = 0;
     __syncthreads();
+#pragma unroll 1
     for (uint32_t i = threadIdx.x; i < to; i += kThreads) {
         const float v = T::load(z[i]);
         if (v > last || (v == last && i <= until)) {
@@ -299,14 +364,15 @@ __device__ __attribute__((noinline)) void trim_part(const typename T::raw *z, ui
 template <class T, bool kTop>
 __device__ void logprob_part(const LogprobArgs &g) {
     __shared__ PartStat wave_stat[kWaves];
-    __shared__ uint32_t lane_key[kTop ? kThreads : 1], counts[kWaves];
+    __shared__ uint32_t lane_key[kTop ? kThreads : 1], counts[kWaves], shared_cut;
+    const uint32_t wave_of = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     __shared__ uint2 list[kTop ? kWaves : 1][kTop ? room_of(DF11_MAX_TOP) : 1];
     const uint32_t row_parts = g.parts;
     const uint64_t row = blockIdx.x / row_parts;
     const uint32_t part = (blockIdx.x % row_parts) * kPart;
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
     Held<T> h;
-    h.load(z, part, g.vocab);
+    h.load(z, part, g.vocab, g.once);
 
     const int64_t token = g.tokens ? g.tokens[row] : -1;
     const bool asked = token >= 0 && token < g.vocab;
@@ -315,47 +381,72 @@ __device__ void logprob_part(const LogprobArgs &g) {
     const float more = asked ? above_of(zt) : zt;
 
     const float lane_max = h.max();
-    const float m = fmaxf(wave_max(lane_max), kLowest);
+    h.again();
+    // before the token equal values count, from it on larger ones: one bound for
+    // all values of a part, except in the token's own
+    const bool here = asked && tok >= part && tok - part < kPart;
+    const float rest = part < tok ? zt : more;
+    const Exponent x_of(wave_max(lane_max), g.tau);
     float s = 0.0f, t = 0.0f;
     uint32_t above = 0;
-    const auto add = [&](float v, float e, float x, uint32_t i, uint32_t) {
-        s += e;
-        t = fmaf(e, fmaxf(x, -300.0f), t);  // no 0 * inf
-        // before the token equal values count, from it on larger ones
-        above += v >= (h.first(part, i) < tok ? zt : more) ? 1u : 0u;
-    };
-    const float shift = each_exp(h, m, g.two_over_tau, add);
-    // in the token's own vector equal ones from the token on were counted too
-    if (asked && tok >= part && tok - part < kPart && (tok - part) % T::kVec != 0 &&
-        (tok - part) / T::kVec % kThreads == threadIdx.x)
-        h.each([&](float v, uint32_t i, uint32_t e) {
+#pragma unroll
+    for (uint32_t i = 0; i < kVecs<T>; ++i) {
+        float v[T::kVec], x[T::kVec], sum = 0.0f;
+        x_of.operator()<T>(h.q[i], v, x);
+#pragma unroll
+        for (uint32_t k = 0; k < T::kVec; ++k) {
+            const float e = __builtin_amdgcn_exp2f(x[k]);
+            s += e;
+            sum = fmaf(e, fmaxf(x[k], -300.0f), sum);  // no 0 * inf
+        }
+        t += sum;
+        if (here) {
             const uint32_t j = h.first(part, i);
-            if (j < tok && tok < j + T::kVec && j + e >= tok && v == zt) --above;
-        });
+#pragma unroll
+            for (uint32_t k = 0; k < T::kVec; ++k) above += v[k] >= (j + k < tok ? zt : more) ? 1u : 0u;
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < T::kVec; ++k) above += v[k] >= rest ? 1u : 0u;
+        }
+        // a vector's values at a time in registers
+        asm volatile("" : "+v"(s), "+v"(t), "+v"(above));
+    }
     s = wave_sum(s);
     t = wave_sum(t);
     above = wave_sum(above);
     if ((threadIdx.x & 63u) == 0) {
-        const float f = __builtin_amdgcn_exp2f(-shift);
-        wave_stat[threadIdx.x >> 6] = PartStat{m, s * f, f * fmaf(-shift, s, t), above};
+        const float shift = x_of.shift(), f = __builtin_amdgcn_exp2f(-shift);
+        wave_stat[threadIdx.x >> 6] = PartStat{x_of.m, s * f, f * fmaf(-shift, s, t), above};
     }
     if constexpr (kTop) lane_key[threadIdx.x] = ordered(lane_max);
     __syncthreads();
-    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.two_over_tau, true);
+    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.tau.two_over, true);
     if constexpr (kTop) {
-        const uint32_t cut = reached_by(lane_key, g.top);
+        if (wave_of == (blockIdx.x & 3u)) {
+            const uint32_t c = reached_by(lane_key, g.top);
+            if ((threadIdx.x & 63u) == 0) shared_cut = c;
+        }
+        __syncthreads();
+        const uint32_t cut = shared_cut;
         const float least = from_ordered(cut);
         const uint32_t wave = threadIdx.x >> 6;
+        h.again();
+        const float low = T::at_least(least, 0), high = T::at_least(least, 1);
         uint32_t n = 0;  // of this wave
-        h.each([&](float v, uint32_t i, uint32_t e) {
-            const uint64_t all = __ballot(v >= least);
-            if (all) {
-                const uint32_t slot = n + before(all);
-                if (v >= least && slot < g.room)
-                    list[wave][slot] = uint2{ordered(v), h.first(part, i) + e};
-                n += __popcll(all);
+#pragma unroll
+        for (uint32_t i = 0; i < kVecs<T>; ++i)
+#pragma unroll
+            for (uint32_t e = 0; e < T::kVec; ++e) {
+                const bool in = T::rough(h.q[i], e) >= (e & 1 ? high : low);
+                const uint64_t all = __ballot(in);
+                if (all) {
+                    const uint32_t slot = n + before(all);
+                    if (in && slot < g.room)
+                        list[wave][slot] = uint2{__float_as_uint(T::get(h.q[i], e)),
+                                                 h.first(part, i) + e};
+                    n += __popcll(all);
+                }
             }
-        });
         if ((threadIdx.x & 63u) == 0) counts[wave] = n;
         __syncthreads();
         uint32_t at = 0, total = 0;
@@ -365,7 +456,10 @@ __device__ void logprob_part(const LogprobArgs &g) {
         }
         uint2 *out = g.candidate + static_cast<uint64_t>(blockIdx.x) * g.room;
         if (total <= g.room) {
-            for (uint32_t i = threadIdx.x & 63u; i < n; i += 64) out[at + i] = list[wave][i];
+            for (uint32_t i = threadIdx.x & 63u; i < n; i += 64) {
+                const uint2 v = list[wave][i];
+                out[at + i] = uint2{ordered(__uint_as_float(v.x)), v.y};
+            }
         } else {
             trim_part<T>(z, part, g.vocab, cut, g.top, out, counts);
             total = g.top;
@@ -375,11 +469,11 @@ __device__ void logprob_part(const LogprobArgs &g) {
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads) void logprob_part_kernel(LogprobArgs g) {
+__global__ __launch_bounds__(kThreads, kOccupancy<T>) void logprob_part_kernel(LogprobArgs g) {
     logprob_part<T, false>(g);
 }
 template <class T>
-__global__ __launch_bounds__(kThreads) void logprob_top_kernel(LogprobArgs g) {
+__global__ __launch_bounds__(kThreads, kOccupancy<T>) void logprob_top_kernel(LogprobArgs g) {
     logprob_part<T, true>(g);
 }
 
@@ -396,19 +490,27 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
     __shared__ uint32_t lane_key[kThreads], counts[kWaves];
     __shared__ uint32_t list_key[kList], list_idx[kList], place[kList];
     __shared__ uint32_t best_key[DF11_MAX_TOP], best_idx[DF11_MAX_TOP];
-    __shared__ float row_m, row_ln_s, row_s;
+    __shared__ double row_ln_s;
+    __shared__ float row_m, row_s;
     const uint64_t row = blockIdx.x, first = row * g.parts;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     uint32_t key[kSlots + 1], idx[kSlots + 1];
     const uint32_t slots = g.parts * g.room;
     const auto load = [&](uint32_t from) {
+        uint32_t q = (from + threadIdx.x) / g.room, r = (from + threadIdx.x) % g.room;
 #pragma unroll
         for (uint32_t e = 0; e < kSlots; ++e) {
-            const uint32_t f = from + kThreads * e + threadIdx.x, q = f / max(g.room, 1u);
-            const bool some = f < slots && f - q * g.room < g.count[first + q];
-            const uint2 v = some ? g.candidate[first * g.room + f] : uint2{0u, ~0u};
+            const bool some = q < g.parts && r < g.count[first + q];
+            const uint2 v =
+                some ? g.candidate[first * g.room + from + kThreads * e + threadIdx.x] : uint2{0u, ~0u};
             key[e] = v.x;
             idx[e] = v.y;
+            q += kThreads / g.room;
+            r += kThreads % g.room;
+            if (r >= g.room) {
+                r -= g.room;
+                ++q;
+            }
         }
     };
     if (g.top) load(0);
@@ -418,19 +520,22 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
         const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
         const float zt = asked ? T::load(z[token]) : 0.0f;
         uint64_t above;
-        const PartStat p = join_parts(g.stat + first, g.parts, g.two_over_tau, true, &above);
+        const PartStat p = join_parts(g.stat + first, g.parts, g.tau.two_over, true, &above);
         const bool broken = !(p.s >= 0.0f) || p.s == INFINITY;
         const bool empty = p.s == 0.0f;
-        const float ln_s = logf(p.s), nan = __builtin_nanf("");
+        const float nan = __builtin_nanf("");
+        // ln S is about 10, and its rounding to 32 bits would be the largest error
+        const double ln_s = log(static_cast<double>(p.s));
         if (lane == 0) {
-            float lp = empty ? -INFINITY : scaled(zt, p.m, g.two_over_tau) - ln_s;
-            const float h = broken ? nan : empty ? 0.0f : ln_s - kLn2 * (p.t / p.s);
+            float lp = empty ? -INFINITY : static_cast<float>(scaled64(zt, p.m, g.tau) - ln_s);
+            const float h =
+                broken ? nan : empty ? 0.0f : static_cast<float>(ln_s - M_LN2 * p.t / p.s);
             if (token < 0) lp = 0.0f;
             if ((token >= 0 && !asked) || broken) lp = nan;
             if (g.logprob) g.logprob[row] = lp;
             if (g.rank) g.rank[row] = asked && !broken ? static_cast<int64_t>(above) : -1;
             if (g.entropy) g.entropy[row] = h;
-            if (g.stats) *reinterpret_cast<float4 *>(g.stats + 4 * row) = float4{p.m, ln_s, h, lp};
+            if (g.stats) *reinterpret_cast<float4 *>(g.stats + 4 * row) = float4{p.m, static_cast<float>(ln_s), h, lp};
             row_m = p.m;
             row_ln_s = ln_s;
             row_s = broken ? -1.0f : p.s;
@@ -528,7 +633,8 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
     const bool broken = row_s < 0.0f;
     for (uint32_t k = threadIdx.x; k < g.top; k += kThreads) {
         const bool some = k < kept;
-        const float lp = scaled(from_ordered(best_key[k]), row_m, g.two_over_tau) - row_ln_s;
+        const double x = scaled64(from_ordered(best_key[k]), row_m, g.tau);
+        const float lp = static_cast<float>(x - row_ln_s);
         g.top_logprob[row * g.top + k] = broken ? __builtin_nanf("") : some ? lp : -INFINITY;
         g.top_index[row * g.top + k] = broken || !some ? -1 : static_cast<int64_t>(best_idx[k]);
     }
@@ -541,20 +647,28 @@ struct LogprobGradArgs {
     const float *stats, *grad_logprob, *grad_entropy;
     uint64_t stride, grad_stride;
     uint32_t vocab, parts;
-    float two_over_tau;
+    Tau tau;
+    bool once;
 };
 
 // Writes f(value, index) for the values of a part.
 template <class T, class F>
-__device__ void store_part(const Held<T> &h, typename T::raw *out, uint32_t part, uint32_t vocab, F f) {
+__device__ void store_part(const Held<T> &h, typename T::raw *out, uint32_t part, uint32_t vocab,
+                           bool once, F f) {
 #pragma unroll
-    for (uint32_t i = 0; i < Held<T>::kVecs; ++i) {
+    for (uint32_t i = 0; i < kVecs<T>; ++i) {
         const uint32_t j = Held<T>::first(part, i);
         typename T::raw r[T::kVec];
 #pragma unroll
         for (uint32_t e = 0; e < T::kVec; ++e) r[e] = T::store(f(T::get(h.q[i], e), j + e));
         if (j + T::kVec <= vocab) {
-            store16(out + j, __builtin_bit_cast(uint4, r));
+            if (once) {
+                keep_apart();
+                store16_once(out + j, __builtin_bit_cast(uint4, r));
+                keep_apart();
+            } else {
+                store16(out + j, __builtin_bit_cast(uint4, r));
+            }
         } else {
 #pragma unroll
             for (uint32_t e = 0; e < T::kVec; ++e)
@@ -566,16 +680,16 @@ __device__ void store_part(const Held<T> &h, typename T::raw *out, uint32_t part
 // grad = p (A + B y), y = log2 p: the formula with its factors drawn together.
 // The token's value, the only other one, is written by the lane that holds it.
 template <class T>
-__global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs g) {
+__global__ __launch_bounds__(kThreads, 8) void logprob_grad_kernel(LogprobGradArgs g) {
     const uint64_t row = blockIdx.x / g.parts;
     const uint32_t part = (blockIdx.x % g.parts) * kPart;
     Held<T> h;
-    h.load(static_cast<const typename T::raw *>(g.logits) + row * g.stride, part, g.vocab);
+    h.load(static_cast<const typename T::raw *>(g.logits) + row * g.stride, part, g.vocab, g.once);
     auto *out = static_cast<typename T::raw *>(g.grad) + row * g.grad_stride;
     const int64_t token = g.tokens ? g.tokens[row] : -1;
     const float4 st = *reinterpret_cast<const float4 *>(g.stats + 4 * row);
     const float m = st.x, ln_s = st.y, entropy = st.z;
-    const float over_tau = 0.5f * g.two_over_tau;
+    const float over_tau = 0.5f * g.tau.two_over;
     float gl = g.grad_logprob && token >= 0 ? g.grad_logprob[row] : 0.0f;
     if (token >= static_cast<int64_t>(g.vocab)) gl = __builtin_nanf("");
     const float ge = g.grad_entropy ? g.grad_entropy[row] : 0.0f;
@@ -583,8 +697,8 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(LogprobGradArgs 
     const float A = -over_tau * fmaf(ge, entropy, gl), B = -over_tau * ge * kLn2;
     const float hit = over_tau * gl, log2_s = ln_s * kLog2e;
     const uint32_t tok = token >= 0 && token < g.vocab ? static_cast<uint32_t>(token) : ~0u;
-    store_part(h, out, part, g.vocab, [&](float v, uint32_t j) {
-        const float y = fmaf(scaled(v, m, g.two_over_tau), kLog2e, -log2_s);
+    store_part(h, out, part, g.vocab, g.once, [&](float v, uint32_t j) {
+        const float y = fmaf(scaled(v, m, g.tau.two_over), kLog2e, -log2_s);
         const float d = __builtin_amdgcn_exp2f(y) * fmaf(B, fmaxf(y, -300.0f), A);
         return empty ? 0.0f : j == tok ? d + hit : d;
     });
@@ -600,7 +714,8 @@ struct DistillArgs {
     float *loss, *stats;
     uint64_t stride, grad_stride;
     uint32_t vocab, parts, top, tail;
-    float two_over_tau;
+    Tau tau;
+    bool once;
 };
 
 // Whether the teacher's entry is there, and whether it is out of range.
@@ -614,13 +729,14 @@ __device__ bool bad_entry(int64_t place, float logprob, uint32_t vocab) {
 // The second sum is kept beside the first, not taken from it by subtraction:
 // where the named places have nearly all the probability nothing would be left.
 template <class T>
-__global__ __launch_bounds__(kThreads) void distill_part_kernel(DistillArgs g) {
+__global__ __launch_bounds__(kThreads, 8) void distill_part_kernel(DistillArgs g) {
     __shared__ PartStat wave_stat[kWaves];
     __shared__ uint32_t bits[kPart / 32];
     const uint64_t row = blockIdx.x / g.parts;
     const uint32_t part = (blockIdx.x % g.parts) * kPart;
     Held<T> h;
-    h.load(static_cast<const typename T::raw *>(g.logits) + row * g.stride, part, g.vocab);
+    const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
+    h.load(z, part, g.vocab, g.once);
     static_assert(kPart / 32 == kThreads, "a word a thread");
     bits[threadIdx.x] = 0;
     __syncthreads();
@@ -630,26 +746,38 @@ __global__ __launch_bounds__(kThreads) void distill_part_kernel(DistillArgs g) {
             atomicOr(&bits[(i - part) >> 5], 1u << ((i - part) & 31));
     }
     __syncthreads();
-    const float m = fmaxf(wave_max(h.max()), kLowest);
+    const Exponent x_of(wave_max(h.max()), g.tau);
+    h.again();
+    // a vector at a time: few of them have a named place in any lane
     float s = 0.0f, t = 0.0f;
-    uint32_t mask = 0;
-    const auto add = [&](float, float e, float, uint32_t i, uint32_t k) {
-        if (k == 0) {
-            const uint32_t at = h.first(0, i);
-            mask = bits[at >> 5] >> (at & 31u);
+#pragma unroll
+    for (uint32_t i = 0; i < kVecs<T>; ++i) {
+        float v[T::kVec], e[T::kVec], sum = 0.0f;
+        x_of.operator()<T>(h.q[i], v, e);
+#pragma unroll
+        for (uint32_t k = 0; k < T::kVec; ++k) {
+            e[k] = __builtin_amdgcn_exp2f(e[k]);
+            sum += e[k];
         }
-        s += e;
-        t += mask >> k & 1u ? 0.0f : e;
-    };
-    const float shift = each_exp(h, m, g.two_over_tau, add);
+        const uint32_t at = h.first(0, i);
+        uint32_t mask = bits[at >> 5] >> (at & 31u) & ((1u << T::kVec) - 1);
+        s += sum;
+        if (__any(mask != 0)) {
+            asm volatile("" : "+v"(mask));  // a branch, not a selection for every vector
+            sum = 0.0f;
+#pragma unroll
+            for (uint32_t k = 0; k < T::kVec; ++k) sum += mask >> k & 1u ? 0.0f : e[k];
+        }
+        t += sum;
+    }
     s = wave_sum(s);
     t = wave_sum(t);
     if ((threadIdx.x & 63u) == 0) {
-        const float f = __builtin_amdgcn_exp2f(-shift);
-        wave_stat[threadIdx.x >> 6] = PartStat{m, s * f, t * f, 0};
+        const float f = __builtin_amdgcn_exp2f(-x_of.shift());
+        wave_stat[threadIdx.x >> 6] = PartStat{x_of.m, s * f, t * f, 0};
     }
     __syncthreads();
-    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.two_over_tau, false);
+    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.tau.two_over, false);
 }
 
 // One wave per row: the loss from the parts and the student's values at the
@@ -661,9 +789,9 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     const uint32_t lane = threadIdx.x;
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
     constexpr uint32_t kMost = DF11_MAX_TOP / 64;
-    float lt[kMost], p[kMost], v[kMost];
+    float lt[kMost], v[kMost];
+    double p[kMost], mass = 0.0;
     bool some = false, bad = false;
-    float mass = 0.0f;
 #pragma unroll
     for (uint32_t e = 0; e < kMost; ++e) {
         const uint32_t k = 64 * e + lane;
@@ -671,7 +799,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
         lt[e] = k < g.top ? g.teacher[row * g.top + k] : 0.0f;
         some |= named(at);
         bad |= bad_entry(at, lt[e], g.vocab);
-        p[e] = named(at) ? expf(lt[e]) : 0.0f;
+        p[e] = named(at) ? exp(static_cast<double>(lt[e])) : 0.0;
         v[e] = named(at) && at < g.vocab ? T::load(z[at]) : 0.0f;
         mass += p[e];
     }
@@ -679,51 +807,55 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     bad = __any(bad);
     mass = wave_sum(mass);
     uint64_t none;
-    const PartStat st = join_parts(g.stat + row * g.parts, g.parts, g.two_over_tau, false, &none);
-    const float ln_s = logf(st.s);
-    const float scale = g.tail ? 1.0f : 1.0f / mass, ln_mass = g.tail ? 0.0f : logf(mass);
-    float loss = 0.0f;
+    const PartStat st = join_parts(g.stat + row * g.parts, g.parts, g.tau.two_over, false, &none);
+    // a row's few terms in 64 bits: the loss is a difference of larger ones
+    const double ln_s = log(static_cast<double>(st.s));
+    const double scale = g.tail ? 1.0 : 1.0 / mass, ln_mass = g.tail ? 0.0 : log(mass);
+    double sum = 0.0;
 #pragma unroll
     for (uint32_t e = 0; e < kMost; ++e)
-        if (p[e] > 0.0f)
-            loss += p[e] * scale * (lt[e] - ln_mass - (scaled(v[e], st.m, g.two_over_tau) - ln_s));
-    loss = wave_sum(loss);
+        if (p[e] > 0.0)
+            sum += p[e] * scale * (lt[e] - ln_mass - (scaled64(v[e], st.m, g.tau) - ln_s));
+    sum = wave_sum(sum);
     if (lane) return;
-    const float left = st.t / st.s, r = fmaxf(0.0f, 1.0f - mass), nan = __builtin_nanf("");
-    float other = 1.0f, factor = scale;
-    if (g.tail && r > 0.0f) {
-        loss += r * (logf(r) - logf(left));
-        other = left > 0.0f ? 1.0f - r / left : 0.0f;
+    const double left = static_cast<double>(st.t) / st.s, r = fmax(0.0, 1.0 - mass);
+    const float nan = __builtin_nanf("");
+    float other = 1.0f, factor = static_cast<float>(scale);
+    if (g.tail && r > 0.0) {
+        sum += r * (log(r) - log(left));
+        other = left > 0.0 ? static_cast<float>(1.0 - r / left) : 0.0f;
     }
+    float loss = static_cast<float>(sum);
     if (st.s == 0.0f) {
         factor = -1.0f;
         loss = INFINITY;
     }
     if (!(st.s >= 0.0f) || st.s == INFINITY) loss = other = nan;
-    if (!some || (!g.tail && mass == 0.0f)) {
+    if (!some || (!g.tail && mass == 0.0)) {
         loss = 0.0f;
         factor = -1.0f;
     }
     if (bad) loss = other = factor = nan;
     g.loss[row] = loss;
-    *reinterpret_cast<float4 *>(g.stats + 4 * row) = float4{st.m, ln_s, other, factor};
+    *reinterpret_cast<float4 *>(g.stats + 4 * row) = 
+        float4{st.m, static_cast<float>(ln_s), other, factor};
 }
 
 // q times its factor everywhere, then the few named places of the part once
 // more, q minus the teacher's probability.  Their logits are read before the
 // first store, so that the gradient may replace the logits.
 template <class T>
-__global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs g) {
+__global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g) {
     __shared__ uint32_t place[DF11_MAX_TOP], many;
     const uint64_t row = blockIdx.x / g.parts;
     const uint32_t part = (blockIdx.x % g.parts) * kPart;
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
     auto *out = static_cast<typename T::raw *>(g.grad) + row * g.grad_stride;
     Held<T> h;
-    h.load(z, part, g.vocab);
+    h.load(z, part, g.vocab, g.once);
     const float4 st = *reinterpret_cast<const float4 *>(g.stats + 4 * row);
     const float m = st.x, log2_s = st.y * kLog2e, other = st.z, factor = st.w;
-    const float w = (g.weight ? g.weight[row] : 1.0f) * (0.5f * g.two_over_tau);
+    const float w = (g.weight ? g.weight[row] : 1.0f) * (0.5f * g.tau.two_over);
     const bool none = factor < 0.0f;  // not for a NaN
     const float every = factor != factor ? factor : other * w;
 
@@ -749,13 +881,13 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs g) {
         }
     }
     __syncthreads();
-    store_part(h, out, part, g.vocab, [&](float v, uint32_t) {
-        const float y = fmaf(scaled(v, m, g.two_over_tau), kLog2e, -log2_s);
+    store_part(h, out, part, g.vocab, g.once, [&](float v, uint32_t) {
+        const float y = fmaf(scaled(v, m, g.tau.two_over), kLog2e, -log2_s);
         return none ? 0.0f : __builtin_amdgcn_exp2f(y) * every;
     });
     __syncthreads();
     if (mine && !none) {
-        const float y = fmaf(scaled(value, m, g.two_over_tau), kLog2e, -log2_s);
+        const float y = fmaf(scaled(value, m, g.tau.two_over), kLog2e, -log2_s);
         out[at] = T::store((__builtin_amdgcn_exp2f(y) - target * factor) * w);
     }
 }
@@ -763,7 +895,9 @@ __global__ __launch_bounds__(kThreads) void distill_grad_kernel(DistillArgs g) {
 // ---- host side
 constexpr uint64_t kMostParts = 1ull << 23;
 
-uint32_t parts_of(uint32_t vocab) { return (vocab - 1) / kPart + 1; }
+uint32_t parts_of(uint32_t vocab) {
+    return (vocab - 1) / kPart + 1;
+}
 
 int check_logits(const void *logits, uint32_t dtype, uint64_t rows, uint32_t vocab,
                  uint64_t stride) {
@@ -792,6 +926,14 @@ int check_grad(const void *logits, const void *grad, uint32_t dtype, uint64_t ro
 int check_workspace(const void *ws, uint64_t have, uint64_t need) {
     if (have < need) return DF11_E_BUFFER_TOO_SMALL;
     return need && (!ws || misaligned(ws, 16)) ? DF11_E_INVALID_ARG : DF11_OK;
+}
+
+// Whether the logits pass the caches by: from 256 MB, what the memory-side cache
+// holds, a gradient would not find there what the forward pass read.  4096 x
+// 128,256 bf16, distillation with its gradient: 608 us through the caches, 560
+// past them; 1023 x 32,001 (65 MB), log probabilities with theirs: 46.8 and 49.0.
+bool streams(uint32_t dtype, uint64_t rows, uint32_t vocab) {
+    return rows * vocab * elem_bytes(dtype) >= (256ull << 20);
 }
 
 // The workspace of `all` parts: their statistics, counts and candidates.
@@ -852,7 +994,8 @@ int df11_logprobs(const void *logits, uint32_t dtype, uint64_t rows, uint32_t vo
     LogprobArgs g{logits, tokens, reinterpret_cast<PartStat *>(ws),
                   reinterpret_cast<uint32_t *>(ws + s.count),
                   reinterpret_cast<uint2 *>(ws + s.candidate), logprob, entropy, top_logprob, stats,
-                  rank, top_index, row_stride, vocab, parts, top, room_of(top), 2.0f / temperature};
+                  rank, top_index, row_stride, vocab, parts, top, room_of(top), Tau(temperature),
+                  top || streams(dtype, rows, vocab)};
     if (top)
         DF11_BY_DTYPE(dtype, logprob_top_kernel, rows * parts, kThreads, stream, g);
     else
@@ -878,7 +1021,8 @@ int df11_logprobs_backward(const void *logits, uint32_t dtype, uint64_t rows, ui
         misaligned(grad_entropy, 4))
         return DF11_E_INVALID_ARG;
     LogprobGradArgs g{logits, grad, tokens, stats, grad_logprob, grad_entropy, row_stride,
-                      grad_stride, vocab, parts_of(vocab), 2.0f / temperature};
+                      grad_stride, vocab, parts_of(vocab), Tau(temperature),
+                      streams(dtype, rows, vocab)};
     DF11_BY_DTYPE(dtype, logprob_grad_kernel, rows * g.parts, kThreads, stream, g);
     return launched();
 }
@@ -912,7 +1056,7 @@ int df11_distill(const void *logits, uint32_t dtype, uint64_t rows, uint32_t voc
     if (rc) return rc;
     DistillArgs g{logits, grad, teacher_index, teacher_logprob, weight,
                   static_cast<PartStat *>(workspace), loss, stats, row_stride, grad_stride, vocab,
-                  parts, top, tail, 2.0f / temperature};
+                  parts, top, tail, Tau(temperature), streams(dtype, rows, vocab)};
     DF11_BY_DTYPE(dtype, distill_part_kernel, rows * parts, kThreads, stream, g);
     if ((rc = launched())) return rc;
     DF11_BY_DTYPE(dtype, distill_join_kernel, rows, 64, stream, g);
@@ -938,7 +1082,7 @@ int df11_distill_backward(const void *logits, uint32_t dtype, uint64_t rows, uin
         return DF11_E_INVALID_ARG;
     DistillArgs g{logits, grad, teacher_index, teacher_logprob, grad_loss, nullptr, nullptr,
                   const_cast<float *>(stats), row_stride, grad_stride, vocab, parts_of(vocab), top,
-                  tail, 2.0f / temperature};
+                  tail, Tau(temperature), streams(dtype, rows, vocab)};
     DF11_BY_DTYPE(dtype, distill_grad_kernel, rows * g.parts, kThreads, stream, g);
     return launched();
 }
