@@ -137,7 +137,7 @@ int df11_distill_backward(const void *logits, uint32_t dtype, uint64_t rows, uin
  * its loads.  The low-rank intermediate keeps 16 bits of mantissa where it
  * meets the matrix cores (two BF16 terms).
  * rank a multiple of 8, 8 <= rank <= DF11_MAX_RANK; cols a multiple of 64 and
- * rows of 16 (as df11_matrix); tokens < 2^31; rows of every tensor 16-byte
+ * rows of 16 (as df11_matrix); tokens <= 2^24; rows of every tensor 16-byte
  * aligned (strides: multiples of 8 BF16 or 4 floats).  tokens = 0 launches
  * nothing.
  *

@@ -1,100 +1,545 @@
 // Low-rank adapters of many requests beside a shared projection, and their
-// gradients.
+// gradients.  With v[t] = A_i x[t] and u[t] = s_i B_i^T dy[t], i the adapter of t:
+//   out = base + s_i B_i v      dx = dx_base + A_i^T u
+//   dA_i = sum u x^T            dB_i = s_i sum dy v^T
+//
+// A rank of 8 to 128 against thousands of columns: everything is bound by
+// reading x, base and dy and writing out and dx once; the products are small and
+// go to the matrix cores (v_mfma_f32_16x16x32_bf16) so that nothing else gets in
+// the way.  Four kernels:
+//   shrink  u and v: 16 tokens by all ranks, the columns over the waves of a
+//           workgroup and over workgroups (partial sums; `expand` and `prepare`
+//           add them in order), so that one token alone still has many loads
+//           under way;
+//   expand  out and dx: 64 columns by 16 tokens a wave, through LDS so that base
+//           and out are read and written in whole rows;
+//   prepare u and v per rank, tokens side by side, for the gradients;
+//   outer   dA and dB: 64 columns a wave over a chunk of tokens, partial sums
+//           for several chunks, then `join`.
+// u and v are sums in 32 bits; where they meet the matrix cores they are split
+// into two BF16 terms (16 bits of mantissa: an fp32 output is good to 2^-17 of
+// the adapter's part), and so is an fp32 dy.  x, A, B and a BF16 dy are BF16 and
+// lose nothing.  A tile of tokens may hold several adapters: a kernel goes
+// through the distinct ones, each for its own tokens' rows; up to kFewTokens
+// tokens they are spread over workgroups instead.  A workgroup reads which
+// adapters its tokens have from `adapter`: nothing is sorted or prepared.
 #include "df11_ops_common.h"
+
+#include <algorithm>
+#include <type_traits>
 
 namespace {
 
 using namespace df11ops;
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 constexpr uint32_t kThreads = 256;
+constexpr uint32_t kWaves = kThreads / 64;
+constexpr uint32_t kTile = 16;        // tokens of a matrix product
+constexpr uint32_t kFewTokens = 256;  // up to these, a workgroup an adapter of a tile
 
-// low[t][r] = scale * sum_c x[t][c] * w[i][r * wr + c * wc], one wave each; 0
-// for a token without an adapter.
-struct ShrinkArgs {
-    const void *x;
-    const uint16_t *w;
-    const float *scale;
-    const int32_t *adapter;
-    float *low;
-    uint64_t x_stride;
-    uint32_t len, rank, n_adapters, wr, wc;
-};
-
-template <class T>
-__global__ __launch_bounds__(64) void lora_shrink_kernel(ShrinkArgs g) {
-    const uint64_t t = blockIdx.x;
-    const uint32_t r = blockIdx.y;
-    const int32_t i = g.adapter[t];
-    if (i < 0 || static_cast<uint32_t>(i) >= g.n_adapters) {
-        if (threadIdx.x == 0) g.low[t * g.rank + r] = 0.0f;
-        return;
-    }
-    const auto *x = static_cast<const typename T::raw *>(g.x) + t * g.x_stride;
-    const uint16_t *w = g.w + static_cast<uint64_t>(i) * g.len * g.rank + static_cast<uint64_t>(r) * g.wr;
-    float s = 0.0f;
-    for (uint32_t c = threadIdx.x; c < g.len; c += 64)
-        s += T::load(x[c]) * BF16::load(w[static_cast<uint64_t>(c) * g.wc]);
-    s = wave_sum(s);
-    if (threadIdx.x == 0) g.low[t * g.rank + r] = s * (g.scale ? g.scale[i] : 1.0f);
+__device__ f32x4 mfma(const uint4 &a, const uint4 &b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// out[t][c] = base[t][c] + sum_r low[t][r] * w[i][c * wc + r * wr]
+// Eight floats as the sum of two BF16 terms each.
+__device__ void split8(const float *v, uint4 *high, uint4 *low) {
+    bf16x8 h, l;
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+        h[e] = static_cast<__bf16>(v[e]);
+        // an infinity or NaN is all in the first term
+        const float rest = v[e] - static_cast<float>(h[e]);
+        l[e] = static_cast<__bf16>(fabsf(static_cast<float>(h[e])) < INFINITY ? rest : 0.0f);
+    }
+    *high = __builtin_bit_cast(uint4, h);
+    *low = __builtin_bit_cast(uint4, l);
+}
+
+__device__ uint4 zero4() { return uint4{0, 0, 0, 0}; }
+
+// The adapter of a token, -1 for none; -2 past the last token.
+__device__ int32_t adapter_of(const int32_t *adapter, uint64_t t, uint64_t tokens, uint32_t n) {
+    if (t >= tokens) return -2;
+    const int32_t i = adapter[t];
+    return i >= 0 && static_cast<uint32_t>(i) < n ? i : -1;
+}
+
+// Calls f(adapter, its tokens' bits) for the distinct adapters from `least` on of
+// a tile; `id` is that of token lane % 16.  Workgroup z of gridDim.z takes every
+// gridDim.z-th of them.
+template <class F>
+__device__ void each_adapter(int32_t id, int32_t least, F f) {
+    uint32_t left = static_cast<uint32_t>(__ballot(id >= least)) & 0xFFFFu, turn = 0;
+    while (left) {
+        const int32_t a = __builtin_amdgcn_readlane(id, __builtin_ctz(left));
+        const uint32_t mine = static_cast<uint32_t>(__ballot(id == a)) & 0xFFFFu;
+        left &= ~mine;
+        if (turn++ % gridDim.z == blockIdx.z) f(a, mine);
+    }
+}
+
+// ---------------------------------------------------------------------- shrink
+// part[split][t][r] = sum over the split's columns of x[t][c] w[i][r][c]; rows of
+// tokens without an adapter are not written (nor read later).
+struct ShrinkJob {
+    const void *x;
+    const uint16_t *w;  // n_adapters x rank x len
+    float *part;
+    uint64_t stride;
+    uint32_t len, per, splits;  // columns, columns of a split (a multiple of 256)
+};
+struct ShrinkArgs {
+    ShrinkJob job[2];  // splits of the first, then of the second, along gridDim.y
+    const int32_t *adapter;
+    uint64_t tokens;
+    uint32_t rank, n_adapters;
+};
+
+template <class T, uint32_t kRanks>
+__device__ void shrink(const ShrinkArgs &g, const ShrinkJob &j, uint32_t split, float *red) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, q = lane >> 4;
+    const uint64_t t0 = uint64_t{blockIdx.x} * kTile, t = t0 + c;
+    const int32_t id = adapter_of(g.adapter, t, g.tokens, g.n_adapters);
+    const auto *x =
+        static_cast<const typename T::raw *>(j.x) + std::min(t, g.tokens - 1) * j.stride;
+    const uint32_t from = split * j.per, to = min(j.len, from + j.per);
+    each_adapter(id, 0, [&](int32_t a, uint32_t mine) {
+        const uint16_t *w = j.w + static_cast<uint64_t>(a) * g.rank * j.len;
+        f32x4 acc[kRanks];
+#pragma unroll
+        for (uint32_t r = 0; r < kRanks; ++r) acc[r] = f32x4{0, 0, 0, 0};
+        // 64 columns a step: lane group q takes 16 of them, in both operands
+        for (uint32_t k0 = from + 64 * wave; k0 < to; k0 += 64 * kWaves) {
+            const uint32_t k = k0 + 16 * q;
+            const bool in = k < to;  // lengths are multiples of 16
+            uint4 xh[2], xl[2];
+            if constexpr (T::kVec == 4) {
+                float v[16];
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) {
+                    const uint4 p = in ? *reinterpret_cast<const uint4 *>(x + k + 4 * e) : zero4();
+                    for (uint32_t i = 0; i < 4; ++i) v[4 * e + i] = F32::get(p, i);
+                }
+                split8(v, &xh[0], &xl[0]);
+                split8(v + 8, &xh[1], &xl[1]);
+            } else {
+                xh[0] = in ? *reinterpret_cast<const uint4 *>(x + k) : zero4();
+                xh[1] = in ? *reinterpret_cast<const uint4 *>(x + k + 8) : zero4();
+            }
+#pragma unroll
+            for (uint32_t r = 0; r < kRanks; ++r) {
+                const uint16_t *wr = w + static_cast<uint64_t>(min(16 * r + c, g.rank - 1)) * j.len;
+#pragma unroll
+                for (uint32_t e = 0; e < 2; ++e) {
+                    const uint4 b = in ? *reinterpret_cast<const uint4 *>(wr + k + 8 * e) : zero4();
+                    acc[r] = mfma(xh[e], b, acc[r]);
+                    if constexpr (T::kVec == 4) acc[r] = mfma(xl[e], b, acc[r]);
+                }
+            }
+        }
+        // the waves' sums through LDS: token 4q + e, rank 16r + c
+        __syncthreads();
+#pragma unroll
+        for (uint32_t r = 0; r < kRanks; ++r)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+                red[(wave * kTile + 4 * q + e) * (16 * kRanks) + 16 * r + c] = acc[r][e];
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < kTile * 16 * kRanks; i += kThreads) {
+            const uint32_t row = i / (16 * kRanks), r = i % (16 * kRanks);
+            if (!(mine >> row & 1u) || r >= g.rank) continue;
+            float s = 0.0f;
+            for (uint32_t v = 0; v < kWaves; ++v) s += red[v * kTile * 16 * kRanks + i];
+            j.part[(split * g.tokens + t0 + row) * g.rank + r] = s;
+        }
+    });
+}
+
+template <class T, uint32_t kRanks>
+__global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs g) {
+    __shared__ float red[kWaves * kTile * 16 * kRanks];
+    if (blockIdx.y < g.job[0].splits)
+        shrink<T, kRanks>(g, g.job[0], blockIdx.y, red);
+    else
+        shrink<BF16, kRanks>(g, g.job[1], blockIdx.y - g.job[0].splits, red);
+}
+
+// ---------------------------------------------------------------------- expand
+// out[t][c] = base[t][c] + scale[i] * sum_r low[t][r] w[i][c][r], low the sum of
+// the parts.
 struct ExpandArgs {
-    const float *low;
-    const uint16_t *w;
+    const float *part;
+    const uint16_t *w;  // n_adapters x len x rank
+    const float *scale;
     const int32_t *adapter;
     const void *base;
     void *out;
-    uint64_t base_stride, out_stride;
-    uint32_t len, rank, n_adapters, wr, wc;
+    uint64_t tokens, base_stride, out_stride;
+    uint32_t len, rank, n_adapters, splits, blocks;  // blocks: of 256 columns
 };
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
-    const uint64_t t = blockIdx.x;
-    const uint32_t c = blockIdx.y * kThreads + threadIdx.x;
-    if (c >= g.len) return;
-    const int32_t i = g.adapter[t];
-    float s = g.base ? T::load(static_cast<const typename T::raw *>(g.base)[t * g.base_stride + c]) : 0.0f;
-    if (i >= 0 && static_cast<uint32_t>(i) < g.n_adapters) {
-        const uint16_t *w = g.w + static_cast<uint64_t>(i) * g.len * g.rank + static_cast<uint64_t>(c) * g.wc;
-        float d = 0.0f;
-        for (uint32_t r = 0; r < g.rank; ++r)
-            d += g.low[t * g.rank + r] * BF16::load(w[static_cast<uint64_t>(r) * g.wr]);
-        s += d;
-    }
-    static_cast<typename T::raw *>(g.out)[t * g.out_stride + c] = T::store(s);
+__device__ void wave_lds_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
-// d[i][c * wc + r * wr] = sum_{t of i} low[t][r] * x[t][c]
-struct OuterArgs {
-    const void *x;
-    const float *low;
-    const int32_t *adapter;
-    float *d;
-    uint64_t x_stride, tokens;
-    uint32_t len, rank, wr, wc;
+// kSteps products of 32 ranks; 0: up to 16 ranks, where one product holds both
+// terms of the split.
+template <class T, uint32_t kSteps, uint32_t kTiles>
+__global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
+    constexpr uint32_t kFrags = kSteps ? kSteps : 1, kCols = 64, kRow = kCols + 4;
+    constexpr uint32_t kLanes = kCols / T::kVec;  // lanes that share a row of base and out
+    constexpr uint32_t kTrips = kTile * kLanes / 64;
+    __shared__ float tile[kWaves][kTile * kRow];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, q = lane >> 4;
+    float *const mytile = tile[wave];
+    const uint32_t n0 = (blockIdx.x % g.blocks * kWaves + wave) * kCols;
+    const uint64_t group = blockIdx.x / g.blocks;
+    if (n0 >= g.len) return;  // no barrier of the workgroup below
+    const uint32_t col = n0 + T::kVec * (lane % kLanes);
+    const auto *base = static_cast<const typename T::raw *>(g.base);
+    auto *out = static_cast<typename T::raw *>(g.out);
+    int32_t loaded = -1;
+    uint4 w[4][kFrags];
+#pragma unroll 1
+    for (uint32_t s = 0; s < kTiles; ++s) {
+        const uint64_t t0 = (group * kTiles + s) * kTile;
+        if (t0 >= g.tokens) return;
+        const int32_t id = adapter_of(g.adapter, t0 + c, g.tokens, g.n_adapters);
+        each_adapter(id, -1, [&](int32_t a, uint32_t mine) {
+            uint4 held[kTrips];
+#pragma unroll
+            for (uint32_t i = 0; i < kTrips; ++i) {
+                const uint32_t row = i * (64 / kLanes) + lane / kLanes;
+                held[i] = zero4();
+                if (base && (mine >> row & 1u) && col < g.len)
+                    held[i] = *reinterpret_cast<const uint4 *>(base + (t0 + row) * g.base_stride + col);
+            }
+            if (a >= 0) {
+                if (a != loaded) {
+                    loaded = a;
+                    const uint16_t *wa = g.w + static_cast<uint64_t>(a) * g.len * g.rank;
+#pragma unroll
+                    for (uint32_t f = 0; f < 4; ++f)
+#pragma unroll
+                        for (uint32_t k = 0; k < kFrags; ++k) {
+                            const uint32_t r = kSteps ? 32 * k + 8 * q : 8 * (q & 1u);
+                            const uint32_t n = min(n0 + 16 * f + c, g.len - 1);
+                            w[f][k] = r < g.rank ? *reinterpret_cast<const uint4 *>(
+                                                       wa + static_cast<uint64_t>(n) * g.rank + r)
+                                                 : zero4();
+                        }
+                }
+                const float scale = g.scale ? g.scale[a] : 1.0f;
+                uint4 high[kFrags], low[kFrags];
+#pragma unroll
+                for (uint32_t k = 0; k < kFrags; ++k) {
+                    const uint32_t r = kSteps ? 32 * k + 8 * q : 8 * (q & 1u);
+                    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    if (r < g.rank && (mine >> c & 1u))
+                        for (uint32_t p = 0; p < g.splits; ++p) {
+                            const auto *from = reinterpret_cast<const float4 *>(
+                                g.part + (p * g.tokens + t0 + c) * g.rank + r);
+                            const float4 x = from[0], y = from[1];
+                            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+                            v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+                        }
+#pragma unroll
+                    for (uint32_t e = 0; e < 8; ++e) v[e] *= scale;
+                    split8(v, &high[k], &low[k]);
+                }
+                if (!kSteps && q >= 2) high[0] = low[0];
+                // column 16f + 4q + e of token c
+#pragma unroll
+                for (uint32_t f = 0; f < 4; ++f) {
+                    f32x4 acc{0, 0, 0, 0};
+#pragma unroll
+                    for (uint32_t k = 0; k < kFrags; ++k) {
+                        acc = mfma(w[f][k], high[k], acc);
+                        if (kSteps) acc = mfma(w[f][k], low[k], acc);
+                    }
+                    *reinterpret_cast<f32x4 *>(mytile + c * kRow + 16 * f + 4 * q) = acc;
+                }
+                wave_lds_sync();
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < kTrips; ++i) {
+                const uint32_t row = i * (64 / kLanes) + lane / kLanes;
+                typename T::raw o[T::kVec];
+                const float *d = mytile + row * kRow + T::kVec * (lane % kLanes);
+#pragma unroll
+                for (uint32_t e = 0; e < T::kVec; e += 4) {
+                    const f32x4 v = a >= 0 ? *reinterpret_cast<const f32x4 *>(d + e) : f32x4{0, 0, 0, 0};
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) o[e + k] = T::store(T::get(held[i], e + k) + v[k]);
+                }
+                if ((mine >> row & 1u) && col < g.len)
+                    *reinterpret_cast<uint4 *>(out + (t0 + row) * g.out_stride + col) =
+                        a >= 0 ? __builtin_bit_cast(uint4, o) : held[i];
+            }
+            wave_lds_sync();
+        });
+    }
+}
+
+// --------------------------------------------------------------- the gradients
+// to[i][r][c] = from[i][c][r], 64 c a workgroup; two matrices, along gridDim.y.
+struct TransposeJob {
+    const uint16_t *from;
+    uint16_t *to;
+    uint32_t rows, cols;  // of `from`
+};
+struct TransposeArgs {
+    TransposeJob job[2];
 };
 
-template <class T>
+__global__ __launch_bounds__(kThreads) void lora_transpose_kernel(TransposeArgs g) {
+    constexpr uint32_t kSide = 64;
+    __shared__ uint16_t tile[kSide][kSide + 2];
+    const TransposeJob j = g.job[blockIdx.y];
+    const uint32_t across = (j.cols + kSide - 1) / kSide, down = (j.rows + kSide - 1) / kSide;
+    if (blockIdx.x >= across * down) return;
+    const uint32_t r0 = blockIdx.x / across * kSide, c0 = blockIdx.x % across * kSide;
+    const uint64_t at = uint64_t{blockIdx.z} * j.rows * j.cols;
+    for (uint32_t i = threadIdx.x; i < kSide * kSide; i += kThreads) {
+        const uint32_t r = i / kSide, c = i % kSide;
+        if (r0 + r < j.rows && c0 + c < j.cols)
+            tile[r][c] = j.from[at + static_cast<uint64_t>(r0 + r) * j.cols + c0 + c];
+    }
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kSide * kSide; i += kThreads) {
+        const uint32_t c = i / kSide, r = i % kSide;
+        if (r0 + r < j.rows && c0 + c < j.cols)
+            j.to[at + static_cast<uint64_t>(c0 + c) * j.rows + r0 + r] = tile[r][c];
+    }
+}
+
+// u and v as two BF16 terms each, a row of `padded` tokens per rank: terms[0..1]
+// of the first, terms[2..3] of the second.  0 for tokens without an adapter and
+// past the last one.
+struct PrepareArgs {
+    const float *part[2];
+    uint16_t *terms;
+    const float *scale;
+    const int32_t *adapter;
+    uint64_t tokens, padded;
+    uint32_t splits[2], rank, n_adapters;
+};
+
+__global__ __launch_bounds__(kThreads) void lora_prepare_kernel(PrepareArgs g) {
+    __shared__ float tile[DF11_MAX_RANK][33];
+    const uint64_t t0 = uint64_t{blockIdx.x} * 32;
+    const uint32_t job = blockIdx.y;
+    for (uint32_t i = threadIdx.x; i < 32 * g.rank; i += kThreads) {
+        const uint32_t row = i / g.rank, r = i % g.rank;
+        const int32_t a = adapter_of(g.adapter, t0 + row, g.tokens, g.n_adapters);
+        float s = 0.0f;
+        if (a >= 0) {
+            for (uint32_t p = 0; p < g.splits[job]; ++p)
+                s += g.part[job][(p * g.tokens + t0 + row) * g.rank + r];
+            s *= g.scale ? g.scale[a] : 1.0f;
+        }
+        tile[r][row] = s;
+    }
+    __syncthreads();
+    uint16_t *high = g.terms + 2 * job * g.rank * g.padded, *low = high + g.rank * g.padded;
+    for (uint32_t i = threadIdx.x; i < 32 * g.rank; i += kThreads) {
+        const uint32_t r = i / 32, row = i % 32;
+        const float v = tile[r][row];
+        const uint16_t h = BF16::store(v);
+        high[r * g.padded + t0 + row] = h;
+        low[r * g.padded + t0 + row] =
+            BF16::store(fabsf(BF16::load(h)) < INFINITY ? v - BF16::load(h) : 0.0f);
+    }
+}
+
+// d[i][...] = sum over the chunk's tokens t of i: m[t][c] w[t][r]
+struct OuterJob {
+    const void *m;
+    const uint16_t *terms;  // two terms of w, each rank x padded
+    float *d;               // n_adapters x len x rank, or rank x len: a chunk's
+    uint64_t stride, chunk_floats;
+    uint32_t len, blocks;
+    bool rank_rows;  // d is rank x len
+};
+struct OuterArgs {
+    OuterJob job[2];
+    const int32_t *adapter;
+    uint32_t *present;  // chunks x n_adapters; null: one chunk, straight into d
+    uint64_t tokens, padded, per;  // per: tokens of a chunk, a multiple of 32
+    uint32_t rank, n_adapters;
+};
+
+constexpr uint32_t kScan = 4096;  // tokens whose adapters are looked at together
+
+template <class T, uint32_t kRanks>
+__device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uint32_t *member) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, q = lane >> 4;
+    const int32_t a = blockIdx.z;
+    const uint32_t c0 = (block * kWaves + wave) * 64;
+    // lane group q takes tokens 8q..8q+7 of a step, lane c of it columns 4c..4c+3
+    const uint32_t col = min(c0 + 4 * c, j.len - 4);
+    const auto *m = static_cast<const typename T::raw *>(j.m);
+    const uint16_t *high = j.terms, *low = high + g.rank * g.padded;
+    const uint64_t from = uint64_t{blockIdx.y} * g.per, to = std::min(g.tokens, from + g.per);
+    f32x4 acc[4][kRanks];
+#pragma unroll
+    for (uint32_t e = 0; e < 4; ++e)
+#pragma unroll
+        for (uint32_t r = 0; r < kRanks; ++r) acc[e][r] = f32x4{0, 0, 0, 0};
+    bool some = false;
+    for (uint64_t s0 = from; s0 < to; s0 += kScan) {
+        // a bit for each token: is it this adapter's
+        __syncthreads();
+        const uint32_t scan = static_cast<uint32_t>(std::min<uint64_t>(kScan, to - s0));
+        for (uint32_t i = threadIdx.x; i - lane < scan; i += kThreads) {
+            const uint64_t all = __ballot(i < scan && g.adapter[s0 + min(i, scan - 1)] == a);
+            if (lane < 2) member[i / 64 * 2 + lane] = static_cast<uint32_t>(all >> (32 * lane));
+        }
+        __syncthreads();
+        const uint32_t steps = (scan + 31) / 32;
+        using Row = typename std::conditional<T::kVec == 4, uint4, uint2>::type;
+        for (uint32_t s = 0; s < steps; ++s) {
+            const uint32_t bits = __builtin_amdgcn_readfirstlane(member[s]);
+            if (!bits) continue;
+            some = true;
+            const uint64_t t0 = s0 + 32 * s;
+            const uint32_t ours = bits >> (8 * q) & 0xFFu;
+            Row row[8];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                const uint64_t t = std::min(t0 + 8 * q + i, g.tokens - 1);
+                row[i] = *reinterpret_cast<const Row *>(m + t * j.stride + col);
+            }
+            uint4 wh[kRanks], wl[kRanks];
+#pragma unroll
+            for (uint32_t r = 0; r < kRanks; ++r) {
+                const uint64_t at = min(16 * r + c, g.rank - 1) * g.padded + t0 + 8 * q;
+                wh[r] = *reinterpret_cast<const uint4 *>(high + at);
+                wl[r] = *reinterpret_cast<const uint4 *>(low + at);
+            }
+            if (bits != ~0u) {
+                // other adapters' tokens: whatever they hold must not count
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (!(ours >> i & 1u)) row[i] = Row{};
+                uint32_t keep[4];
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    keep[i] = (ours >> (2 * i) & 1u ? 0xFFFFu : 0u) |
+                              (ours >> (2 * i + 1) & 1u ? 0xFFFF0000u : 0u);
+#pragma unroll
+                for (uint32_t r = 0; r < kRanks; ++r) {
+                    wh[r].x &= keep[0], wh[r].y &= keep[1], wh[r].z &= keep[2], wh[r].w &= keep[3];
+                    wl[r].x &= keep[0], wl[r].y &= keep[1], wl[r].z &= keep[2], wl[r].w &= keep[3];
+                }
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) {
+                // column 4c + e of the lane's eight tokens
+                uint4 mh, ml = zero4();
+                if constexpr (T::kVec == 4) {
+                    float v[8];
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) v[i] = F32::get(row[i], e);
+                    split8(v, &mh, &ml);
+                } else {
+                    uint32_t p[4];
+                    const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        const uint32_t x = e < 2 ? row[2 * i].x : row[2 * i].y;
+                        const uint32_t y = e < 2 ? row[2 * i + 1].x : row[2 * i + 1].y;
+                        p[i] = __builtin_amdgcn_perm(y, x, pick);
+                    }
+                    mh = uint4{p[0], p[1], p[2], p[3]};
+                }
+#pragma unroll
+                for (uint32_t r = 0; r < kRanks; ++r) {
+                    acc[e][r] = mfma(mh, wh[r], acc[e][r]);
+                    acc[e][r] = mfma(mh, wl[r], acc[e][r]);
+                    if constexpr (T::kVec == 4) acc[e][r] = mfma(ml, wh[r], acc[e][r]);
+                }
+            }
+        }
+    }
+    if (g.present) {
+        if (block == 0 && threadIdx.x == 0 && blockIdx.x == 0)
+            g.present[blockIdx.y * g.n_adapters + a] = some ? 1u : 0u;
+        if (!some) return;
+    }
+    // acc[e][r][k]: column 4 (4q + k) + e, rank 16r + c
+    float *d = j.d + blockIdx.y * j.chunk_floats + static_cast<uint64_t>(a) * j.len * g.rank;
+#pragma unroll
+    for (uint32_t r = 0; r < kRanks; ++r) {
+        const uint32_t rank = 16 * r + c;
+        if (rank >= g.rank) continue;
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+            const uint32_t n = c0 + 16 * q + 4 * k;
+            if (n >= j.len) continue;
+            if (j.rank_rows) {
+                *reinterpret_cast<f32x4 *>(d + static_cast<uint64_t>(rank) * j.len + n) =
+                    f32x4{acc[0][r][k], acc[1][r][k], acc[2][r][k], acc[3][r][k]};
+            } else {
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+                    d[static_cast<uint64_t>(n + e) * g.rank + rank] = acc[e][r][k];
+            }
+        }
+    }
+}
+
+template <class T, uint32_t kRanks>
 __global__ __launch_bounds__(kThreads) void lora_outer_kernel(OuterArgs g) {
-    const uint32_t c = blockIdx.x * kThreads + threadIdx.x, r = blockIdx.y, i = blockIdx.z;
-    if (c >= g.len) return;
-    float s = 0.0f;
-    for (uint64_t t = 0; t < g.tokens; ++t)
-        if (g.adapter[t] == static_cast<int32_t>(i))
-            s += g.low[t * g.rank + r] *
-                 T::load(static_cast<const typename T::raw *>(g.x)[t * g.x_stride + c]);
-    g.d[static_cast<uint64_t>(i) * g.len * g.rank + static_cast<uint64_t>(c) * g.wc +
-        static_cast<uint64_t>(r) * g.wr] = s;
+    __shared__ uint32_t member[kScan / 32];
+    if (blockIdx.x < g.job[0].blocks)
+        outer<T, kRanks>(g, g.job[0], blockIdx.x, member);
+    else
+        outer<BF16, kRanks>(g, g.job[1], blockIdx.x - g.job[0].blocks, member);
+}
+
+// d = the chunks' sums in order; 0 for an adapter without tokens.
+struct JoinArgs {
+    const float *from[2];
+    float *to[2];
+    const uint32_t *present;
+    uint64_t each[2], all[2];  // floats of an adapter, of all of them
+    uint32_t chunks, n_adapters;
+};
+
+__global__ __launch_bounds__(kThreads) void lora_join_kernel(JoinArgs g) {
+    const uint32_t job = blockIdx.y;
+    for (uint64_t i = (uint64_t{blockIdx.x} * kThreads + threadIdx.x) * 4; i < g.all[job];
+         i += uint64_t{gridDim.x} * kThreads * 4) {
+        const uint32_t a = static_cast<uint32_t>(i / g.each[job]);
+        f32x4 s{0, 0, 0, 0};
+        for (uint32_t k = 0; k < g.chunks; ++k)
+            if (g.present[k * g.n_adapters + a])
+                s += *reinterpret_cast<const f32x4 *>(g.from[job] + k * g.all[job] + i);
+        *reinterpret_cast<f32x4 *>(g.to[job] + i) = s;
+    }
+}
+
+// Zeros, where there are no tokens: a kernel, which a graph may record.
+__global__ __launch_bounds__(kThreads) void lora_zero_kernel(float *p, uint64_t n) {
+    for (uint64_t i = uint64_t{blockIdx.x} * kThreads + threadIdx.x; i < n;
+         i += uint64_t{gridDim.x} * kThreads)
+        p[i] = 0.0f;
 }
 
 // ---- host side
+uint64_t up(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
+
 int check_shapes(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank,
                  uint32_t n_adapters) {
     if (!cols || !rows || !rank || !n_adapters) return DF11_E_INVALID_ARG;
-    if (cols % 64 || rows % 16 || rank % 8 || rank > DF11_MAX_RANK || tokens > 0x7FFFFFFFull ||
-        n_adapters > 65535u || cols > (1u << 24) || rows > (1u << 24))
+    if (cols % 64 || rows % 16 || rank % 8 || rank > DF11_MAX_RANK || tokens > (1ull << 24) ||
+        n_adapters > 65535u || cols > (1u << 23) || rows > (1u << 23))
         return DF11_E_UNSUPPORTED;
     return DF11_OK;
 }
@@ -122,6 +567,117 @@ int check_workspace(const void *ws, uint64_t have, uint64_t need) {
     return need && (!ws || misaligned(ws, 16)) ? DF11_E_INVALID_ARG : DF11_OK;
 }
 
+// Columns of a split and how many splits: about 1024 workgroups in all, each of
+// at least 512 columns (two steps of its four waves), at most 32 sums to add.
+void split_columns(uint32_t len, uint64_t tokens, uint32_t n_adapters, ShrinkJob *j) {
+    const uint64_t tiles = (tokens + kTile - 1) / kTile;
+    const uint64_t wgs = tiles * (tokens <= kFewTokens ? std::min<uint64_t>({16, n_adapters, tokens}) : 1);
+    const uint32_t most = std::min(32u, std::max(1u, len / 512));
+    const uint32_t want = static_cast<uint32_t>(std::min<uint64_t>(most, (1024 + wgs - 1) / wgs));
+    j->len = len;
+    j->per = static_cast<uint32_t>(up((len + want - 1) / want, 256));
+    j->splits = (len + j->per - 1) / j->per;
+}
+
+// Tokens of a chunk of the gradients: about 512 workgroups, chunks of at least 128
+// tokens, and at most 128 MB of partial sums.
+uint64_t chunk_tokens(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank,
+                      uint32_t n_adapters) {
+    const uint64_t blocks = (cols + 255) / 256 + (rows + 255) / 256;
+    const uint64_t each = 4ull * n_adapters * rank * (uint64_t{cols} + rows);
+    uint64_t chunks = std::min((512 + blocks - 1) / blocks, (tokens + 127) / 128);
+    chunks = std::max<uint64_t>(1, std::min<uint64_t>(chunks, (128ull << 20) / each));
+    return up((tokens + chunks - 1) / chunks, 32);
+}
+
+template <class T>
+int launch_shrink(const ShrinkArgs &s, hipStream_t stream) {
+    const dim3 grid((s.tokens + kTile - 1) / kTile, s.job[0].splits + s.job[1].splits,
+                    s.tokens <= kFewTokens ? std::min<uint64_t>({16, s.n_adapters, s.tokens}) : 1);
+    const dim3 block(kThreads);
+    const uint32_t ranks = (s.rank + 15) / 16;
+    if (ranks == 1)
+        hipLaunchKernelGGL((lora_shrink_kernel<T, 1>), grid, block, 0, stream, s);
+    else if (ranks == 2)
+        hipLaunchKernelGGL((lora_shrink_kernel<T, 2>), grid, block, 0, stream, s);
+    else if (ranks <= 4)
+        hipLaunchKernelGGL((lora_shrink_kernel<T, 4>), grid, block, 0, stream, s);
+    else
+        hipLaunchKernelGGL((lora_shrink_kernel<T, 8>), grid, block, 0, stream, s);
+    return launched();
+}
+
+template <class T, uint32_t kTiles>
+int launch_expand(ExpandArgs e, hipStream_t stream) {
+    e.blocks = (e.len + 255) / 256;
+    const uint64_t wgs = (e.tokens + kTile * kTiles - 1) / (kTile * kTiles) * e.blocks;
+    if (wgs > 0xFFFFFFFFull / kThreads) return DF11_E_UNSUPPORTED;
+    const dim3 grid(wgs, 1,
+                    kTiles == 1 ? std::min<uint64_t>({16, uint64_t{e.n_adapters} + 1, e.tokens}) : 1);
+    const dim3 block(kThreads);
+    if (e.rank <= 16)
+        hipLaunchKernelGGL((lora_expand_kernel<T, 0, kTiles>), grid, block, 0, stream, e);
+    else if (e.rank <= 32)
+        hipLaunchKernelGGL((lora_expand_kernel<T, 1, kTiles>), grid, block, 0, stream, e);
+    else if (e.rank <= 64)
+        hipLaunchKernelGGL((lora_expand_kernel<T, 2, kTiles>), grid, block, 0, stream, e);
+    else
+        hipLaunchKernelGGL((lora_expand_kernel<T, 4, kTiles>), grid, block, 0, stream, e);
+    return launched();
+}
+
+int launch_expand(const ExpandArgs &e, uint32_t dtype, hipStream_t stream) {
+    if (e.tokens <= kFewTokens)
+        return dtype == DF11_F32 ? launch_expand<F32, 1>(e, stream) : launch_expand<BF16, 1>(e, stream);
+    return dtype == DF11_F32 ? launch_expand<F32, 4>(e, stream) : launch_expand<BF16, 4>(e, stream);
+}
+
+template <class T>
+int launch_outer(const OuterArgs &o, uint64_t chunks, hipStream_t stream) {
+    const dim3 grid(o.job[0].blocks + o.job[1].blocks, chunks, o.n_adapters), block(kThreads);
+    const uint32_t ranks = (o.rank + 15) / 16;
+    if (ranks == 1)
+        hipLaunchKernelGGL((lora_outer_kernel<T, 1>), grid, block, 0, stream, o);
+    else if (ranks == 2)
+        hipLaunchKernelGGL((lora_outer_kernel<T, 2>), grid, block, 0, stream, o);
+    else if (ranks <= 4)
+        hipLaunchKernelGGL((lora_outer_kernel<T, 4>), grid, block, 0, stream, o);
+    else
+        hipLaunchKernelGGL((lora_outer_kernel<T, 8>), grid, block, 0, stream, o);
+    return launched();
+}
+
+// The backward pass's workspace, in bytes from its start.
+struct Space {
+    uint64_t bt, at, u, v, terms, present, db, da, bytes;
+    uint64_t padded, per, chunks;
+    ShrinkJob ju, jv;
+};
+Space space_of(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank, uint32_t n_adapters) {
+    Space s{};
+    s.padded = up(tokens, 32);
+    split_columns(rows, std::max<uint64_t>(tokens, 1), n_adapters, &s.ju);
+    split_columns(cols, std::max<uint64_t>(tokens, 1), n_adapters, &s.jv);
+    s.per = std::max<uint64_t>(32, chunk_tokens(tokens, cols, rows, rank, n_adapters));
+    s.chunks = std::max<uint64_t>(1, (tokens + s.per - 1) / s.per);
+    uint64_t at = 0;
+    const auto take = [&](uint64_t bytes) {
+        const uint64_t from = at;
+        at += up(bytes, 256);
+        return from;
+    };
+    s.bt = take(2ull * n_adapters * rows * rank);
+    s.at = take(2ull * n_adapters * cols * rank);
+    s.u = take(4ull * s.ju.splits * tokens * rank);
+    s.v = take(4ull * s.jv.splits * tokens * rank);
+    s.terms = take(8ull * rank * s.padded);
+    s.present = take(4ull * s.chunks * n_adapters);
+    s.db = take(s.chunks > 1 ? 4ull * s.chunks * n_adapters * rows * rank : 0);
+    s.da = take(s.chunks > 1 ? 4ull * s.chunks * n_adapters * cols * rank : 0);
+    s.bytes = at;
+    return s;
+}
+
 }  // namespace
 
 extern "C" {
@@ -131,7 +687,9 @@ int df11_lora_workspace_bytes(uint64_t tokens, uint32_t cols, uint32_t rows, uin
     if (!bytes) return DF11_E_INVALID_ARG;
     const int rc = check_shapes(tokens, cols, rows, rank, n_adapters);
     if (rc) return rc;
-    *bytes = 4 * tokens * rank;
+    ShrinkJob j{};
+    if (tokens) split_columns(cols, tokens, n_adapters, &j);
+    *bytes = 4 * tokens * rank * j.splits;
     return DF11_OK;
 }
 
@@ -152,24 +710,28 @@ int df11_lora(const uint16_t *x, uint64_t x_stride, uint64_t tokens, uint32_t co
     if (!rc && base == out && tokens > 1 && base_stride != out_stride) rc = DF11_E_INVALID_ARG;
     if (!rc) rc = check_workspace(workspace, workspace_bytes, need);
     if (rc) return rc;
-    float *low = static_cast<float *>(workspace);
-    ShrinkArgs s{x, a, scale, adapter, low, x_stride, cols, rank, n_adapters, cols, 1};
-    hipLaunchKernelGGL(lora_shrink_kernel<BF16>, dim3(tokens, rank), dim3(64), 0, stream, s);
-    if ((rc = launched())) return rc;
-    ExpandArgs e{low, b, adapter, base, out, base_stride, out_stride, rows, rank, n_adapters, 1, rank};
-    const dim3 grid(tokens, (rows + kThreads - 1) / kThreads);
-    if (dtype == DF11_F32)
-        hipLaunchKernelGGL(lora_expand_kernel<F32>, grid, dim3(kThreads), 0, stream, e);
-    else
-        hipLaunchKernelGGL(lora_expand_kernel<BF16>, grid, dim3(kThreads), 0, stream, e);
-    return launched();
+    ShrinkArgs s{};
+    s.job[0].x = x;
+    s.job[0].w = a;
+    s.job[0].part = static_cast<float *>(workspace);
+    s.job[0].stride = x_stride;
+    split_columns(cols, tokens, n_adapters, &s.job[0]);
+    s.adapter = adapter;
+    s.tokens = tokens;
+    s.rank = rank;
+    s.n_adapters = n_adapters;
+    if ((rc = launch_shrink<BF16>(s, stream))) return rc;
+    const ExpandArgs e{s.job[0].part, b, scale, adapter, base, out, tokens, base_stride, out_stride,
+                       rows, rank, n_adapters, s.job[0].splits, 0};
+    return launch_expand(e, dtype, stream);
 }
 
 int df11_lora_backward_workspace_bytes(uint64_t tokens, uint32_t cols, uint32_t rows,
                                        uint32_t rank, uint32_t n_adapters, uint64_t *bytes) {
-    const int rc = df11_lora_workspace_bytes(tokens, cols, rows, rank, n_adapters, bytes);
+    if (!bytes) return DF11_E_INVALID_ARG;
+    const int rc = check_shapes(tokens, cols, rows, rank, n_adapters);
     if (rc) return rc;
-    *bytes = 8 * tokens * rank;
+    *bytes = tokens ? space_of(tokens, cols, rows, rank, n_adapters).bytes : 0;
     return DF11_OK;
 }
 
@@ -185,50 +747,85 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
     if (rc) return rc;
     if (dy_dtype > DF11_BF16 || !da != !db || (!dx && !da)) return DF11_E_INVALID_ARG;
     if (misaligned(da, 16) || misaligned(db, 16)) return DF11_E_INVALID_ARG;
-    if (tokens) {
-        rc = check_common(x, x_stride, tokens, cols, a, b, scale, adapter);
-        if (!rc) rc = check_rows(dy, dy_stride, rows, tokens, elem_bytes(dy_dtype));
-        if (!rc && dx) rc = check_rows(dx, dx_stride, cols, tokens, 2);
-        if (!rc && dx_base) rc = check_rows(dx_base, dx_base_stride, cols, tokens, 2);
-        if (!rc && dx_base && dx_base == dx && tokens > 1 && dx_base_stride != dx_stride)
-            rc = DF11_E_INVALID_ARG;
-        if (!rc) rc = check_workspace(workspace, workspace_bytes, need);
-        if (rc) return rc;
-    }
-    float *u = static_cast<float *>(workspace), *v = u + tokens * rank;
-    if (tokens) {
-        ShrinkArgs s{dy, b, scale, adapter, u, dy_stride, rows, rank, n_adapters, 1, rank};
-        if (dy_dtype == DF11_F32)
-            hipLaunchKernelGGL(lora_shrink_kernel<F32>, dim3(tokens, rank), dim3(64), 0, stream, s);
-        else
-            hipLaunchKernelGGL(lora_shrink_kernel<BF16>, dim3(tokens, rank), dim3(64), 0, stream, s);
+    if (!tokens) {
+        if (!da) return DF11_OK;
+        hipLaunchKernelGGL(lora_zero_kernel, dim3(256), dim3(kThreads), 0, stream, da,
+                           uint64_t{n_adapters} * cols * rank);
         if ((rc = launched())) return rc;
-        if (dx) {
-            ExpandArgs e{u, a, adapter, dx_base, dx, dx_base_stride, dx_stride, cols, rank,
-                         n_adapters, cols, 1};
-            hipLaunchKernelGGL(lora_expand_kernel<BF16>,
-                               dim3(tokens, (cols + kThreads - 1) / kThreads), dim3(kThreads), 0,
-                               stream, e);
-            if ((rc = launched())) return rc;
-        }
+        hipLaunchKernelGGL(lora_zero_kernel, dim3(256), dim3(kThreads), 0, stream, db,
+                           uint64_t{n_adapters} * rows * rank);
+        return launched();
+    }
+    rc = check_common(x, x_stride, tokens, cols, a, b, scale, adapter);
+    if (!rc) rc = check_rows(dy, dy_stride, rows, tokens, elem_bytes(dy_dtype));
+    if (!rc && dx) rc = check_rows(dx, dx_stride, cols, tokens, 2);
+    if (!rc && dx_base) rc = check_rows(dx_base, dx_base_stride, cols, tokens, 2);
+    if (!rc && dx_base && dx_base == dx && tokens > 1 && dx_base_stride != dx_stride)
+        rc = DF11_E_INVALID_ARG;
+    if (!rc) rc = check_workspace(workspace, workspace_bytes, need);
+    if (rc) return rc;
+
+    const Space s = space_of(tokens, cols, rows, rank, n_adapters);
+    char *ws = static_cast<char *>(workspace);
+    auto *bt = reinterpret_cast<uint16_t *>(ws + s.bt), *at = reinterpret_cast<uint16_t *>(ws + s.at);
+    auto *u = reinterpret_cast<float *>(ws + s.u), *v = reinterpret_cast<float *>(ws + s.v);
+    auto *terms = reinterpret_cast<uint16_t *>(ws + s.terms);
+
+    const TransposeArgs t{{{b, bt, rows, rank}, {a, at, rank, cols}}};
+    const uint32_t sides = (rank + 63) / 64 * ((std::max(rows, cols) + 63) / 64);
+    hipLaunchKernelGGL(lora_transpose_kernel, dim3(sides, dx ? 2 : 1, n_adapters), dim3(kThreads),
+                       0, stream, t);
+    if ((rc = launched())) return rc;
+
+    ShrinkArgs h{};
+    h.job[0] = s.ju;
+    h.job[0].x = dy;
+    h.job[0].w = bt;
+    h.job[0].part = u;
+    h.job[0].stride = dy_stride;
+    if (da) {
+        h.job[1] = s.jv;
+        h.job[1].x = x;
+        h.job[1].w = a;
+        h.job[1].part = v;
+        h.job[1].stride = x_stride;
+    }
+    h.adapter = adapter;
+    h.tokens = tokens;
+    h.rank = rank;
+    h.n_adapters = n_adapters;
+    rc = dy_dtype == DF11_F32 ? launch_shrink<F32>(h, stream) : launch_shrink<BF16>(h, stream);
+    if (rc) return rc;
+
+    if (dx) {
+        const ExpandArgs e{u, at, scale, adapter, dx_base, dx, tokens, dx_base_stride, dx_stride,
+                           cols, rank, n_adapters, s.ju.splits, 0};
+        if ((rc = launch_expand(e, DF11_BF16, stream))) return rc;
     }
     if (!da) return DF11_OK;
-    if (tokens) {
-        ShrinkArgs s{x, a, scale, adapter, v, x_stride, cols, rank, n_adapters, cols, 1};
-        hipLaunchKernelGGL(lora_shrink_kernel<BF16>, dim3(tokens, rank), dim3(64), 0, stream, s);
-        if ((rc = launched())) return rc;
-    }
-    OuterArgs o{x, u, adapter, da, x_stride, tokens, cols, rank, cols, 1};
-    hipLaunchKernelGGL(lora_outer_kernel<BF16>,
-                       dim3((cols + kThreads - 1) / kThreads, rank, n_adapters), dim3(kThreads), 0,
-                       stream, o);
+
+    const PrepareArgs p{{u, v}, terms, scale, adapter, tokens, s.padded,
+                        {s.ju.splits, s.jv.splits}, rank, n_adapters};
+    hipLaunchKernelGGL(lora_prepare_kernel, dim3(s.padded / 32, 2), dim3(kThreads), 0, stream, p);
     if ((rc = launched())) return rc;
-    OuterArgs p{dy, v, adapter, db, dy_stride, tokens, rows, rank, 1, rank};
-    const dim3 grid((rows + kThreads - 1) / kThreads, rank, n_adapters);
-    if (dy_dtype == DF11_F32)
-        hipLaunchKernelGGL(lora_outer_kernel<F32>, grid, dim3(kThreads), 0, stream, p);
-    else
-        hipLaunchKernelGGL(lora_outer_kernel<BF16>, grid, dim3(kThreads), 0, stream, p);
+
+    const bool many = s.chunks > 1;
+    auto *present = reinterpret_cast<uint32_t *>(ws + s.present);
+    auto *pb = reinterpret_cast<float *>(ws + s.db), *pa = reinterpret_cast<float *>(ws + s.da);
+    const uint64_t fb = uint64_t{n_adapters} * rows * rank, fa = uint64_t{n_adapters} * cols * rank;
+    // dB takes v, the second pair of terms, and dA takes u, the first
+    const OuterArgs o{{{dy, terms + 2 * rank * s.padded, many ? pb : db, dy_stride, fb, rows,
+                        (rows + 255) / 256, false},
+                       {x, terms, many ? pa : da, x_stride, fa, cols, (cols + 255) / 256, true}},
+                      adapter, many ? present : nullptr, tokens, s.padded, s.per, rank, n_adapters};
+    rc = dy_dtype == DF11_F32 ? launch_outer<F32>(o, s.chunks, stream)
+                              : launch_outer<BF16>(o, s.chunks, stream);
+    if (rc || !many) return rc;
+    const JoinArgs j{{pb, pa}, {db, da}, present, {uint64_t{rows} * rank, uint64_t{cols} * rank},
+                     {fb, fa}, static_cast<uint32_t>(s.chunks), n_adapters};
+    const uint64_t wgs = (std::max(fa, fb) / 4 + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL(lora_join_kernel, dim3(std::min<uint64_t>(wgs, 8192), 2), dim3(kThreads), 0,
+                       stream, j);
     return launched();
 }
 
