@@ -6,14 +6,14 @@
 // A rank of 8 to 128 against thousands of columns: everything is bound by
 // reading x, base and dy and writing out and dx once; the products are small and
 // go to the matrix cores (v_mfma_f32_16x16x32_bf16) so that nothing else gets in
-// the way.  Four kernels:
+// the way.  The kernels:
 //   shrink  u and v: 16 tokens by all ranks, the columns over the waves of a
 //           workgroup and over workgroups (partial sums; `expand` and `prepare`
 //           add them in order), so that one token alone still has many loads
 //           under way;
+//   prepare u and v, their parts added, as the terms that the others multiply;
 //   expand  out and dx: 64 columns by 16 tokens a wave, through LDS so that base
-//           and out are read and written in whole rows;
-//   prepare u and v per rank, tokens side by side, for the gradients;
+//           and out are read and written in whole rows; few tokens one by one;
 //   outer   dA and dB: 64 columns a wave over a chunk of tokens, partial sums
 //           for several chunks, then `join`.
 // u and v are sums in 32 bits; where they meet the matrix cores they are split
@@ -39,6 +39,7 @@ constexpr uint32_t kThreads = 256;
 constexpr uint32_t kWaves = kThreads / 64;
 constexpr uint32_t kTile = 16;        // tokens of a matrix product
 constexpr uint32_t kFewTokens = 256;  // up to these, a workgroup an adapter of a tile
+constexpr uint32_t kFewValues = 1024; // tokens x rank up to which `expand` takes single tokens
 
 __device__ f32x4 mfma(const uint4 &a, const uint4 &b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
@@ -99,82 +100,116 @@ struct ShrinkArgs {
     uint32_t rank, n_adapters;
 };
 
+// 64 columns of 16 tokens and of the ranks: lane group q takes 16 of the columns,
+// in both operands, so that every load brings whole 128-byte lines.
 template <class T, uint32_t kRanks>
+struct Columns {
+    uint4 x[T::kVec == 4 ? 4 : 2], w[kRanks][2];
+    __device__ void load(const typename T::raw *row, const uint16_t *w0, uint32_t k, uint32_t len,
+                         uint32_t rank, uint32_t c, bool in) {
+#pragma unroll
+        for (uint32_t e = 0; e < sizeof(x) / 16; ++e)
+            x[e] = in ? *reinterpret_cast<const uint4 *>(row + k + T::kVec * e) : zero4();
+#pragma unroll
+        for (uint32_t r = 0; r < kRanks; ++r) {
+            const uint16_t *wr = w0 + static_cast<uint64_t>(min(16 * r + c, rank - 1)) * len + k;
+#pragma unroll
+            for (uint32_t e = 0; e < 2; ++e)
+                w[r][e] = in ? *reinterpret_cast<const uint4 *>(wr + 8 * e) : zero4();
+        }
+    }
+    __device__ void add(f32x4 *acc) const {
+#pragma unroll
+        for (uint32_t e = 0; e < 2; ++e) {
+            uint4 high, low;
+            if constexpr (T::kVec == 4) {
+                float v[8];
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) v[i] = F32::get(x[2 * e + i / 4], i % 4);
+                split8(v, &high, &low);
+            } else {
+                high = x[e];
+            }
+#pragma unroll
+            for (uint32_t r = 0; r < kRanks; ++r) {
+                acc[r] = mfma(high, w[r][e], acc[r]);
+                if constexpr (T::kVec == 4) acc[r] = mfma(low, w[r][e], acc[r]);
+            }
+        }
+    }
+};
+
+// kWide: each wave takes a tile of its own, over all the columns of the split (the
+// waves' loads of w meet in the L1 cache); else the waves share one tile's columns
+// and add their sums through LDS, so that a single tile has four times the loads
+// under way.
+template <class T, uint32_t kRanks, bool kWide>
 __device__ void shrink(const ShrinkArgs &g, const ShrinkJob &j, uint32_t split, float *red) {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, q = lane >> 4;
-    const uint64_t t0 = uint64_t{blockIdx.x} * kTile, t = t0 + c;
-    const int32_t id = adapter_of(g.adapter, t, g.tokens, g.n_adapters);
+    const uint64_t t0 = (uint64_t{blockIdx.x} * (kWide ? kWaves : 1) + (kWide ? wave : 0)) * kTile;
+    if (t0 >= g.tokens) return;  // a whole workgroup, or a wave that meets no barrier
+    const int32_t id = adapter_of(g.adapter, t0 + c, g.tokens, g.n_adapters);
     const auto *x =
-        static_cast<const typename T::raw *>(j.x) + std::min(t, g.tokens - 1) * j.stride;
+        static_cast<const typename T::raw *>(j.x) + std::min(t0 + c, g.tokens - 1) * j.stride;
     const uint32_t from = split * j.per, to = min(j.len, from + j.per);
+    constexpr uint32_t kStep = 64 * (kWide ? 1 : kWaves);
     each_adapter(id, 0, [&](int32_t a, uint32_t mine) {
         const uint16_t *w = j.w + static_cast<uint64_t>(a) * g.rank * j.len;
         f32x4 acc[kRanks];
 #pragma unroll
         for (uint32_t r = 0; r < kRanks; ++r) acc[r] = f32x4{0, 0, 0, 0};
-        // 64 columns a step: lane group q takes 16 of them, in both operands
-        for (uint32_t k0 = from + 64 * wave; k0 < to; k0 += 64 * kWaves) {
-            const uint32_t k = k0 + 16 * q;
-            const bool in = k < to;  // lengths are multiples of 16
-            uint4 xh[2], xl[2];
-            if constexpr (T::kVec == 4) {
-                float v[16];
-#pragma unroll
-                for (uint32_t e = 0; e < 4; ++e) {
-                    const uint4 p = in ? *reinterpret_cast<const uint4 *>(x + k + 4 * e) : zero4();
-                    for (uint32_t i = 0; i < 4; ++i) v[4 * e + i] = F32::get(p, i);
-                }
-                split8(v, &xh[0], &xl[0]);
-                split8(v + 8, &xh[1], &xl[1]);
-            } else {
-                xh[0] = in ? *reinterpret_cast<const uint4 *>(x + k) : zero4();
-                xh[1] = in ? *reinterpret_cast<const uint4 *>(x + k + 8) : zero4();
-            }
-#pragma unroll
-            for (uint32_t r = 0; r < kRanks; ++r) {
-                const uint16_t *wr = w + static_cast<uint64_t>(min(16 * r + c, g.rank - 1)) * j.len;
-#pragma unroll
-                for (uint32_t e = 0; e < 2; ++e) {
-                    const uint4 b = in ? *reinterpret_cast<const uint4 *>(wr + k + 8 * e) : zero4();
-                    acc[r] = mfma(xh[e], b, acc[r]);
-                    if constexpr (T::kVec == 4) acc[r] = mfma(xl[e], b, acc[r]);
-                }
-            }
+        // two steps' loads at a time; lengths are multiples of 16
+        for (uint32_t k0 = from + (kWide ? 0 : 64 * wave) + 16 * q; k0 - 16 * q < to; k0 += 2 * kStep) {
+            Columns<T, kRanks> one, two;
+            one.load(x, w, k0, j.len, g.rank, c, k0 < to);
+            two.load(x, w, k0 + kStep, j.len, g.rank, c, k0 + kStep < to);
+            one.add(acc);
+            two.add(acc);
         }
-        // the waves' sums through LDS: token 4q + e, rank 16r + c
-        __syncthreads();
+        // token 4q + e, rank 16r + c
+        if constexpr (kWide) {
 #pragma unroll
-        for (uint32_t r = 0; r < kRanks; ++r)
+            for (uint32_t r = 0; r < kRanks; ++r)
 #pragma unroll
-            for (uint32_t e = 0; e < 4; ++e)
-                red[(wave * kTile + 4 * q + e) * (16 * kRanks) + 16 * r + c] = acc[r][e];
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < kTile * 16 * kRanks; i += kThreads) {
-            const uint32_t row = i / (16 * kRanks), r = i % (16 * kRanks);
-            if (!(mine >> row & 1u) || r >= g.rank) continue;
-            float s = 0.0f;
-            for (uint32_t v = 0; v < kWaves; ++v) s += red[v * kTile * 16 * kRanks + i];
-            j.part[(split * g.tokens + t0 + row) * g.rank + r] = s;
+                for (uint32_t e = 0; e < 4; ++e)
+                    if (mine >> (4 * q + e) & 1u && 16 * r + c < g.rank)
+                        j.part[(split * g.tokens + t0 + 4 * q + e) * g.rank + 16 * r + c] = acc[r][e];
+        } else {
+            __syncthreads();
+#pragma unroll
+            for (uint32_t r = 0; r < kRanks; ++r)
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+                    red[(wave * kTile + 4 * q + e) * (16 * kRanks) + 16 * r + c] = acc[r][e];
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < kTile * 16 * kRanks; i += kThreads) {
+                const uint32_t row = i / (16 * kRanks), r = i % (16 * kRanks);
+                if (!(mine >> row & 1u) || r >= g.rank) continue;
+                float s = 0.0f;
+                for (uint32_t v = 0; v < kWaves; ++v) s += red[v * kTile * 16 * kRanks + i];
+                j.part[(split * g.tokens + t0 + row) * g.rank + r] = s;
+            }
         }
     });
 }
 
-template <class T, uint32_t kRanks>
+template <class T, uint32_t kRanks, bool kWide>
 __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs g) {
-    __shared__ float red[kWaves * kTile * 16 * kRanks];
+    __shared__ float red[kWide ? 1 : kWaves * kTile * 16 * kRanks];
     if (blockIdx.y < g.job[0].splits)
-        shrink<T, kRanks>(g, g.job[0], blockIdx.y, red);
+        shrink<T, kRanks, kWide>(g, g.job[0], blockIdx.y, red);
     else
-        shrink<BF16, kRanks>(g, g.job[1], blockIdx.y - g.job[0].splits, red);
+        shrink<BF16, kRanks, kWide>(g, g.job[1], blockIdx.y - g.job[0].splits, red);
 }
 
 // ---------------------------------------------------------------------- expand
-// out[t][c] = base[t][c] + scale[i] * sum_r low[t][r] w[i][c][r], low the sum of
-// the parts.
+// out[t][c] = base[t][c] + sum_r low[t][r] w[i][c][r], low the sum of the parts
+// times scale[i].
 struct ExpandArgs {
     const float *part;
-    const uint16_t *w;  // n_adapters x len x rank
     const float *scale;
+    const uint16_t *high, *low;  // low as two terms, tokens x rank each
+    const uint16_t *w;           // n_adapters x len x rank
     const int32_t *adapter;
     const void *base;
     void *out;
@@ -234,23 +269,14 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
                                                  : zero4();
                         }
                 }
-                const float scale = g.scale ? g.scale[a] : 1.0f;
                 uint4 high[kFrags], low[kFrags];
 #pragma unroll
                 for (uint32_t k = 0; k < kFrags; ++k) {
                     const uint32_t r = kSteps ? 32 * k + 8 * q : 8 * (q & 1u);
-                    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                    if (r < g.rank && (mine >> c & 1u))
-                        for (uint32_t p = 0; p < g.splits; ++p) {
-                            const auto *from = reinterpret_cast<const float4 *>(
-                                g.part + (p * g.tokens + t0 + c) * g.rank + r);
-                            const float4 x = from[0], y = from[1];
-                            v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-                            v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
-                        }
-#pragma unroll
-                    for (uint32_t e = 0; e < 8; ++e) v[e] *= scale;
-                    split8(v, &high[k], &low[k]);
+                    const bool in = r < g.rank && (mine >> c & 1u);
+                    const uint64_t at = (t0 + c) * g.rank + r;
+                    high[k] = in ? *reinterpret_cast<const uint4 *>(g.high + at) : zero4();
+                    low[k] = in ? *reinterpret_cast<const uint4 *>(g.low + at) : zero4();
                 }
                 if (!kSteps && q >= 2) high[0] = low[0];
                 // column 16f + 4q + e of token c
@@ -286,6 +312,40 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
     }
 }
 
+// The same for few tokens, a thread a column of one token: no tile to fill, no
+// terms to prepare, and no more than two loads after one another.
+template <class T>
+__global__ __launch_bounds__(kThreads) void lora_expand_few_kernel(ExpandArgs g) {
+    __shared__ float low[DF11_MAX_RANK];
+    const uint64_t t = blockIdx.y;
+    const int32_t a = adapter_of(g.adapter, t, g.tokens, g.n_adapters);
+    const uint32_t col = blockIdx.x * kThreads + threadIdx.x;
+    const bool in = col < g.len;
+    float v = 0.0f;
+    if (in && g.base) v = T::load(static_cast<const typename T::raw *>(g.base)[t * g.base_stride + col]);
+    if (a >= 0) {
+        if (threadIdx.x < g.rank) {
+            float s = 0.0f;
+#pragma unroll 4
+            for (uint32_t p = 0; p < g.splits; ++p) s += g.part[(p * g.tokens + t) * g.rank + threadIdx.x];
+            low[threadIdx.x] = s * (g.scale ? g.scale[a] : 1.0f);
+        }
+        __syncthreads();
+        if (in) {
+            const uint16_t *w = g.w + (static_cast<uint64_t>(a) * g.len + col) * g.rank;
+            float d = 0.0f;
+#pragma unroll 2
+            for (uint32_t r = 0; r < g.rank; r += 8) {
+                const uint4 q = *reinterpret_cast<const uint4 *>(w + r);
+#pragma unroll
+                for (uint32_t e = 0; e < 8; ++e) d = fmaf(low[r + e], BF16::get(q, e), d);
+            }
+            v += d;
+        }
+    }
+    if (in) static_cast<typename T::raw *>(g.out)[t * g.out_stride + col] = T::store(v);
+}
+
 // --------------------------------------------------------------- the gradients
 // to[i][r][c] = from[i][c][r], 64 c a workgroup; two matrices, along gridDim.y.
 struct TransposeJob {
@@ -298,62 +358,104 @@ struct TransposeArgs {
 };
 
 __global__ __launch_bounds__(kThreads) void lora_transpose_kernel(TransposeArgs g) {
-    constexpr uint32_t kSide = 64;
-    __shared__ uint16_t tile[kSide][kSide + 2];
+    constexpr uint32_t kSide = 64, kRow = kSide + 2;
+    __shared__ uint16_t tile[kSide * kRow];
     const TransposeJob j = g.job[blockIdx.y];
     const uint32_t across = (j.cols + kSide - 1) / kSide, down = (j.rows + kSide - 1) / kSide;
     if (blockIdx.x >= across * down) return;
     const uint32_t r0 = blockIdx.x / across * kSide, c0 = blockIdx.x % across * kSide;
     const uint64_t at = uint64_t{blockIdx.z} * j.rows * j.cols;
-    for (uint32_t i = threadIdx.x; i < kSide * kSide; i += kThreads) {
-        const uint32_t r = i / kSide, c = i % kSide;
+    // eight values a load and a store: both sides are multiples of 8
+    uint4 v[2];
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        const uint32_t r = threadIdx.x / 8 + 32 * i, c = threadIdx.x % 8 * 8;
         if (r0 + r < j.rows && c0 + c < j.cols)
-            tile[r][c] = j.from[at + static_cast<uint64_t>(r0 + r) * j.cols + c0 + c];
+            v[i] = *reinterpret_cast<const uint4 *>(j.from + at + static_cast<uint64_t>(r0 + r) * j.cols + c0 + c);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        const uint32_t r = threadIdx.x / 8 + 32 * i, c = threadIdx.x % 8 * 8;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e)
+            tile[(c + e) * kRow + r] = static_cast<uint16_t>(F32::word(v[i], e / 2) >> 16 * (e & 1u));
     }
     __syncthreads();
-    for (uint32_t i = threadIdx.x; i < kSide * kSide; i += kThreads) {
-        const uint32_t c = i / kSide, r = i % kSide;
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        const uint32_t c = threadIdx.x / 8 + 32 * i, r = threadIdx.x % 8 * 8;
+        uint32_t w[4];
+        for (uint32_t e = 0; e < 4; ++e)
+            w[e] = tile[c * kRow + r + 2 * e] | static_cast<uint32_t>(tile[c * kRow + r + 2 * e + 1]) << 16;
         if (r0 + r < j.rows && c0 + c < j.cols)
-            j.to[at + static_cast<uint64_t>(c0 + c) * j.rows + r0 + r] = tile[r][c];
+            *reinterpret_cast<uint4 *>(j.to + at + static_cast<uint64_t>(c0 + c) * j.rows + r0 + r) =
+                uint4{w[0], w[1], w[2], w[3]};
     }
 }
 
-// u and v as two BF16 terms each, a row of `padded` tokens per rank: terms[0..1]
-// of the first, terms[2..3] of the second.  0 for tokens without an adapter and
-// past the last one.
+// u and v, their parts added, times the scale, as two BF16 terms each: tokens x
+// rank for the expand kernel, and rank x `padded` tokens for the gradients (0 for
+// tokens without an adapter and past the last one).
+struct PrepareJob {
+    const float *part;
+    uint16_t *rows, *ranks;  // the high terms; the low ones behind them; either may be null
+    uint32_t splits;
+};
 struct PrepareArgs {
-    const float *part[2];
-    uint16_t *terms;
+    PrepareJob job[2];
     const float *scale;
     const int32_t *adapter;
     uint64_t tokens, padded;
-    uint32_t splits[2], rank, n_adapters;
+    uint32_t rank, n_adapters;
 };
 
+// Four values as their high and their low terms.
+__device__ void split4(const float4 &v, uint2 *high, uint2 *low) {
+    const float x[8] = {v.x, v.y, v.z, v.w, 0, 0, 0, 0};
+    uint4 h, l;
+    split8(x, &h, &l);
+    *high = uint2{h.x, h.y};
+    *low = uint2{l.x, l.y};
+}
+
 __global__ __launch_bounds__(kThreads) void lora_prepare_kernel(PrepareArgs g) {
-    __shared__ float tile[DF11_MAX_RANK][33];
-    const uint64_t t0 = uint64_t{blockIdx.x} * 32;
-    const uint32_t job = blockIdx.y;
-    for (uint32_t i = threadIdx.x; i < 32 * g.rank; i += kThreads) {
-        const uint32_t row = i / g.rank, r = i % g.rank;
+    constexpr uint32_t kTokens = 32;
+    __shared__ float tile[kTokens][DF11_MAX_RANK + 1];
+    const uint64_t t0 = uint64_t{blockIdx.x} * kTokens;
+    const PrepareJob j = g.job[blockIdx.y];
+    const uint32_t quads = g.rank / 4;
+    for (uint32_t i = threadIdx.x; i < kTokens * quads; i += kThreads) {
+        const uint32_t row = i / quads, r = i % quads * 4;
         const int32_t a = adapter_of(g.adapter, t0 + row, g.tokens, g.n_adapters);
-        float s = 0.0f;
+        float4 s{0, 0, 0, 0};
         if (a >= 0) {
-            for (uint32_t p = 0; p < g.splits[job]; ++p)
-                s += g.part[job][(p * g.tokens + t0 + row) * g.rank + r];
-            s *= g.scale ? g.scale[a] : 1.0f;
+            const float scale = g.scale ? g.scale[a] : 1.0f;
+#pragma unroll 4
+            for (uint32_t p = 0; p < j.splits; ++p) {
+                const float4 v = *reinterpret_cast<const float4 *>(
+                    j.part + (p * g.tokens + t0 + row) * g.rank + r);
+                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+            }
+            s.x *= scale, s.y *= scale, s.z *= scale, s.w *= scale;
         }
-        tile[r][row] = s;
+        if (j.rows && a >= -1) {
+            uint2 high, low;
+            split4(s, &high, &low);
+            uint16_t *to = j.rows + (t0 + row) * g.rank + r;
+            *reinterpret_cast<uint2 *>(to) = high;
+            *reinterpret_cast<uint2 *>(to + g.tokens * g.rank) = low;
+        }
+        tile[row][r] = s.x, tile[row][r + 1] = s.y, tile[row][r + 2] = s.z, tile[row][r + 3] = s.w;
     }
+    if (!j.ranks) return;
     __syncthreads();
-    uint16_t *high = g.terms + 2 * job * g.rank * g.padded, *low = high + g.rank * g.padded;
-    for (uint32_t i = threadIdx.x; i < 32 * g.rank; i += kThreads) {
-        const uint32_t r = i / 32, row = i % 32;
-        const float v = tile[r][row];
-        const uint16_t h = BF16::store(v);
-        high[r * g.padded + t0 + row] = h;
-        low[r * g.padded + t0 + row] =
-            BF16::store(fabsf(BF16::load(h)) < INFINITY ? v - BF16::load(h) : 0.0f);
+    for (uint32_t i = threadIdx.x; i < kTokens / 4 * g.rank; i += kThreads) {
+        const uint32_t r = i / (kTokens / 4), row = i % (kTokens / 4) * 4;
+        uint2 high, low;
+        split4(float4{tile[row][r], tile[row + 1][r], tile[row + 2][r], tile[row + 3][r]}, &high, &low);
+        uint16_t *to = j.ranks + r * g.padded + t0 + row;
+        *reinterpret_cast<uint2 *>(to) = high;
+        *reinterpret_cast<uint2 *>(to + g.rank * g.padded) = low;
     }
 }
 
@@ -403,18 +505,30 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
         __syncthreads();
         const uint32_t steps = (scan + 31) / 32;
         using Row = typename std::conditional<T::kVec == 4, uint4, uint2>::type;
-        for (uint32_t s = 0; s < steps; ++s) {
+        // the steps that hold tokens of this adapter, with the next one's rows under way
+        const auto from_step = [&](uint32_t s) {
+            while (s < steps && !__builtin_amdgcn_readfirstlane(member[s])) ++s;
+            return s;
+        };
+        const auto load = [&](uint32_t s, Row *row) {
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                const uint64_t t = std::min(s0 + 32 * s + 8 * q + i, g.tokens - 1);
+                row[i] = *reinterpret_cast<const Row *>(m + t * j.stride + col);
+            }
+        };
+        uint32_t s = from_step(0);
+        Row ahead[8];
+        if (s < steps) load(s, ahead);
+        while (s < steps) {
             const uint32_t bits = __builtin_amdgcn_readfirstlane(member[s]);
-            if (!bits) continue;
             some = true;
             const uint64_t t0 = s0 + 32 * s;
             const uint32_t ours = bits >> (8 * q) & 0xFFu;
             Row row[8];
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-                const uint64_t t = std::min(t0 + 8 * q + i, g.tokens - 1);
-                row[i] = *reinterpret_cast<const Row *>(m + t * j.stride + col);
-            }
+            for (uint32_t i = 0; i < 8; ++i) row[i] = ahead[i];
+            s = from_step(s + 1);
             uint4 wh[kRanks], wl[kRanks];
 #pragma unroll
             for (uint32_t r = 0; r < kRanks; ++r) {
@@ -422,6 +536,7 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
                 wh[r] = *reinterpret_cast<const uint4 *>(high + at);
                 wl[r] = *reinterpret_cast<const uint4 *>(low + at);
             }
+            if (s < steps) load(s, ahead);
             if (bits != ~0u) {
                 // other adapters' tokens: whatever they hold must not count
 #pragma unroll
@@ -568,10 +683,11 @@ int check_workspace(const void *ws, uint64_t have, uint64_t need) {
 }
 
 // Columns of a split and how many splits: about 1024 workgroups in all, each of
-// at least 512 columns (two steps of its four waves), at most 32 sums to add.
+// at least 512 columns, at most 32 sums to add.
 void split_columns(uint32_t len, uint64_t tokens, uint32_t n_adapters, ShrinkJob *j) {
-    const uint64_t tiles = (tokens + kTile - 1) / kTile;
-    const uint64_t wgs = tiles * (tokens <= kFewTokens ? std::min<uint64_t>({16, n_adapters, tokens}) : 1);
+    const uint64_t wgs = tokens <= kFewTokens
+                             ? (tokens + kTile - 1) / kTile * std::min<uint64_t>({16, n_adapters, tokens})
+                             : (tokens + kTile * kWaves - 1) / (kTile * kWaves);
     const uint32_t most = std::min(32u, std::max(1u, len / 512));
     const uint32_t want = static_cast<uint32_t>(std::min<uint64_t>(most, (1024 + wgs - 1) / wgs));
     j->len = len;
@@ -590,20 +706,36 @@ uint64_t chunk_tokens(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t ra
     return up((tokens + chunks - 1) / chunks, 32);
 }
 
-template <class T>
+template <class T, bool kWide>
 int launch_shrink(const ShrinkArgs &s, hipStream_t stream) {
-    const dim3 grid((s.tokens + kTile - 1) / kTile, s.job[0].splits + s.job[1].splits,
-                    s.tokens <= kFewTokens ? std::min<uint64_t>({16, s.n_adapters, s.tokens}) : 1);
+    const uint64_t tile = kTile * (kWide ? kWaves : 1);
+    const dim3 grid((s.tokens + tile - 1) / tile, s.job[0].splits + s.job[1].splits,
+                    kWide ? 1 : std::min<uint64_t>({16, s.n_adapters, s.tokens}));
     const dim3 block(kThreads);
     const uint32_t ranks = (s.rank + 15) / 16;
     if (ranks == 1)
-        hipLaunchKernelGGL((lora_shrink_kernel<T, 1>), grid, block, 0, stream, s);
+        hipLaunchKernelGGL((lora_shrink_kernel<T, 1, kWide>), grid, block, 0, stream, s);
     else if (ranks == 2)
-        hipLaunchKernelGGL((lora_shrink_kernel<T, 2>), grid, block, 0, stream, s);
+        hipLaunchKernelGGL((lora_shrink_kernel<T, 2, kWide>), grid, block, 0, stream, s);
     else if (ranks <= 4)
-        hipLaunchKernelGGL((lora_shrink_kernel<T, 4>), grid, block, 0, stream, s);
+        hipLaunchKernelGGL((lora_shrink_kernel<T, 4, kWide>), grid, block, 0, stream, s);
     else
-        hipLaunchKernelGGL((lora_shrink_kernel<T, 8>), grid, block, 0, stream, s);
+        hipLaunchKernelGGL((lora_shrink_kernel<T, 8, kWide>), grid, block, 0, stream, s);
+    return launched();
+}
+
+int launch_shrink(const ShrinkArgs &s, uint32_t dtype, hipStream_t stream) {
+    if (s.tokens <= kFewTokens)
+        return dtype == DF11_F32 ? launch_shrink<F32, false>(s, stream) : launch_shrink<BF16, false>(s, stream);
+    return dtype == DF11_F32 ? launch_shrink<F32, true>(s, stream) : launch_shrink<BF16, true>(s, stream);
+}
+
+int launch_expand_few(const ExpandArgs &e, uint32_t dtype, hipStream_t stream) {
+    const dim3 grid((e.len + kThreads - 1) / kThreads, e.tokens), block(kThreads);
+    if (dtype == DF11_F32)
+        hipLaunchKernelGGL(lora_expand_few_kernel<F32>, grid, block, 0, stream, e);
+    else
+        hipLaunchKernelGGL(lora_expand_few_kernel<BF16>, grid, block, 0, stream, e);
     return launched();
 }
 
@@ -649,7 +781,7 @@ int launch_outer(const OuterArgs &o, uint64_t chunks, hipStream_t stream) {
 
 // The backward pass's workspace, in bytes from its start.
 struct Space {
-    uint64_t bt, at, u, v, terms, present, db, da, bytes;
+    uint64_t bt, at, u, v, rows, terms, present, db, da, bytes;
     uint64_t padded, per, chunks;
     ShrinkJob ju, jv;
 };
@@ -670,6 +802,7 @@ Space space_of(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank, uin
     s.at = take(2ull * n_adapters * cols * rank);
     s.u = take(4ull * s.ju.splits * tokens * rank);
     s.v = take(4ull * s.jv.splits * tokens * rank);
+    s.rows = take(4ull * rank * tokens);
     s.terms = take(8ull * rank * s.padded);
     s.present = take(4ull * s.chunks * n_adapters);
     s.db = take(s.chunks > 1 ? 4ull * s.chunks * n_adapters * rows * rank : 0);
@@ -689,7 +822,8 @@ int df11_lora_workspace_bytes(uint64_t tokens, uint32_t cols, uint32_t rows, uin
     if (rc) return rc;
     ShrinkJob j{};
     if (tokens) split_columns(cols, tokens, n_adapters, &j);
-    *bytes = 4 * tokens * rank * j.splits;
+    // the parts, and their sum as two terms where there are more than few values
+    *bytes = 4 * tokens * rank * (j.splits + (tokens * rank > kFewValues ? 1 : 0));
     return DF11_OK;
 }
 
@@ -720,9 +854,16 @@ int df11_lora(const uint16_t *x, uint64_t x_stride, uint64_t tokens, uint32_t co
     s.tokens = tokens;
     s.rank = rank;
     s.n_adapters = n_adapters;
-    if ((rc = launch_shrink<BF16>(s, stream))) return rc;
-    const ExpandArgs e{s.job[0].part, b, scale, adapter, base, out, tokens, base_stride, out_stride,
-                       rows, rank, n_adapters, s.job[0].splits, 0};
+    if ((rc = launch_shrink(s, DF11_BF16, stream))) return rc;
+    const float *part = s.job[0].part;
+    auto *terms = reinterpret_cast<uint16_t *>(s.job[0].part + s.job[0].splits * tokens * rank);
+    const ExpandArgs e{part, scale, terms, terms + tokens * rank, b, adapter, base, out, tokens, base_stride,
+                       out_stride, rows, rank, n_adapters, s.job[0].splits, 0};
+    if (tokens * rank <= kFewValues) return launch_expand_few(e, dtype, stream);
+    const PrepareArgs p{{{part, terms, nullptr, s.job[0].splits}, {}}, scale, adapter, tokens, 0, rank,
+                        n_adapters};
+    hipLaunchKernelGGL(lora_prepare_kernel, dim3((tokens + 31) / 32), dim3(kThreads), 0, stream, p);
+    if ((rc = launched())) return rc;
     return launch_expand(e, dtype, stream);
 }
 
@@ -794,20 +935,21 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
     h.tokens = tokens;
     h.rank = rank;
     h.n_adapters = n_adapters;
-    rc = dy_dtype == DF11_F32 ? launch_shrink<F32>(h, stream) : launch_shrink<BF16>(h, stream);
-    if (rc) return rc;
+    if ((rc = launch_shrink(h, dy_dtype, stream))) return rc;
+
+    auto *by_row = reinterpret_cast<uint16_t *>(ws + s.rows);
+    const PrepareArgs p{{{u, dx ? by_row : nullptr, da ? terms : nullptr, s.ju.splits},
+                         {v, nullptr, terms + 2 * rank * s.padded, s.jv.splits}},
+                        scale, adapter, tokens, s.padded, rank, n_adapters};
+    hipLaunchKernelGGL(lora_prepare_kernel, dim3(s.padded / 32, da ? 2 : 1), dim3(kThreads), 0, stream, p);
+    if ((rc = launched())) return rc;
 
     if (dx) {
-        const ExpandArgs e{u, at, scale, adapter, dx_base, dx, tokens, dx_base_stride, dx_stride,
-                           cols, rank, n_adapters, s.ju.splits, 0};
+        const ExpandArgs e{u, scale, by_row, by_row + tokens * rank, at, adapter, dx_base, dx, tokens,
+                           dx_base_stride, dx_stride, cols, rank, n_adapters, s.ju.splits, 0};
         if ((rc = launch_expand(e, DF11_BF16, stream))) return rc;
     }
     if (!da) return DF11_OK;
-
-    const PrepareArgs p{{u, v}, terms, scale, adapter, tokens, s.padded,
-                        {s.ju.splits, s.jv.splits}, rank, n_adapters};
-    hipLaunchKernelGGL(lora_prepare_kernel, dim3(s.padded / 32, 2), dim3(kThreads), 0, stream, p);
-    if ((rc = launched())) return rc;
 
     const bool many = s.chunks > 1;
     auto *present = reinterpret_cast<uint32_t *>(ws + s.present);
