@@ -14,6 +14,7 @@ other, ``codec.DF11Error`` for what the library refuses.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import NamedTuple, Optional
 
 import torch
@@ -118,6 +119,14 @@ def _gpu(t, what):
     return t.device
 
 
+@functools.lru_cache(maxsize=1024)
+def _bytes(size, *sizes):
+    """What the library's size function says for these sizes."""
+    n = ctypes.c_uint64()
+    codec._check(getattr(lib(), size)(*sizes, ctypes.byref(n)), size)
+    return int(n.value)
+
+
 def _workspace(given, size, sizes, device, stream):
     """(tensor, bytes): the given workspace or one of the size the library asks for."""
     if given is not None:
@@ -125,24 +134,25 @@ def _workspace(given, size, sizes, device, stream):
         if not given.is_contiguous():
             raise ValueError("workspace must be contiguous")
         return given, given.numel() * given.element_size()
-    n = ctypes.c_uint64()
-    codec._check(getattr(lib(), size)(*sizes, ctypes.byref(n)), size)
-    if n.value == 0:
+    n = _bytes(size, *sizes)
+    if n == 0:
         return None, 0
-    ws = torch.empty(n.value, dtype=torch.uint8, device=device)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
     if stream is not None:
         # the kernels run on `stream`: the caching allocator must not hand this
         # memory out again before that stream has finished with it
         if not hasattr(stream, "cuda_stream"):
             stream = torch.cuda.ExternalStream(int(stream), device=device)
         ws.record_stream(stream)
-    return ws, n.value
+    return ws, n
 
 
-def _bytes(size, *sizes):
-    n = ctypes.c_uint64()
-    codec._check(getattr(lib(), size)(*sizes, ctypes.byref(n)), size)
-    return int(n.value)
+def _handle(stream, device):
+    """codec._handle without making a Stream object for torch's current stream,
+    which costs as much as a launch."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    return codec._handle(stream, device)
 
 
 # ----------------------------------------------------------- log probabilities
@@ -180,7 +190,7 @@ def logprobs(logits, tokens=None, top: int = 0, temperature: float = 1.0, out=No
     codec._check(lib().df11_logprobs(
         logits.data_ptr(), dt, rows, vocab, stride, _ptr(tokens), top, temperature,
         _ptr(out.logprob), _ptr(out.rank), _ptr(out.entropy), _ptr(out.top_logprob),
-        _ptr(out.top_index), _ptr(out.stats), _ptr(ws), ws_bytes, codec._handle(stream, device)),
+        _ptr(out.top_index), _ptr(out.stats), _ptr(ws), ws_bytes, _handle(stream, device)),
         "df11_logprobs")
     return out
 
@@ -204,7 +214,7 @@ def logprobs_backward(logits, tokens, stats, grad_logprob=None, grad_entropy=Non
     codec._check(lib().df11_logprobs_backward(
         logits.data_ptr(), DTYPES[logits.dtype], rows, vocab, stride, _ptr(tokens),
         stats.data_ptr(), _ptr(grad_logprob), _ptr(grad_entropy), temperature, out.data_ptr(),
-        grad_stride, codec._handle(stream, device)), "df11_logprobs_backward")
+        grad_stride, _handle(stream, device)), "df11_logprobs_backward")
     return out
 
 
@@ -252,7 +262,7 @@ def distill(logits, teacher_index, teacher_logprob, tail: bool = True, temperatu
         logits.data_ptr(), dt, rows, vocab, stride, teacher_index.data_ptr(),
         teacher_logprob.data_ptr(), top, bool(tail), temperature, _ptr(weight), loss.data_ptr(),
         stats.data_ptr(), _ptr(grad), grad_stride, _ptr(ws), ws_bytes,
-        codec._handle(stream, device)), "df11_distill")
+        _handle(stream, device)), "df11_distill")
     return Distill(loss, stats, grad)
 
 
@@ -273,7 +283,7 @@ def distill_backward(logits, teacher_index, teacher_logprob, stats, grad_loss=No
     codec._check(lib().df11_distill_backward(
         logits.data_ptr(), DTYPES[logits.dtype], rows, vocab, stride, teacher_index.data_ptr(),
         teacher_logprob.data_ptr(), top, bool(tail), temperature, stats.data_ptr(),
-        _ptr(grad_loss), out.data_ptr(), grad_stride, codec._handle(stream, device)),
+        _ptr(grad_loss), out.data_ptr(), grad_stride, _handle(stream, device)),
         "df11_distill_backward")
     return out
 
@@ -322,7 +332,7 @@ def lora(x, a, b, scale, adapter, base=None, out=None, workspace=None, stream=No
     codec._check(lib().df11_lora(
         x.data_ptr(), x_stride, *shapes, a.data_ptr(), b.data_ptr(), _ptr(scale),
         adapter.data_ptr(), _ptr(base), base_stride, out.data_ptr(), out_stride, DTYPES[out.dtype],
-        _ptr(ws), ws_bytes, codec._handle(stream, device)), "df11_lora")
+        _ptr(ws), ws_bytes, _handle(stream, device)), "df11_lora")
     return out
 
 
@@ -364,5 +374,5 @@ def lora_backward(x, a, b, scale, adapter, dy, dx_base=None, dx=None, da=None, d
         x.data_ptr(), x_stride, *shapes, a.data_ptr(), b.data_ptr(), _ptr(scale),
         adapter.data_ptr(), dy.data_ptr(), dy_stride, DTYPES[dy.dtype], _ptr(dx_base), dxb_stride,
         _ptr(dx), dx_stride, _ptr(da), _ptr(db), _ptr(ws), ws_bytes,
-        codec._handle(stream, device)), "df11_lora_backward")
+        _handle(stream, device)), "df11_lora_backward")
     return LoraGrads(dx, da, db)
