@@ -226,13 +226,15 @@ __device__ PartStat join_waves(const PartStat *w, float two_over_tau, bool xsum)
     return p;
 }
 
-// The parts' statistics of a row as one, by a wave.
-__device__ PartStat join_parts(const PartStat *stat, uint32_t parts, float two_over_tau, bool xsum,
-                               uint64_t *above) {
+constexpr PartStat kNoStat{kLowest, 0.0f, 0.0f, 0};
+
+// The parts' statistics of a row as one, by a wave.  `mine`: this lane's, of the
+// first 64.
+__device__ PartStat join_parts(PartStat mine, const PartStat *stat, uint32_t parts,
+                               float two_over_tau, bool xsum, uint64_t *above) {
     const uint32_t lane = threadIdx.x & 63u;
-    PartStat mine{kLowest, 0.0f, 0.0f, 0};
-    uint64_t count = 0;
-    for (uint32_t i = lane; i < parts; i += 64) {  // one round up to 524,288 values
+    uint64_t count = mine.above;
+    for (uint32_t i = lane + 64; i < parts; i += 64) {  // past 524,288 values
         const PartStat p = stat[i];
         const float M = fmaxf(mine.m, p.m);
         PartStat both{M, 0.0f, 0.0f, 0};
@@ -496,15 +498,12 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     uint32_t key[kSlots + 1], idx[kSlots + 1];
     const uint32_t slots = g.parts * g.room;
-    const auto load = [&](uint32_t from) {
+    // slots are `room` apart in part: which are filled, then what they hold
+    const auto filled = [&](uint32_t from, bool *some) {
         uint32_t q = (from + threadIdx.x) / g.room, r = (from + threadIdx.x) % g.room;
 #pragma unroll
         for (uint32_t e = 0; e < kSlots; ++e) {
-            const bool some = q < g.parts && r < g.count[first + q];
-            const uint2 v =
-                some ? g.candidate[first * g.room + from + kThreads * e + threadIdx.x] : uint2{0u, ~0u};
-            key[e] = v.x;
-            idx[e] = v.y;
+            some[e] = q < g.parts && r < g.count[first + min(q, g.parts - 1)];
             q += kThreads / g.room;
             r += kThreads % g.room;
             if (r >= g.room) {
@@ -513,14 +512,29 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
             }
         }
     };
-    if (g.top) load(0);
+    const auto load = [&](uint32_t from, const bool *some) {
+#pragma unroll
+        for (uint32_t e = 0; e < kSlots; ++e) {
+            const uint2 *at = g.candidate + first * g.room + from + kThreads * e + threadIdx.x;
+            const uint2 v = some[e] ? *at : uint2{0u, ~0u};
+            key[e] = v.x;
+            idx[e] = v.y;
+        }
+    };
+    // a row alone is all latency: what does not depend on another load goes first
+    const PartStat mine = lane < g.parts ? g.stat[first + lane] : kNoStat;
+    const int64_t token = g.tokens ? g.tokens[row] : -1;
+    const bool asked = token >= 0 && token < g.vocab;
+    if (g.top) {
+        bool some[kSlots];
+        filled(0, some);
+        load(0, some);
+    }
+    const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
+    const float zt = asked ? T::load(z[token]) : 0.0f;
     if (wave == 0) {
-        const int64_t token = g.tokens ? g.tokens[row] : -1;
-        const bool asked = token >= 0 && token < g.vocab;
-        const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
-        const float zt = asked ? T::load(z[token]) : 0.0f;
         uint64_t above;
-        const PartStat p = join_parts(g.stat + first, g.parts, g.tau.two_over, true, &above);
+        const PartStat p = join_parts(mine, g.stat + first, g.parts, g.tau.two_over, true, &above);
         const bool broken = !(p.s >= 0.0f) || p.s == INFINITY;
         const bool empty = p.s == 0.0f;
         const float nan = __builtin_nanf("");
@@ -559,8 +573,23 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
             for (uint32_t e = 0; e <= kSlots; ++e) c += f(key[e], idx[e]) ? 1u : 0u;
             return wg_sum(c, counts);
         };
-        n = count([&](uint32_t k, uint32_t) { return k >= cut; });
+        // how many of each wave's are kept, and of all
+        const auto keep = [&](uint32_t e) {
+            return key[e] > cut || (key[e] == cut && idx[e] <= last);
+        };
+        const auto kept_by_waves = [&] {
+            uint32_t c = 0;
+#pragma unroll
+            for (uint32_t e = 0; e <= kSlots; ++e) c += __popcll(__ballot(keep(e)));
+            if (lane == 0) counts[wave] = c;
+            __syncthreads();
+            uint32_t all = 0;
+            for (uint32_t w = 0; w < kWaves; ++w) all += counts[w];
+            return all;
+        };
+        n = kept_by_waves();
         if (n > kList) {  // equal ones, or a few lanes with all the large ones
+            __syncthreads();
             uint32_t hi = ~0u;
             while (cut < hi) {
                 const uint32_t mid = hi - (hi - cut) / 2;
@@ -585,20 +614,15 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
                     low = mid + 1;
                 }
             }
+            __syncthreads();
+            n = kept_by_waves();
         }
         // to the list: each wave behind those below it
-        uint32_t mine = 0;
-#pragma unroll
-        for (uint32_t e = 0; e <= kSlots; ++e)
-            mine += __popcll(__ballot(key[e] > cut || (key[e] == cut && idx[e] <= last)));
-        __syncthreads();
-        if (lane == 0) counts[wave] = mine;
-        __syncthreads();
         uint32_t at = 0;
         for (uint32_t w = 0; w < wave; ++w) at += counts[w];
 #pragma unroll
         for (uint32_t e = 0; e <= kSlots; ++e) {
-            const bool in = key[e] > cut || (key[e] == cut && idx[e] <= last);
+            const bool in = keep(e);
             const uint64_t all = __ballot(in);
             if (in) {
                 list_key[at + before(all)] = key[e];
@@ -628,7 +652,9 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
         kept = min(n, g.top);
         from += kThreads * kSlots;
         if (from >= slots) break;
-        load(from);
+        bool some[kSlots];
+        filled(from, some);
+        load(from, some);
     }
     const bool broken = row_s < 0.0f;
     for (uint32_t k = threadIdx.x; k < g.top; k += kThreads) {
@@ -788,6 +814,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     const uint64_t row = blockIdx.x;
     const uint32_t lane = threadIdx.x;
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
+    const PartStat first = lane < g.parts ? g.stat[row * g.parts + lane] : kNoStat;
     constexpr uint32_t kMost = DF11_MAX_TOP / 64;
     float lt[kMost], v[kMost];
     double p[kMost], mass = 0.0;
@@ -807,7 +834,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     bad = __any(bad);
     mass = wave_sum(mass);
     uint64_t none;
-    const PartStat st = join_parts(g.stat + row * g.parts, g.parts, g.tau.two_over, false, &none);
+    const PartStat st = join_parts(first, g.stat + row * g.parts, g.parts, g.tau.two_over, false, &none);
     // a row's few terms in 64 bits: the loss is a difference of larger ones
     const double ln_s = log(static_cast<double>(st.s));
     const double scale = g.tail ? 1.0 : 1.0 / mass, ln_mass = g.tail ? 0.0 : log(mass);

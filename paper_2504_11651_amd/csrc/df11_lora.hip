@@ -70,14 +70,15 @@ __device__ int32_t adapter_of(const int32_t *adapter, uint64_t t, uint64_t token
 }
 
 // Calls f(adapter, its tokens' bits) for the distinct adapters from `least` on of
-// a tile; `id` is that of token lane % 16.  Workgroup z of gridDim.z takes every
+// the first kTokens lanes' `id`.  Workgroup z of gridDim.z takes every
 // gridDim.z-th of them.
-template <class F>
+template <uint32_t kTokens, class F>
 __device__ void each_adapter(int32_t id, int32_t least, F f) {
-    uint32_t left = static_cast<uint32_t>(__ballot(id >= least)) & 0xFFFFu, turn = 0;
+    constexpr uint32_t kAll = kTokens == 32 ? ~0u : (1u << kTokens) - 1;
+    uint32_t left = static_cast<uint32_t>(__ballot(id >= least)) & kAll, turn = 0;
     while (left) {
         const int32_t a = __builtin_amdgcn_readlane(id, __builtin_ctz(left));
-        const uint32_t mine = static_cast<uint32_t>(__ballot(id == a)) & 0xFFFFu;
+        const uint32_t mine = static_cast<uint32_t>(__ballot(id == a)) & kAll;
         left &= ~mine;
         if (turn++ % gridDim.z == blockIdx.z) f(a, mine);
     }
@@ -100,16 +101,18 @@ struct ShrinkArgs {
     uint32_t rank, n_adapters;
 };
 
-// 64 columns of 16 tokens and of the ranks: lane group q takes 16 of the columns,
-// in both operands, so that every load brings whole 128-byte lines.
-template <class T, uint32_t kRanks>
+// 64 columns of kSub tiles of 16 tokens and of the ranks: lane group q takes 16 of
+// the columns, in both operands, so that every load brings whole 128-byte lines.
+template <class T, uint32_t kRanks, uint32_t kSub>
 struct Columns {
-    uint4 x[T::kVec == 4 ? 4 : 2], w[kRanks][2];
-    __device__ void load(const typename T::raw *row, const uint16_t *w0, uint32_t k, uint32_t len,
+    uint4 x[kSub][T::kVec == 4 ? 4 : 2], w[kRanks][2];
+    __device__ void load(const typename T::raw *const *row, const uint16_t *w0, uint32_t k, uint32_t len,
                          uint32_t rank, uint32_t c, bool in) {
 #pragma unroll
-        for (uint32_t e = 0; e < sizeof(x) / 16; ++e)
-            x[e] = in ? *reinterpret_cast<const uint4 *>(row + k + T::kVec * e) : zero4();
+        for (uint32_t s = 0; s < kSub; ++s)
+#pragma unroll
+            for (uint32_t e = 0; e < sizeof(x[0]) / 16; ++e)
+                x[s][e] = in ? *reinterpret_cast<const uint4 *>(row[s] + k + T::kVec * e) : zero4();
 #pragma unroll
         for (uint32_t r = 0; r < kRanks; ++r) {
             const uint16_t *wr = w0 + static_cast<uint64_t>(min(16 * r + c, rank - 1)) * len + k;
@@ -118,69 +121,86 @@ struct Columns {
                 w[r][e] = in ? *reinterpret_cast<const uint4 *>(wr + 8 * e) : zero4();
         }
     }
-    __device__ void add(f32x4 *acc) const {
+    __device__ void add(f32x4 (*acc)[kRanks]) const {
 #pragma unroll
-        for (uint32_t e = 0; e < 2; ++e) {
-            uint4 high, low;
-            if constexpr (T::kVec == 4) {
-                float v[8];
+        for (uint32_t s = 0; s < kSub; ++s)
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i) v[i] = F32::get(x[2 * e + i / 4], i % 4);
-                split8(v, &high, &low);
-            } else {
-                high = x[e];
+            for (uint32_t e = 0; e < 2; ++e) {
+                uint4 high, low;
+                if constexpr (T::kVec == 4) {
+                    float v[8];
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) v[i] = F32::get(x[s][2 * e + i / 4], i % 4);
+                    split8(v, &high, &low);
+                } else {
+                    high = x[s][e];
+                }
+#pragma unroll
+                for (uint32_t r = 0; r < kRanks; ++r) {
+                    acc[s][r] = mfma(high, w[r][e], acc[s][r]);
+                    if constexpr (T::kVec == 4) acc[s][r] = mfma(low, w[r][e], acc[s][r]);
+                }
             }
-#pragma unroll
-            for (uint32_t r = 0; r < kRanks; ++r) {
-                acc[r] = mfma(high, w[r][e], acc[r]);
-                if constexpr (T::kVec == 4) acc[r] = mfma(low, w[r][e], acc[r]);
-            }
-        }
     }
 };
 
-// kWide: each wave takes a tile of its own, over all the columns of the split (the
-// waves' loads of w meet in the L1 cache); else the waves share one tile's columns
-// and add their sums through LDS, so that a single tile has four times the loads
-// under way.
+// Tiles of 16 tokens that a wave of the wide kernel takes.
+constexpr uint32_t kWideTiles = 2, kWideTokens = kTile * kWideTiles * kWaves;
+
+// kWide: each wave takes tiles of its own, over all the columns of the split (the
+// waves' loads of w meet in the L1 cache, and each serves two tiles); else the
+// waves share one tile's columns and add their sums through LDS, so that a single
+// tile has four times the loads under way.
 template <class T, uint32_t kRanks, bool kWide>
 __device__ void shrink(const ShrinkArgs &g, const ShrinkJob &j, uint32_t split, float *red) {
+    constexpr uint32_t kSub = kWide ? kWideTiles : 1, kTokens = kSub * kTile;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, q = lane >> 4;
-    const uint64_t t0 = (uint64_t{blockIdx.x} * (kWide ? kWaves : 1) + (kWide ? wave : 0)) * kTile;
+    const uint64_t t0 = (uint64_t{blockIdx.x} * (kWide ? kWaves : 1) + (kWide ? wave : 0)) * kTokens;
     if (t0 >= g.tokens) return;  // a whole workgroup, or a wave that meets no barrier
-    const int32_t id = adapter_of(g.adapter, t0 + c, g.tokens, g.n_adapters);
-    const auto *x =
-        static_cast<const typename T::raw *>(j.x) + std::min(t0 + c, g.tokens - 1) * j.stride;
+    const int32_t id = adapter_of(g.adapter, t0 + (lane & (kTokens - 1)), g.tokens, g.n_adapters);
+    const typename T::raw *x[kSub];
+#pragma unroll
+    for (uint32_t s = 0; s < kSub; ++s)
+        x[s] = static_cast<const typename T::raw *>(j.x) +
+               std::min(t0 + kTile * s + c, g.tokens - 1) * j.stride;
     const uint32_t from = split * j.per, to = min(j.len, from + j.per);
     constexpr uint32_t kStep = 64 * (kWide ? 1 : kWaves);
-    each_adapter(id, 0, [&](int32_t a, uint32_t mine) {
+    each_adapter<kTokens>(id, 0, [&](int32_t a, uint32_t mine) {
         const uint16_t *w = j.w + static_cast<uint64_t>(a) * g.rank * j.len;
-        f32x4 acc[kRanks];
+        f32x4 acc[kSub][kRanks];
 #pragma unroll
-        for (uint32_t r = 0; r < kRanks; ++r) acc[r] = f32x4{0, 0, 0, 0};
-        // two steps' loads at a time; lengths are multiples of 16
-        for (uint32_t k0 = from + (kWide ? 0 : 64 * wave) + 16 * q; k0 - 16 * q < to; k0 += 2 * kStep) {
-            Columns<T, kRanks> one, two;
-            one.load(x, w, k0, j.len, g.rank, c, k0 < to);
-            two.load(x, w, k0 + kStep, j.len, g.rank, c, k0 + kStep < to);
+        for (uint32_t s = 0; s < kSub; ++s)
+#pragma unroll
+            for (uint32_t r = 0; r < kRanks; ++r) acc[s][r] = f32x4{0, 0, 0, 0};
+        // the next step's loads are under way; lengths are multiples of 16
+        Columns<T, kRanks, kSub> one, two;
+        uint32_t k = from + (kWide ? 0 : 64 * wave) + 16 * q;
+        one.load(x, w, k, j.len, g.rank, c, k < to);
+        for (; k - 16 * q < to; k += 2 * kStep) {
+            two.load(x, w, k + kStep, j.len, g.rank, c, k + kStep < to);
             one.add(acc);
+            one.load(x, w, k + 2 * kStep, j.len, g.rank, c, k + 2 * kStep < to);
             two.add(acc);
         }
-        // token 4q + e, rank 16r + c
+        // token 4q + e of a tile, rank 16r + c
         if constexpr (kWide) {
 #pragma unroll
-            for (uint32_t r = 0; r < kRanks; ++r)
+            for (uint32_t s = 0; s < kSub; ++s)
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e)
-                    if (mine >> (4 * q + e) & 1u && 16 * r + c < g.rank)
-                        j.part[(split * g.tokens + t0 + 4 * q + e) * g.rank + 16 * r + c] = acc[r][e];
+                for (uint32_t r = 0; r < kRanks; ++r)
+#pragma unroll
+                    for (uint32_t e = 0; e < 4; ++e) {
+                        const uint32_t row = kTile * s + 4 * q + e;
+                        if (mine >> row & 1u && 16 * r + c < g.rank)
+                            j.part[(split * g.tokens + t0 + row) * g.rank + 16 * r + c] = acc[s][r][e];
+                    }
         } else {
             __syncthreads();
 #pragma unroll
             for (uint32_t r = 0; r < kRanks; ++r)
 #pragma unroll
                 for (uint32_t e = 0; e < 4; ++e)
-                    red[(wave * kTile + 4 * q + e) * (16 * kRanks) + 16 * r + c] = acc[r][e];
+                    red[(wave * kTile + 4 * q + e) * (16 * kRanks) + 16 * r + c] = acc[0][r][e];
             __syncthreads();
             for (uint32_t i = threadIdx.x; i < kTile * 16 * kRanks; i += kThreads) {
                 const uint32_t row = i / (16 * kRanks), r = i % (16 * kRanks);
@@ -245,7 +265,7 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
         const uint64_t t0 = (group * kTiles + s) * kTile;
         if (t0 >= g.tokens) return;
         const int32_t id = adapter_of(g.adapter, t0 + c, g.tokens, g.n_adapters);
-        each_adapter(id, -1, [&](int32_t a, uint32_t mine) {
+        each_adapter<kTile>(id, -1, [&](int32_t a, uint32_t mine) {
             uint4 held[kTrips];
 #pragma unroll
             for (uint32_t i = 0; i < kTrips; ++i) {
@@ -478,16 +498,21 @@ struct OuterArgs {
 
 constexpr uint32_t kScan = 4096;  // tokens whose adapters are looked at together
 
+// The terms of 128 tokens in LDS, a row per rank: 8 values more keep the 16 lanes
+// that read 16 bytes of 16 rows apart.
+constexpr uint32_t kPiece = 128, kPieceRow = kPiece + 8;
+
 template <class T, uint32_t kRanks>
-__device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uint32_t *member) {
+__device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uint32_t *member,
+                      uint16_t *terms) {
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, q = lane >> 4;
     const int32_t a = blockIdx.z;
     const uint32_t c0 = (block * kWaves + wave) * 64;
     // lane group q takes tokens 8q..8q+7 of a step, lane c of it columns 4c..4c+3
     const uint32_t col = min(c0 + 4 * c, j.len - 4);
     const auto *m = static_cast<const typename T::raw *>(j.m);
-    const uint16_t *high = j.terms, *low = high + g.rank * g.padded;
     const uint64_t from = uint64_t{blockIdx.y} * g.per, to = std::min(g.tokens, from + g.per);
+    uint16_t *const wh = terms, *const wl = terms + 16 * kRanks * kPieceRow;
     f32x4 acc[4][kRanks];
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e)
@@ -517,51 +542,53 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
                 row[i] = *reinterpret_cast<const Row *>(m + t * j.stride + col);
             }
         };
-        uint32_t s = from_step(0);
+        uint32_t s = from_step(0), piece = ~0u;
         Row ahead[8];
         if (s < steps) load(s, ahead);
         while (s < steps) {
-            const uint32_t bits = __builtin_amdgcn_readfirstlane(member[s]);
+            const uint32_t bits = __builtin_amdgcn_readfirstlane(member[s]), now = s;
             some = true;
-            const uint64_t t0 = s0 + 32 * s;
             const uint32_t ours = bits >> (8 * q) & 0xFFu;
+            // the terms of the step's piece: every wave comes here for the same steps
+            if (now / (kPiece / 32) != piece) {
+                piece = now / (kPiece / 32);
+                const uint64_t p0 = s0 + piece * kPiece;
+                __syncthreads();
+                constexpr uint32_t kEach = kPiece / 8;  // loads of a row
+                for (uint32_t i = threadIdx.x; i < 2 * g.rank * kEach; i += kThreads) {
+                    const uint32_t r = i / kEach, at = i % kEach * 8;  // r: high terms, then low ones
+                    const uint32_t rank = r < g.rank ? r : r - g.rank;
+                    if (p0 + at < g.padded)
+                        *reinterpret_cast<uint4 *>((r < g.rank ? wh : wl) + rank * kPieceRow + at) =
+                            *reinterpret_cast<const uint4 *>(j.terms + r * g.padded + p0 + at);
+                }
+                __syncthreads();
+            }
             Row row[8];
 #pragma unroll
             for (uint32_t i = 0; i < 8; ++i) row[i] = ahead[i];
-            s = from_step(s + 1);
-            uint4 wh[kRanks], wl[kRanks];
-#pragma unroll
-            for (uint32_t r = 0; r < kRanks; ++r) {
-                const uint64_t at = min(16 * r + c, g.rank - 1) * g.padded + t0 + 8 * q;
-                wh[r] = *reinterpret_cast<const uint4 *>(high + at);
-                wl[r] = *reinterpret_cast<const uint4 *>(low + at);
-            }
+            s = from_step(now + 1);
             if (s < steps) load(s, ahead);
+            uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
             if (bits != ~0u) {
                 // other adapters' tokens: whatever they hold must not count
 #pragma unroll
                 for (uint32_t i = 0; i < 8; ++i)
                     if (!(ours >> i & 1u)) row[i] = Row{};
-                uint32_t keep[4];
 #pragma unroll
                 for (uint32_t i = 0; i < 4; ++i)
                     keep[i] = (ours >> (2 * i) & 1u ? 0xFFFFu : 0u) |
                               (ours >> (2 * i + 1) & 1u ? 0xFFFF0000u : 0u);
-#pragma unroll
-                for (uint32_t r = 0; r < kRanks; ++r) {
-                    wh[r].x &= keep[0], wh[r].y &= keep[1], wh[r].z &= keep[2], wh[r].w &= keep[3];
-                    wl[r].x &= keep[0], wl[r].y &= keep[1], wl[r].z &= keep[2], wl[r].w &= keep[3];
-                }
             }
+            // column 4c + e of the lane's eight tokens
+            uint4 mh[4], ml[4];
 #pragma unroll
             for (uint32_t e = 0; e < 4; ++e) {
-                // column 4c + e of the lane's eight tokens
-                uint4 mh, ml = zero4();
                 if constexpr (T::kVec == 4) {
                     float v[8];
 #pragma unroll
                     for (uint32_t i = 0; i < 8; ++i) v[i] = F32::get(row[i], e);
-                    split8(v, &mh, &ml);
+                    split8(v, &mh[e], &ml[e]);
                 } else {
                     uint32_t p[4];
                     const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
@@ -571,19 +598,26 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
                         const uint32_t y = e < 2 ? row[2 * i + 1].x : row[2 * i + 1].y;
                         p[i] = __builtin_amdgcn_perm(y, x, pick);
                     }
-                    mh = uint4{p[0], p[1], p[2], p[3]};
+                    mh[e] = uint4{p[0], p[1], p[2], p[3]};
                 }
+            }
 #pragma unroll
-                for (uint32_t r = 0; r < kRanks; ++r) {
-                    acc[e][r] = mfma(mh, wh[r], acc[e][r]);
-                    acc[e][r] = mfma(mh, wl[r], acc[e][r]);
-                    if constexpr (T::kVec == 4) acc[e][r] = mfma(ml, wh[r], acc[e][r]);
+            for (uint32_t r = 0; r < kRanks; ++r) {
+                const uint32_t at = min(16 * r + c, g.rank - 1) * kPieceRow + now % (kPiece / 32) * 32 + 8 * q;
+                uint4 h = *reinterpret_cast<const uint4 *>(wh + at), l = *reinterpret_cast<const uint4 *>(wl + at);
+                h.x &= keep[0], h.y &= keep[1], h.z &= keep[2], h.w &= keep[3];
+                l.x &= keep[0], l.y &= keep[1], l.z &= keep[2], l.w &= keep[3];
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) {
+                    acc[e][r] = mfma(mh[e], h, acc[e][r]);
+                    acc[e][r] = mfma(mh[e], l, acc[e][r]);
+                    if constexpr (T::kVec == 4) acc[e][r] = mfma(ml[e], h, acc[e][r]);
                 }
             }
         }
     }
     if (g.present) {
-        if (block == 0 && threadIdx.x == 0 && blockIdx.x == 0)
+        if (blockIdx.x == 0 && threadIdx.x == 0)
             g.present[blockIdx.y * g.n_adapters + a] = some ? 1u : 0u;
         if (!some) return;
     }
@@ -612,10 +646,11 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
 template <class T, uint32_t kRanks>
 __global__ __launch_bounds__(kThreads) void lora_outer_kernel(OuterArgs g) {
     __shared__ uint32_t member[kScan / 32];
+    __shared__ __align__(16) uint16_t terms[2 * 16 * kRanks * kPieceRow];
     if (blockIdx.x < g.job[0].blocks)
-        outer<T, kRanks>(g, g.job[0], blockIdx.x, member);
+        outer<T, kRanks>(g, g.job[0], blockIdx.x, member, terms);
     else
-        outer<BF16, kRanks>(g, g.job[1], blockIdx.x - g.job[0].blocks, member);
+        outer<BF16, kRanks>(g, g.job[1], blockIdx.x - g.job[0].blocks, member, terms);
 }
 
 // d = the chunks' sums in order; 0 for an adapter without tokens.
@@ -687,7 +722,7 @@ int check_workspace(const void *ws, uint64_t have, uint64_t need) {
 void split_columns(uint32_t len, uint64_t tokens, uint32_t n_adapters, ShrinkJob *j) {
     const uint64_t wgs = tokens <= kFewTokens
                              ? (tokens + kTile - 1) / kTile * std::min<uint64_t>({16, n_adapters, tokens})
-                             : (tokens + kTile * kWaves - 1) / (kTile * kWaves);
+                             : (tokens + kWideTokens - 1) / kWideTokens;
     const uint32_t most = std::min(32u, std::max(1u, len / 512));
     const uint32_t want = static_cast<uint32_t>(std::min<uint64_t>(most, (1024 + wgs - 1) / wgs));
     j->len = len;
@@ -708,7 +743,7 @@ uint64_t chunk_tokens(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t ra
 
 template <class T, bool kWide>
 int launch_shrink(const ShrinkArgs &s, hipStream_t stream) {
-    const uint64_t tile = kTile * (kWide ? kWaves : 1);
+    const uint64_t tile = kWide ? kWideTokens : kTile;
     const dim3 grid((s.tokens + tile - 1) / tile, s.job[0].splits + s.job[1].splits,
                     kWide ? 1 : std::min<uint64_t>({16, s.n_adapters, s.tokens}));
     const dim3 block(kThreads);
