@@ -74,11 +74,12 @@ __device__ int32_t adapter_of(const int32_t *adapter, uint64_t t, uint64_t token
 // gridDim.z-th of them.
 template <uint32_t kTokens, class F>
 __device__ void each_adapter(int32_t id, int32_t least, F f) {
-    constexpr uint32_t kAll = kTokens == 32 ? ~0u : (1u << kTokens) - 1;
-    uint32_t left = static_cast<uint32_t>(__ballot(id >= least)) & kAll, turn = 0;
+    constexpr uint64_t kAll = kTokens == 64 ? ~0ull : (1ull << kTokens) - 1;
+    uint64_t left = __ballot(id >= least) & kAll;
+    uint32_t turn = 0;
     while (left) {
-        const int32_t a = __builtin_amdgcn_readlane(id, __builtin_ctz(left));
-        const uint32_t mine = static_cast<uint32_t>(__ballot(id == a)) & kAll;
+        const int32_t a = __builtin_amdgcn_readlane(id, __builtin_ctzll(left));
+        const uint64_t mine = __ballot(id == a) & kAll;
         left &= ~mine;
         if (turn++ % gridDim.z == blockIdx.z) f(a, mine);
     }
@@ -144,14 +145,22 @@ struct Columns {
     }
 };
 
-// Tiles of 16 tokens that a wave of the wide kernel takes.
-constexpr uint32_t kWideTiles = 2, kWideTokens = kTile * kWideTiles * kWaves;
+// Tiles of 16 tokens that a wave of the wide kernel takes.  From 32 ranks the loads
+// of w are more than those of x, and tiles share them (8192 tokens, rank 64: one
+// tile 92 us, two 72, four 61), with an fp32 x at any rank (1024 tokens x 128,256,
+// rank 16: one 124 us, two 110); else more tiles only lower the number of waves
+// (6001 tokens, rank 16: one 18.1 us, two 21.6).  Above 64 ranks four do not fit the
+// registers.
+constexpr uint32_t wide_tiles(uint32_t rank, bool f32) { return !f32 && rank > 32 && rank <= 64 ? 4 : rank > 16 || f32 ? 2 : 1; }
+constexpr uint32_t wide_tokens(uint32_t rank, bool f32) {
+    return kTile * kWaves * wide_tiles(rank, f32);
+}
 
 // kWide: each wave takes tiles of its own, over all the columns of the split (the
 // waves' loads of w meet in the L1 cache, and each serves two tiles); else the
 // waves share one tile's columns and add their sums through LDS, so that a single
 // tile has four times the loads under way.
-template <class T, uint32_t kRanks, bool kWide>
+template <class T, uint32_t kRanks, bool kWide, uint32_t kWideTiles>
 __device__ void shrink(const ShrinkArgs &g, const ShrinkJob &j, uint32_t split, float *red) {
     constexpr uint32_t kSub = kWide ? kWideTiles : 1, kTokens = kSub * kTile;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, q = lane >> 4;
@@ -165,7 +174,7 @@ __device__ void shrink(const ShrinkArgs &g, const ShrinkJob &j, uint32_t split, 
                std::min(t0 + kTile * s + c, g.tokens - 1) * j.stride;
     const uint32_t from = split * j.per, to = min(j.len, from + j.per);
     constexpr uint32_t kStep = 64 * (kWide ? 1 : kWaves);
-    each_adapter<kTokens>(id, 0, [&](int32_t a, uint32_t mine) {
+    each_adapter<kTokens>(id, 0, [&](int32_t a, uint64_t mine) {
         const uint16_t *w = j.w + static_cast<uint64_t>(a) * g.rank * j.len;
         f32x4 acc[kSub][kRanks];
 #pragma unroll
@@ -216,10 +225,11 @@ __device__ void shrink(const ShrinkArgs &g, const ShrinkJob &j, uint32_t split, 
 template <class T, uint32_t kRanks, bool kWide>
 __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs g) {
     __shared__ float red[kWide ? 1 : kWaves * kTile * 16 * kRanks];
+    constexpr uint32_t kTiles = wide_tiles(16 * kRanks, T::kVec == 4);
     if (blockIdx.y < g.job[0].splits)
-        shrink<T, kRanks, kWide>(g, g.job[0], blockIdx.y, red);
+        shrink<T, kRanks, kWide, kTiles>(g, g.job[0], blockIdx.y, red);
     else
-        shrink<BF16, kRanks, kWide>(g, g.job[1], blockIdx.y - g.job[0].splits, red);
+        shrink<BF16, kRanks, kWide, kTiles>(g, g.job[1], blockIdx.y - g.job[0].splits, red);
 }
 
 // ---------------------------------------------------------------------- expand
@@ -265,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
         const uint64_t t0 = (group * kTiles + s) * kTile;
         if (t0 >= g.tokens) return;
         const int32_t id = adapter_of(g.adapter, t0 + c, g.tokens, g.n_adapters);
-        each_adapter<kTile>(id, -1, [&](int32_t a, uint32_t mine) {
+        each_adapter<kTile>(id, -1, [&](int32_t a, uint64_t mine) {
             uint4 held[kTrips];
 #pragma unroll
             for (uint32_t i = 0; i < kTrips; ++i) {
@@ -644,7 +654,7 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
 }
 
 template <class T, uint32_t kRanks>
-__global__ __launch_bounds__(kThreads) void lora_outer_kernel(OuterArgs g) {
+__global__ __launch_bounds__(kThreads, kRanks <= 2 ? 3 : 2) void lora_outer_kernel(OuterArgs g) {
     __shared__ uint32_t member[kScan / 32];
     __shared__ __align__(16) uint16_t terms[2 * 16 * kRanks * kPieceRow];
     if (blockIdx.x < g.job[0].blocks)
@@ -719,10 +729,11 @@ int check_workspace(const void *ws, uint64_t have, uint64_t need) {
 
 // Columns of a split and how many splits: about 1024 workgroups in all, each of
 // at least 512 columns, at most 32 sums to add.
-void split_columns(uint32_t len, uint64_t tokens, uint32_t n_adapters, ShrinkJob *j) {
+void split_columns(uint32_t len, uint64_t tokens, uint32_t rank, uint32_t n_adapters,
+                   ShrinkJob *j) {
     const uint64_t wgs = tokens <= kFewTokens
                              ? (tokens + kTile - 1) / kTile * std::min<uint64_t>({16, n_adapters, tokens})
-                             : (tokens + kWideTokens - 1) / kWideTokens;
+                             : (tokens + wide_tokens(rank, false) - 1) / wide_tokens(rank, false);
     const uint32_t most = std::min(32u, std::max(1u, len / 512));
     const uint32_t want = static_cast<uint32_t>(std::min<uint64_t>(most, (1024 + wgs - 1) / wgs));
     j->len = len;
@@ -743,7 +754,7 @@ uint64_t chunk_tokens(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t ra
 
 template <class T, bool kWide>
 int launch_shrink(const ShrinkArgs &s, hipStream_t stream) {
-    const uint64_t tile = kWide ? kWideTokens : kTile;
+    const uint64_t tile = kWide ? wide_tokens(s.rank, T::kVec == 4) : kTile;
     const dim3 grid((s.tokens + tile - 1) / tile, s.job[0].splits + s.job[1].splits,
                     kWide ? 1 : std::min<uint64_t>({16, s.n_adapters, s.tokens}));
     const dim3 block(kThreads);
@@ -823,8 +834,8 @@ struct Space {
 Space space_of(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank, uint32_t n_adapters) {
     Space s{};
     s.padded = up(tokens, 32);
-    split_columns(rows, std::max<uint64_t>(tokens, 1), n_adapters, &s.ju);
-    split_columns(cols, std::max<uint64_t>(tokens, 1), n_adapters, &s.jv);
+    split_columns(rows, std::max<uint64_t>(tokens, 1), rank, n_adapters, &s.ju);
+    split_columns(cols, std::max<uint64_t>(tokens, 1), rank, n_adapters, &s.jv);
     s.per = std::max<uint64_t>(32, chunk_tokens(tokens, cols, rows, rank, n_adapters));
     s.chunks = std::max<uint64_t>(1, (tokens + s.per - 1) / s.per);
     uint64_t at = 0;
@@ -856,7 +867,7 @@ int df11_lora_workspace_bytes(uint64_t tokens, uint32_t cols, uint32_t rows, uin
     const int rc = check_shapes(tokens, cols, rows, rank, n_adapters);
     if (rc) return rc;
     ShrinkJob j{};
-    if (tokens) split_columns(cols, tokens, n_adapters, &j);
+    if (tokens) split_columns(cols, tokens, rank, n_adapters, &j);
     // the parts, and their sum as two terms where there are more than few values
     *bytes = 4 * tokens * rank * (j.splits + (tokens * rank > kFewValues ? 1 : 0));
     return DF11_OK;
@@ -884,7 +895,7 @@ int df11_lora(const uint16_t *x, uint64_t x_stride, uint64_t tokens, uint32_t co
     s.job[0].w = a;
     s.job[0].part = static_cast<float *>(workspace);
     s.job[0].stride = x_stride;
-    split_columns(cols, tokens, n_adapters, &s.job[0]);
+    split_columns(cols, tokens, rank, n_adapters, &s.job[0]);
     s.adapter = adapter;
     s.tokens = tokens;
     s.rank = rank;
