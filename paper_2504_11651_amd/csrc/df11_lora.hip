@@ -16,10 +16,9 @@
 //           and out are read and written in whole rows; few tokens one by one;
 //   outer   dA and dB: 64 columns a wave over a chunk of tokens, partial sums
 //           for several chunks, then `join`.
-// u and v are sums in 32 bits; where they meet the matrix cores they are split
-// into two BF16 terms (16 bits of mantissa: an fp32 output is good to 2^-17 of
-// the adapter's part), and so is an fp32 dy.  x, A, B and a BF16 dy are BF16 and
-// lose nothing.  A tile of tokens may hold several adapters: a kernel goes
+// u and v are sums in 32 bits; where they meet the matrix cores they are cut into
+// three BF16 terms, which lose nothing, and so is an fp32 dy.  x, A, B and a BF16
+// dy are BF16 as they are.  A tile of tokens may hold several adapters: a kernel goes
 // through the distinct ones, each for its own tokens' rows; up to kFewTokens
 // tokens they are spread over workgroups instead.  A workgroup reads which
 // adapters its tokens have from `adapter`: nothing is sorted or prepared.
@@ -46,18 +45,39 @@ __device__ f32x4 mfma(const uint4 &a, const uint4 &b, f32x4 c) {
                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Eight floats as the sum of two BF16 terms each.
-__device__ void split8(const float *v, uint4 *high, uint4 *low) {
-    bf16x8 h, l;
+// Eight floats as the sums of three BF16 terms each, exactly: 24 bits of mantissa
+// cut into 8, 8 and 8, each remainder a difference without rounding.  An infinity
+// is all in the first term, and so is a NaN.
+constexpr uint32_t kTerms = 3;
+__device__ void split8(const float *v, uint4 *terms) {
+    uint32_t first[8], second[8], third[8];
+    float most = 0.0f;
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e) {
-        h[e] = static_cast<__bf16>(v[e]);
-        // an infinity or NaN is all in the first term
-        const float rest = v[e] - static_cast<float>(h[e]);
-        l[e] = static_cast<__bf16>(fabsf(static_cast<float>(h[e])) < INFINITY ? rest : 0.0f);
+        first[e] = __float_as_uint(v[e]) & 0xFFFF0000u;
+        const float rest = v[e] - __uint_as_float(first[e]);
+        second[e] = __float_as_uint(rest) & 0xFFFF0000u;
+        third[e] = __float_as_uint(rest - __uint_as_float(second[e]));
+        most += fabsf(rest);
     }
-    *high = __builtin_bit_cast(uint4, h);
-    *low = __builtin_bit_cast(uint4, l);
+    if (__any(!(most < INFINITY))) {  // inf - inf
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e)
+            if (!(fabsf(v[e]) < INFINITY)) {
+                // the quiet bit: cutting must not leave an infinity of a NaN
+                first[e] |= v[e] != v[e] ? 0x00400000u : 0u;
+                second[e] = third[e] = 0;
+            }
+    }
+    const auto pack = [](const uint32_t *w) {  // the upper halves
+        return uint4{__builtin_amdgcn_perm(w[1], w[0], 0x07060302u),
+                     __builtin_amdgcn_perm(w[3], w[2], 0x07060302u),
+                     __builtin_amdgcn_perm(w[5], w[4], 0x07060302u),
+                     __builtin_amdgcn_perm(w[7], w[6], 0x07060302u)};
+    };
+    terms[0] = pack(first);
+    terms[1] = pack(second);
+    terms[2] = pack(third);
 }
 
 __device__ uint4 zero4() { return uint4{0, 0, 0, 0}; }
@@ -127,20 +147,20 @@ struct Columns {
         for (uint32_t s = 0; s < kSub; ++s)
 #pragma unroll
             for (uint32_t e = 0; e < 2; ++e) {
-                uint4 high, low;
+                constexpr uint32_t kParts = T::kVec == 4 ? kTerms : 1;
+                uint4 t[kParts];
                 if constexpr (T::kVec == 4) {
                     float v[8];
 #pragma unroll
                     for (uint32_t i = 0; i < 8; ++i) v[i] = F32::get(x[s][2 * e + i / 4], i % 4);
-                    split8(v, &high, &low);
+                    split8(v, t);
                 } else {
-                    high = x[s][e];
+                    t[0] = x[s][e];
                 }
 #pragma unroll
-                for (uint32_t r = 0; r < kRanks; ++r) {
-                    acc[s][r] = mfma(high, w[r][e], acc[s][r]);
-                    if constexpr (T::kVec == 4) acc[s][r] = mfma(low, w[r][e], acc[s][r]);
-                }
+                for (uint32_t r = 0; r < kRanks; ++r)
+#pragma unroll
+                    for (uint32_t i = 0; i < kParts; ++i) acc[s][r] = mfma(t[i], w[r][e], acc[s][r]);
             }
     }
 };
@@ -238,8 +258,8 @@ __global__ __launch_bounds__(kThreads) void lora_shrink_kernel(ShrinkArgs g) {
 struct ExpandArgs {
     const float *part;
     const float *scale;
-    const uint16_t *high, *low;  // low as two terms, tokens x rank each
-    const uint16_t *w;           // n_adapters x len x rank
+    const uint16_t *terms;  // low as three terms, tokens x rank each
+    const uint16_t *w;      // n_adapters x len x rank
     const int32_t *adapter;
     const void *base;
     void *out;
@@ -252,8 +272,9 @@ __device__ void wave_lds_sync() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// kSteps products of 32 ranks; 0: up to 16 ranks, where one product holds both
-// terms of the split.
+// kSteps products of 32 ranks a term; 0: up to 16 ranks, where one product holds two
+// terms.  A BF16 out takes two terms (2^-16 of the adapter's part, where out itself
+// is rounded to 2^-9), an fp32 one all three.
 template <class T, uint32_t kSteps, uint32_t kTiles>
 __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
     constexpr uint32_t kFrags = kSteps ? kSteps : 1, kCols = 64, kRow = kCols + 4;
@@ -299,25 +320,29 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
                                                  : zero4();
                         }
                 }
-                uint4 high[kFrags], low[kFrags];
+                constexpr uint32_t kUse = T::kVec == 4 ? 3 : 2, kProducts = kSteps ? kUse : 2;
+                uint4 t[kProducts][kFrags];
 #pragma unroll
-                for (uint32_t k = 0; k < kFrags; ++k) {
-                    const uint32_t r = kSteps ? 32 * k + 8 * q : 8 * (q & 1u);
-                    const bool in = r < g.rank && (mine >> c & 1u);
-                    const uint64_t at = (t0 + c) * g.rank + r;
-                    high[k] = in ? *reinterpret_cast<const uint4 *>(g.high + at) : zero4();
-                    low[k] = in ? *reinterpret_cast<const uint4 *>(g.low + at) : zero4();
-                }
-                if (!kSteps && q >= 2) high[0] = low[0];
+                for (uint32_t k = 0; k < kFrags; ++k)
+#pragma unroll
+                    for (uint32_t i = 0; i < kProducts; ++i) {
+                        const uint32_t r = kSteps ? 32 * k + 8 * q : 8 * (q & 1u);
+                        // up to 16 ranks lane groups 2 and 3 hold the next term
+                        const uint32_t term = kSteps ? i : 2 * i + q / 2;
+                        const bool in = r < g.rank && (mine >> c & 1u) && term < kUse;
+                        t[i][k] = in ? *reinterpret_cast<const uint4 *>(
+                                           g.terms + (term * g.tokens + t0 + c) * g.rank + r)
+                                     : zero4();
+                    }
                 // column 16f + 4q + e of token c
 #pragma unroll
                 for (uint32_t f = 0; f < 4; ++f) {
                     f32x4 acc{0, 0, 0, 0};
 #pragma unroll
-                    for (uint32_t k = 0; k < kFrags; ++k) {
-                        acc = mfma(w[f][k], high[k], acc);
-                        if (kSteps) acc = mfma(w[f][k], low[k], acc);
-                    }
+                    for (uint32_t k = 0; k < kFrags; ++k)
+#pragma unroll
+                        for (uint32_t i = 0; i < (kSteps || kUse > 2 ? kProducts : 1); ++i)
+                            acc = mfma(w[f][k], t[i][k], acc);
                     *reinterpret_cast<f32x4 *>(mytile + c * kRow + 16 * f + 4 * q) = acc;
                 }
                 wave_lds_sync();
@@ -423,12 +448,12 @@ __global__ __launch_bounds__(kThreads) void lora_transpose_kernel(TransposeArgs 
     }
 }
 
-// u and v, their parts added, times the scale, as two BF16 terms each: tokens x
+// u and v, their parts added, times the scale, as three BF16 terms each: tokens x
 // rank for the expand kernel, and rank x `padded` tokens for the gradients (0 for
 // tokens without an adapter and past the last one).
 struct PrepareJob {
     const float *part;
-    uint16_t *rows, *ranks;  // the high terms; the low ones behind them; either may be null
+    uint16_t *rows, *ranks;  // the first terms, the others behind them; either may be null
     uint32_t splits;
 };
 struct PrepareArgs {
@@ -439,13 +464,14 @@ struct PrepareArgs {
     uint32_t rank, n_adapters;
 };
 
-// Four values as their high and their low terms.
-__device__ void split4(const float4 &v, uint2 *high, uint2 *low) {
+// Writes the terms of four values, `apart` values from each other.
+__device__ void put4(float4 v, uint16_t *to, uint64_t apart) {
     const float x[8] = {v.x, v.y, v.z, v.w, 0, 0, 0, 0};
-    uint4 h, l;
-    split8(x, &h, &l);
-    *high = uint2{h.x, h.y};
-    *low = uint2{l.x, l.y};
+    uint4 t[kTerms];
+    split8(x, t);
+#pragma unroll
+    for (uint32_t i = 0; i < kTerms; ++i)
+        *reinterpret_cast<uint2 *>(to + i * apart) = uint2{t[i].x, t[i].y};
 }
 
 __global__ __launch_bounds__(kThreads) void lora_prepare_kernel(PrepareArgs g) {
@@ -468,31 +494,22 @@ __global__ __launch_bounds__(kThreads) void lora_prepare_kernel(PrepareArgs g) {
             }
             s.x *= scale, s.y *= scale, s.z *= scale, s.w *= scale;
         }
-        if (j.rows && a >= -1) {
-            uint2 high, low;
-            split4(s, &high, &low);
-            uint16_t *to = j.rows + (t0 + row) * g.rank + r;
-            *reinterpret_cast<uint2 *>(to) = high;
-            *reinterpret_cast<uint2 *>(to + g.tokens * g.rank) = low;
-        }
+        if (j.rows && a >= -1) put4(s, j.rows + (t0 + row) * g.rank + r, g.tokens * g.rank);
         tile[row][r] = s.x, tile[row][r + 1] = s.y, tile[row][r + 2] = s.z, tile[row][r + 3] = s.w;
     }
     if (!j.ranks) return;
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kTokens / 4 * g.rank; i += kThreads) {
         const uint32_t r = i / (kTokens / 4), row = i % (kTokens / 4) * 4;
-        uint2 high, low;
-        split4(float4{tile[row][r], tile[row + 1][r], tile[row + 2][r], tile[row + 3][r]}, &high, &low);
-        uint16_t *to = j.ranks + r * g.padded + t0 + row;
-        *reinterpret_cast<uint2 *>(to) = high;
-        *reinterpret_cast<uint2 *>(to + g.rank * g.padded) = low;
+        put4(float4{tile[row][r], tile[row + 1][r], tile[row + 2][r], tile[row + 3][r]},
+             j.ranks + r * g.padded + t0 + row, g.rank * g.padded);
     }
 }
 
 // d[i][...] = sum over the chunk's tokens t of i: m[t][c] w[t][r]
 struct OuterJob {
     const void *m;
-    const uint16_t *terms;  // two terms of w, each rank x padded
+    const uint16_t *terms;  // three terms of w, each rank x padded
     float *d;               // n_adapters x len x rank, or rank x len: a chunk's
     uint64_t stride, chunk_floats;
     uint32_t len, blocks;
@@ -508,9 +525,13 @@ struct OuterArgs {
 
 constexpr uint32_t kScan = 4096;  // tokens whose adapters are looked at together
 
-// The terms of 128 tokens in LDS, a row per rank: 8 values more keep the 16 lanes
-// that read 16 bytes of 16 rows apart.
-constexpr uint32_t kPiece = 128, kPieceRow = kPiece + 8;
+// The terms of some tokens in LDS, a row per rank: 8 values more keep the 16 lanes
+// that read 16 bytes of 16 rows apart.  128 tokens up to rank 64, 52 KB, so that
+// three workgroups of rank 64 fit a CU.
+template <uint32_t kRanks>
+constexpr uint32_t kPiece = kRanks > 4 ? 64 : 128;
+template <uint32_t kRanks>
+constexpr uint32_t kPieceRow = kPiece<kRanks> + 8;
 
 template <class T, uint32_t kRanks>
 __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uint32_t *member,
@@ -522,7 +543,7 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
     const uint32_t col = min(c0 + 4 * c, j.len - 4);
     const auto *m = static_cast<const typename T::raw *>(j.m);
     const uint64_t from = uint64_t{blockIdx.y} * g.per, to = std::min(g.tokens, from + g.per);
-    uint16_t *const wh = terms, *const wl = terms + 16 * kRanks * kPieceRow;
+    constexpr uint32_t kPieceSteps = kPiece<kRanks> / 32, kTermSize = 16 * kRanks * kPieceRow<kRanks>;
     f32x4 acc[4][kRanks];
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e)
@@ -560,16 +581,16 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
             some = true;
             const uint32_t ours = bits >> (8 * q) & 0xFFu;
             // the terms of the step's piece: every wave comes here for the same steps
-            if (now / (kPiece / 32) != piece) {
-                piece = now / (kPiece / 32);
-                const uint64_t p0 = s0 + piece * kPiece;
+            if (now / kPieceSteps != piece) {
+                piece = now / kPieceSteps;
+                const uint64_t p0 = s0 + piece * kPiece<kRanks>;
                 __syncthreads();
-                constexpr uint32_t kEach = kPiece / 8;  // loads of a row
-                for (uint32_t i = threadIdx.x; i < 2 * g.rank * kEach; i += kThreads) {
-                    const uint32_t r = i / kEach, at = i % kEach * 8;  // r: high terms, then low ones
-                    const uint32_t rank = r < g.rank ? r : r - g.rank;
+                constexpr uint32_t kEach = kPiece<kRanks> / 8;  // loads of a row
+                for (uint32_t i = threadIdx.x; i < kTerms * g.rank * kEach; i += kThreads) {
+                    const uint32_t r = i / kEach, at = i % kEach * 8, term = r / g.rank;
                     if (p0 + at < g.padded)
-                        *reinterpret_cast<uint4 *>((r < g.rank ? wh : wl) + rank * kPieceRow + at) =
+                        *reinterpret_cast<uint4 *>(terms + term * kTermSize +
+                                                   (r - term * g.rank) * kPieceRow<kRanks> + at) =
                             *reinterpret_cast<const uint4 *>(j.terms + r * g.padded + p0 + at);
                 }
                 __syncthreads();
@@ -591,15 +612,36 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
                               (ours >> (2 * i + 1) & 1u ? 0xFFFF0000u : 0u);
             }
             // column 4c + e of the lane's eight tokens
-            uint4 mh[4], ml[4];
+            const auto w_term = [&](uint32_t r, uint32_t i) {
+                const uint32_t at = min(16 * r + c, g.rank - 1) * kPieceRow<kRanks> +
+                                    now % kPieceSteps * 32 + 8 * q;
+                uint4 w = *reinterpret_cast<const uint4 *>(terms + i * kTermSize + at);
+                w.x &= keep[0], w.y &= keep[1], w.z &= keep[2], w.w &= keep[3];
+                return w;
+            };
+            if constexpr (T::kVec == 4) {
+                // a column's terms at a time: four columns' do not fit the registers
 #pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) {
-                if constexpr (T::kVec == 4) {
+                for (uint32_t e = 0; e < 4; ++e) {
                     float v[8];
+                    uint4 t[kTerms];
 #pragma unroll
                     for (uint32_t i = 0; i < 8; ++i) v[i] = F32::get(row[i], e);
-                    split8(v, &mh[e], &ml[e]);
-                } else {
+                    split8(v, t);
+#pragma unroll
+                    for (uint32_t r = 0; r < kRanks; ++r)
+#pragma unroll
+                        for (uint32_t i = 0; i < kTerms; ++i) {
+                            const uint4 w = w_term(r, i);
+                            // products of 2^-24 and less of the whole are left out
+#pragma unroll
+                            for (uint32_t p = 0; p + i < kTerms; ++p) acc[e][r] = mfma(t[p], w, acc[e][r]);
+                        }
+                }
+            } else {
+                uint4 t[4];
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) {
                     uint32_t p[4];
                     const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;
 #pragma unroll
@@ -608,21 +650,16 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
                         const uint32_t y = e < 2 ? row[2 * i + 1].x : row[2 * i + 1].y;
                         p[i] = __builtin_amdgcn_perm(y, x, pick);
                     }
-                    mh[e] = uint4{p[0], p[1], p[2], p[3]};
+                    t[e] = uint4{p[0], p[1], p[2], p[3]};
                 }
-            }
 #pragma unroll
-            for (uint32_t r = 0; r < kRanks; ++r) {
-                const uint32_t at = min(16 * r + c, g.rank - 1) * kPieceRow + now % (kPiece / 32) * 32 + 8 * q;
-                uint4 h = *reinterpret_cast<const uint4 *>(wh + at), l = *reinterpret_cast<const uint4 *>(wl + at);
-                h.x &= keep[0], h.y &= keep[1], h.z &= keep[2], h.w &= keep[3];
-                l.x &= keep[0], l.y &= keep[1], l.z &= keep[2], l.w &= keep[3];
+                for (uint32_t r = 0; r < kRanks; ++r)
 #pragma unroll
-                for (uint32_t e = 0; e < 4; ++e) {
-                    acc[e][r] = mfma(mh[e], h, acc[e][r]);
-                    acc[e][r] = mfma(mh[e], l, acc[e][r]);
-                    if constexpr (T::kVec == 4) acc[e][r] = mfma(ml[e], h, acc[e][r]);
-                }
+                    for (uint32_t i = 0; i < kTerms; ++i) {
+                        const uint4 w = w_term(r, i);
+#pragma unroll
+                        for (uint32_t e = 0; e < 4; ++e) acc[e][r] = mfma(t[e], w, acc[e][r]);
+                    }
             }
         }
     }
@@ -653,10 +690,17 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
     }
 }
 
+// Waves on a SIMD: as many as the registers hold without spilling.
+template <class T>
+constexpr int outer_waves(uint32_t ranks) {
+    if (T::kVec == 4) return ranks == 1 ? 3 : ranks == 2 ? 2 : 1;
+    return ranks <= 2 ? 3 : ranks <= 4 ? 2 : 1;
+}
+
 template <class T, uint32_t kRanks>
-__global__ __launch_bounds__(kThreads, kRanks <= 2 ? 3 : 2) void lora_outer_kernel(OuterArgs g) {
+__global__ __launch_bounds__(kThreads, outer_waves<T>(kRanks)) void lora_outer_kernel(OuterArgs g) {
     __shared__ uint32_t member[kScan / 32];
-    __shared__ __align__(16) uint16_t terms[2 * 16 * kRanks * kPieceRow];
+    __shared__ __align__(16) uint16_t terms[kTerms * 16 * kRanks * kPieceRow<kRanks>];
     if (blockIdx.x < g.job[0].blocks)
         outer<T, kRanks>(g, g.job[0], blockIdx.x, member, terms);
     else
@@ -848,8 +892,8 @@ Space space_of(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank, uin
     s.at = take(2ull * n_adapters * cols * rank);
     s.u = take(4ull * s.ju.splits * tokens * rank);
     s.v = take(4ull * s.jv.splits * tokens * rank);
-    s.rows = take(4ull * rank * tokens);
-    s.terms = take(8ull * rank * s.padded);
+    s.rows = take(2ull * kTerms * rank * tokens);
+    s.terms = take(4ull * kTerms * rank * s.padded);
     s.present = take(4ull * s.chunks * n_adapters);
     s.db = take(s.chunks > 1 ? 4ull * s.chunks * n_adapters * rows * rank : 0);
     s.da = take(s.chunks > 1 ? 4ull * s.chunks * n_adapters * cols * rank : 0);
@@ -868,8 +912,8 @@ int df11_lora_workspace_bytes(uint64_t tokens, uint32_t cols, uint32_t rows, uin
     if (rc) return rc;
     ShrinkJob j{};
     if (tokens) split_columns(cols, tokens, rank, n_adapters, &j);
-    // the parts, and their sum as two terms where there are more than few values
-    *bytes = 4 * tokens * rank * (j.splits + (tokens * rank > kFewValues ? 1 : 0));
+    // the parts, and their sum as three terms where there are more than few values
+    *bytes = tokens * rank * (4 * j.splits + (tokens * rank > kFewValues ? 2 * kTerms : 0));
     return DF11_OK;
 }
 
@@ -903,7 +947,7 @@ int df11_lora(const uint16_t *x, uint64_t x_stride, uint64_t tokens, uint32_t co
     if ((rc = launch_shrink(s, DF11_BF16, stream))) return rc;
     const float *part = s.job[0].part;
     auto *terms = reinterpret_cast<uint16_t *>(s.job[0].part + s.job[0].splits * tokens * rank);
-    const ExpandArgs e{part, scale, terms, terms + tokens * rank, b, adapter, base, out, tokens, base_stride,
+    const ExpandArgs e{part, scale, terms, b, adapter, base, out, tokens, base_stride,
                        out_stride, rows, rank, n_adapters, s.job[0].splits, 0};
     if (tokens * rank <= kFewValues) return launch_expand_few(e, dtype, stream);
     const PrepareArgs p{{{part, terms, nullptr, s.job[0].splits}, {}}, scale, adapter, tokens, 0, rank,
@@ -985,13 +1029,13 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
 
     auto *by_row = reinterpret_cast<uint16_t *>(ws + s.rows);
     const PrepareArgs p{{{u, dx ? by_row : nullptr, da ? terms : nullptr, s.ju.splits},
-                         {v, nullptr, terms + 2 * rank * s.padded, s.jv.splits}},
+                         {v, nullptr, terms + kTerms * rank * s.padded, s.jv.splits}},
                         scale, adapter, tokens, s.padded, rank, n_adapters};
     hipLaunchKernelGGL(lora_prepare_kernel, dim3(s.padded / 32, da ? 2 : 1), dim3(kThreads), 0, stream, p);
     if ((rc = launched())) return rc;
 
     if (dx) {
-        const ExpandArgs e{u, scale, by_row, by_row + tokens * rank, at, adapter, dx_base, dx, tokens,
+        const ExpandArgs e{u, scale, by_row, at, adapter, dx_base, dx, tokens,
                            dx_base_stride, dx_stride, cols, rank, n_adapters, s.ju.splits, 0};
         if ((rc = launch_expand(e, DF11_BF16, stream))) return rc;
     }
@@ -1002,7 +1046,7 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
     auto *pb = reinterpret_cast<float *>(ws + s.db), *pa = reinterpret_cast<float *>(ws + s.da);
     const uint64_t fb = uint64_t{n_adapters} * rows * rank, fa = uint64_t{n_adapters} * cols * rank;
     // dB takes v, the second pair of terms, and dA takes u, the first
-    const OuterArgs o{{{dy, terms + 2 * rank * s.padded, many ? pb : db, dy_stride, fb, rows,
+    const OuterArgs o{{{dy, terms + kTerms * rank * s.padded, many ? pb : db, dy_stride, fb, rows,
                         (rows + 255) / 256, false},
                        {x, terms, many ? pa : da, x_stride, fa, cols, (cols + 255) / 256, true}},
                       adapter, many ? present : nullptr, tokens, s.padded, s.per, rank, n_adapters};
