@@ -103,21 +103,16 @@ struct Held {
         // whole vectors first, all loads under way before the first is looked at;
         // then the lane whose vector the row's end cuts takes single values
         constexpr uint32_t both = T::kVec == 8 ? T::kMasked * 0x10001u : T::kMasked;
-        const uint4 masked{both, both, both, both};
-        if (vocab >= T::kVec) {
 #pragma unroll
-            for (uint32_t i = 0; i < kVecs<T>; ++i) {
-                const uint32_t j = first(part, i);
-                q[i] = load16(z + (j + T::kVec <= vocab ? j : 0));
-            }
+        for (uint32_t i = 0; i < kVecs<T>; ++i) {
+            const uint32_t j = first(part, i);
+            q[i] = uint4{both, both, both, both};
+            if (j + T::kVec <= vocab) q[i] = load16(z + j);
         }
 #pragma unroll
         for (uint32_t i = 0; i < kVecs<T>; ++i) {
             const uint32_t j = first(part, i);
-            if (j + T::kVec > vocab) {
-                q[i] = masked;
-                if (j < vocab) q[i] = cut_vector(z + j, vocab - j);
-            }
+            if (j < vocab && j + T::kVec > vocab) q[i] = cut_vector(z + j, vocab - j);
         }
     }
     __device__ static uint4 cut_vector(const typename T::raw *z, uint32_t n) {

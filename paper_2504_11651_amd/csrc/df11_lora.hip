@@ -291,11 +291,13 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
     auto *out = static_cast<typename T::raw *>(g.out);
     int32_t loaded = -1;
     uint4 w[4][kFrags];
+    static_assert(kTiles * kTile <= 64, "a lane a token");
+    const int32_t ids = adapter_of(g.adapter, group * kTiles * kTile + lane, g.tokens, g.n_adapters);
 #pragma unroll 1
     for (uint32_t s = 0; s < kTiles; ++s) {
         const uint64_t t0 = (group * kTiles + s) * kTile;
         if (t0 >= g.tokens) return;
-        const int32_t id = adapter_of(g.adapter, t0 + c, g.tokens, g.n_adapters);
+        const int32_t id = __shfl(ids, kTile * s + c);
         each_adapter<kTile>(id, -1, [&](int32_t a, uint64_t mine) {
             uint4 held[kTrips];
 #pragma unroll
@@ -586,12 +588,26 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
                 const uint64_t p0 = s0 + piece * kPiece<kRanks>;
                 __syncthreads();
                 constexpr uint32_t kEach = kPiece<kRanks> / 8;  // loads of a row
-                for (uint32_t i = threadIdx.x; i < kTerms * g.rank * kEach; i += kThreads) {
-                    const uint32_t r = i / kEach, at = i % kEach * 8, term = r / g.rank;
-                    if (p0 + at < g.padded)
-                        *reinterpret_cast<uint4 *>(terms + term * kTermSize +
-                                                   (r - term * g.rank) * kPieceRow<kRanks> + at) =
-                            *reinterpret_cast<const uint4 *>(j.terms + r * g.padded + p0 + at);
+                constexpr uint32_t kLoads = kTerms * 16 * kRanks * kEach / kThreads, kBatch = 6;
+                static_assert(kLoads % kBatch == 0 || kLoads < kBatch, "whole batches");
+                // a batch of loads under way at a time; rows past the rank repeat the last
+                // one, which is never multiplied into a rank that is kept
+#pragma unroll
+                for (uint32_t b = 0; b < kLoads; b += kBatch) {
+                    uint4 v[kBatch];
+#pragma unroll
+                    for (uint32_t k = 0; k < kBatch && b + k < kLoads; ++k) {
+                        const uint32_t i = (b + k) * kThreads + threadIdx.x, row = i / kEach;
+                        const uint32_t term = row / (16 * kRanks), r = row % (16 * kRanks);
+                        const uint64_t at = std::min<uint64_t>(p0 + i % kEach * 8, g.padded - 8);
+                        v[k] = *reinterpret_cast<const uint4 *>(
+                            j.terms + (term * g.rank + min(r, g.rank - 1)) * g.padded + at);
+                    }
+#pragma unroll
+                    for (uint32_t k = 0; k < kBatch && b + k < kLoads; ++k) {
+                        const uint32_t i = (b + k) * kThreads + threadIdx.x, row = i / kEach;
+                        *reinterpret_cast<uint4 *>(terms + row * kPieceRow<kRanks> + i % kEach * 8) = v[k];
+                    }
                 }
                 __syncthreads();
             }
@@ -613,8 +629,7 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
             }
             // column 4c + e of the lane's eight tokens
             const auto w_term = [&](uint32_t r, uint32_t i) {
-                const uint32_t at = min(16 * r + c, g.rank - 1) * kPieceRow<kRanks> +
-                                    now % kPieceSteps * 32 + 8 * q;
+                const uint32_t at = (16 * r + c) * kPieceRow<kRanks> + now % kPieceSteps * 32 + 8 * q;
                 uint4 w = *reinterpret_cast<const uint4 *>(terms + i * kTermSize + at);
                 w.x &= keep[0], w.y &= keep[1], w.z &= keep[2], w.w &= keep[3];
                 return w;

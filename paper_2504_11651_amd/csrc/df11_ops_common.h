@@ -78,9 +78,10 @@ struct BF16 {
     using Max = PackedMax<BF16>;
     // A word taken as a float is its upper value with the lower one's bits behind
     // its mantissa: it compares with a rounded bound as the upper value does, which
-    // need not be cut out first.  (-inf becomes a NaN: not at least anything.)
+    // need not be cut out first.  (-inf becomes a NaN: not at least anything.)  The
+    // bound of a negative value, and of 0 for the sake of -0, has all those bits set.
     static __device__ float at_least(float least, uint32_t e) {
-        const uint32_t u = __float_as_uint(least);
+        const uint32_t u = __float_as_uint(least == 0.0f ? -0.0f : least);
         return e & 1 && u & 0x80000000u ? __uint_as_float(u | 0xFFFFu) : least;
     }
     static __device__ float rough(const uint4 &q, uint32_t e) {

@@ -146,6 +146,22 @@ def test_alternatives_among_equal_and_ordered_values(kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("best", [-0.0, 0.0, -1.0, -2.0 ** -14])
+def test_few_alternatives_above_negative_values(best, dtype):
+    """The bound of the alternatives is 0 or negative, in either half of a word."""
+    vocab = 9001
+    for odd in (0, 1):
+        z = torch.full((2, vocab), -3.5)
+        z[:, 1::2] = -4.25
+        places = torch.arange(7) * 1200 + 2 * torch.arange(7) + odd
+        z[0, places] = best
+        z[1, places[:3]] = best
+        z[1, places[3:]] = 0.0 if best == 0 else best
+        check_logprobs(place(z, dtype), torch.tensor([int(places[3]), 5]), 7, 1.0)
+        check_logprobs(place(z, dtype, 1), torch.tensor([int(places[3]), 5]), 3, 0.5)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_masked_rows(dtype):
     vocab, top = 18001, 40
     z, _ = draw(9, vocab, 5)

@@ -148,6 +148,29 @@ def test_adapters(kind, tokens):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rank", [8, 16, 24, 32, 40, 64, 72, 128])
+@pytest.mark.parametrize("kind", ["runs", "scattered", "one for all", "mostly none"])
+def test_many_tokens(kind, rank, dtype):
+    """More tokens than are spread over workgroups by adapter."""
+    n, tokens = 5, 333
+    g = torch.Generator().manual_seed(rank)
+    adapter = {"runs": runs(tokens, n, rank), "scattered": torch.randint(-1, n, (tokens,), generator=g).int(),
+               "one for all": torch.full((tokens,), 2, dtype=torch.int32),
+               "mostly none": torch.where(torch.rand(tokens, generator=g) < 0.05, 4, -1).int()}[kind]
+    check(tokens, 448, 336, rank, n, adapter, dtype, rank)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n", [1, 3, 40])
+def test_chunks_of_tokens(n, dtype):
+    """Token counts that the gradients take in several chunks, and in more than one
+    look at the adapters; some chunks hold nothing of an adapter."""
+    tokens = 9100
+    adapter = (torch.arange(tokens) // 700 % (n + 1) - 1).int()
+    check(tokens, 64, 48, 16, n, adapter, dtype, n)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_optional_arguments(dtype):
     tokens, n = 37, 3
     x, a, b, scale, y, z = draw(tokens, 128, 96, 16, n, 5)
