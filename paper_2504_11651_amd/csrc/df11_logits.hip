@@ -180,16 +180,23 @@ struct Exponent {
         : m(fmaxf(most, kLowest)), c(tau.c), rest(tau.rest),
           mc(most == -INFINITY ? 0.0f : m * c), two_over_tau(tau.two_over),
           near(fabsf(mc) < 1e38f) {}
-    // what is to be taken from x: m (c + rest) is mc plus this
-    __device__ float shift() const {
-        return near && m != kLowest ? fmaf(m, rest, fmaf(m, c, -mc)) : 0.0f;
+    // what is to be taken from x: m c, with the second part of c if x has it, is mc
+    // plus this
+    __device__ float shift(bool whole) const {
+        if (!near || m == kLowest) return 0.0f;
+        return whole ? fmaf(m, rest, fmaf(m, c, -mc)) : fmaf(m, c, -mc);
     }
-    template <class T>
+    // Without the second part each x is short of a 2^-24th, so that sum e is short of
+    // that times ln 2 sum e x, and sum e x of that times itself, to first order.
+    __device__ float more() const { return near ? rest / c : 0.0f; }
+    // kWhole: with the second part of c; without it the sums are corrected by more()
+    template <class T, bool kWhole>
     __device__ void operator()(const uint4 &q, float *v, float *x) const {
 #pragma unroll
         for (uint32_t k = 0; k < T::kVec; ++k) {
             v[k] = T::get(q, k);
-            x[k] = fmaf(v[k], rest, fmaf(v[k], c, -mc));
+            x[k] = fmaf(v[k], c, -mc);
+            if constexpr (kWhole) x[k] = fmaf(v[k], rest, x[k]);
         }
         if (!near) {
             float far = two_over_tau;
@@ -388,32 +395,41 @@ __device__ void logprob_part(const LogprobArgs &g) {
     uint32_t above = 0;
 #pragma unroll
     for (uint32_t i = 0; i < kVecs<T>; ++i) {
-        float v[T::kVec], x[T::kVec], sum = 0.0f;
-        x_of.operator()<T>(h.q[i], v, x);
+        float v[T::kVec], x[T::kVec], e[T::kVec], sum = 0.0f;
+        x_of.operator()<T, false>(h.q[i], v, x);
 #pragma unroll
         for (uint32_t k = 0; k < T::kVec; ++k) {
-            const float e = __builtin_amdgcn_exp2f(x[k]);
-            s += e;
-            sum = fmaf(e, fmaxf(x[k], -300.0f), sum);  // no 0 * inf
+            e[k] = __builtin_amdgcn_exp2f(x[k]);
+            s += e[k];
+            sum = fmaf(e[k], x[k], sum);
+        }
+        if (__any(sum != sum)) {  // 0 * -inf of a masked value
+            asm volatile("" : "+v"(sum));
+            sum = 0.0f;
+#pragma unroll
+            for (uint32_t k = 0; k < T::kVec; ++k) sum = fmaf(e[k], fmaxf(x[k], -300.0f), sum);
         }
         t += sum;
         if (here) {
             const uint32_t j = h.first(part, i);
 #pragma unroll
-            for (uint32_t k = 0; k < T::kVec; ++k) above += v[k] >= (j + k < tok ? zt : more) ? 1u : 0u;
+            for (uint32_t k = 0; k < T::kVec; ++k)
+                above += __popcll(__ballot(v[k] >= (j + k < tok ? zt : more)));
         } else {
 #pragma unroll
-            for (uint32_t k = 0; k < T::kVec; ++k) above += v[k] >= rest ? 1u : 0u;
+            for (uint32_t k = 0; k < T::kVec; ++k) above += __popcll(__ballot(v[k] >= rest));
         }
         // a vector's values at a time in registers
-        asm volatile("" : "+v"(s), "+v"(t), "+v"(above));
+        asm volatile("" : "+v"(s), "+v"(t), "+s"(above));
     }
     s = wave_sum(s);
     t = wave_sum(t);
-    above = wave_sum(above);
     if ((threadIdx.x & 63u) == 0) {
-        const float shift = x_of.shift(), f = __builtin_amdgcn_exp2f(-shift);
-        wave_stat[threadIdx.x >> 6] = PartStat{x_of.m, s * f, f * fmaf(-shift, s, t), above};
+        const float shift = x_of.shift(false), f = __builtin_amdgcn_exp2f(-shift);
+        t = fmaf(-shift, s, t);
+        s = fmaf(x_of.more() * kLn2, t, s);
+        t = fmaf(x_of.more(), t, t);
+        wave_stat[threadIdx.x >> 6] = PartStat{x_of.m, s * f, t * f, above};
     }
     if constexpr (kTop) lane_key[threadIdx.x] = ordered(lane_max);
     __syncthreads();
@@ -544,7 +560,9 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
             if (g.logprob) g.logprob[row] = lp;
             if (g.rank) g.rank[row] = asked && !broken ? static_cast<int64_t>(above) : -1;
             if (g.entropy) g.entropy[row] = h;
-            if (g.stats) *reinterpret_cast<float4 *>(g.stats + 4 * row) = float4{p.m, static_cast<float>(ln_s), h, lp};
+            if (g.stats)
+                *reinterpret_cast<float4 *>(g.stats + 4 * row) =
+                    float4{p.m, static_cast<float>(ln_s), h, lp};
             row_m = p.m;
             row_ln_s = ln_s;
             row_s = broken ? -1.0f : p.s;
@@ -673,9 +691,9 @@ struct LogprobGradArgs {
 };
 
 // Writes f(value, index) for the values of a part.
-template <class T, class F>
-__device__ void store_part(const Held<T> &h, typename T::raw *out, uint32_t part, uint32_t vocab,
-                           bool once, F f) {
+template <class T, bool kOnce, class F>
+__device__ void store_values(const Held<T> &h, typename T::raw *out, uint32_t part, uint32_t vocab,
+                             F f) {
 #pragma unroll
     for (uint32_t i = 0; i < kVecs<T>; ++i) {
         const uint32_t j = Held<T>::first(part, i);
@@ -683,18 +701,26 @@ __device__ void store_part(const Held<T> &h, typename T::raw *out, uint32_t part
 #pragma unroll
         for (uint32_t e = 0; e < T::kVec; ++e) r[e] = T::store(f(T::get(h.q[i], e), j + e));
         if (j + T::kVec <= vocab) {
-            if (once) {
-                keep_apart();
+            if constexpr (kOnce)
                 store16_once(out + j, __builtin_bit_cast(uint4, r));
-                keep_apart();
-            } else {
+            else
                 store16(out + j, __builtin_bit_cast(uint4, r));
-            }
         } else {
 #pragma unroll
             for (uint32_t e = 0; e < T::kVec; ++e)
                 if (j + e < vocab) out[j + e] = r[e];
         }
+    }
+}
+template <class T, class F>
+__device__ void store_part(const Held<T> &h, typename T::raw *out, uint32_t part, uint32_t vocab,
+                           bool once, F f) {
+    if (once) {
+        keep_apart();
+        store_values<T, true>(h, out, part, vocab, f);
+        keep_apart();
+    } else {
+        store_values<T, false>(h, out, part, vocab, f);
     }
 }
 
@@ -774,7 +800,7 @@ __global__ __launch_bounds__(kThreads, 8) void distill_part_kernel(DistillArgs g
 #pragma unroll
     for (uint32_t i = 0; i < kVecs<T>; ++i) {
         float v[T::kVec], e[T::kVec], sum = 0.0f;
-        x_of.operator()<T>(h.q[i], v, e);
+        x_of.operator()<T, true>(h.q[i], v, e);
 #pragma unroll
         for (uint32_t k = 0; k < T::kVec; ++k) {
             e[k] = __builtin_amdgcn_exp2f(e[k]);
@@ -794,7 +820,7 @@ __global__ __launch_bounds__(kThreads, 8) void distill_part_kernel(DistillArgs g
     s = wave_sum(s);
     t = wave_sum(t);
     if ((threadIdx.x & 63u) == 0) {
-        const float f = __builtin_amdgcn_exp2f(-x_of.shift());
+        const float f = __builtin_amdgcn_exp2f(-x_of.shift(true));
         wave_stat[threadIdx.x >> 6] = PartStat{x_of.m, s * f, t * f, 0};
     }
     __syncthreads();
@@ -829,7 +855,8 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     bad = __any(bad);
     mass = wave_sum(mass);
     uint64_t none;
-    const PartStat st = join_parts(first, g.stat + row * g.parts, g.parts, g.tau.two_over, false, &none);
+    const PartStat st =
+        join_parts(first, g.stat + row * g.parts, g.parts, g.tau.two_over, false, &none);
     // a row's few terms in 64 bits: the loss is a difference of larger ones
     const double ln_s = log(static_cast<double>(st.s));
     const double scale = g.tail ? 1.0 : 1.0 / mass, ln_mass = g.tail ? 0.0 : log(mass);

@@ -127,8 +127,8 @@ struct ShrinkArgs {
 template <class T, uint32_t kRanks, uint32_t kSub>
 struct Columns {
     uint4 x[kSub][T::kVec == 4 ? 4 : 2], w[kRanks][2];
-    __device__ void load(const typename T::raw *const *row, const uint16_t *w0, uint32_t k, uint32_t len,
-                         uint32_t rank, uint32_t c, bool in) {
+    __device__ void load(const typename T::raw *const *row, const uint16_t *w0, uint32_t k,
+                         uint32_t len, uint32_t rank, uint32_t c, bool in) {
 #pragma unroll
         for (uint32_t s = 0; s < kSub; ++s)
 #pragma unroll
@@ -160,7 +160,8 @@ struct Columns {
 #pragma unroll
                 for (uint32_t r = 0; r < kRanks; ++r)
 #pragma unroll
-                    for (uint32_t i = 0; i < kParts; ++i) acc[s][r] = mfma(t[i], w[r][e], acc[s][r]);
+                    for (uint32_t i = 0; i < kParts; ++i)
+                        acc[s][r] = mfma(t[i], w[r][e], acc[s][r]);
             }
     }
 };
@@ -171,7 +172,9 @@ struct Columns {
 // rank 16: one 124 us, two 110); else more tiles only lower the number of waves
 // (6001 tokens, rank 16: one 18.1 us, two 21.6).  Above 64 ranks four do not fit the
 // registers.
-constexpr uint32_t wide_tiles(uint32_t rank, bool f32) { return !f32 && rank > 32 && rank <= 64 ? 4 : rank > 16 || f32 ? 2 : 1; }
+constexpr uint32_t wide_tiles(uint32_t rank, bool f32) {
+    return !f32 && rank > 32 && rank <= 64 ? 4 : rank > 16 || f32 ? 2 : 1;
+}
 constexpr uint32_t wide_tokens(uint32_t rank, bool f32) {
     return kTile * kWaves * wide_tiles(rank, f32);
 }
@@ -184,7 +187,8 @@ template <class T, uint32_t kRanks, bool kWide, uint32_t kWideTiles>
 __device__ void shrink(const ShrinkArgs &g, const ShrinkJob &j, uint32_t split, float *red) {
     constexpr uint32_t kSub = kWide ? kWideTiles : 1, kTokens = kSub * kTile;
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, c = lane & 15u, q = lane >> 4;
-    const uint64_t t0 = (uint64_t{blockIdx.x} * (kWide ? kWaves : 1) + (kWide ? wave : 0)) * kTokens;
+    const uint64_t t0 =
+        (uint64_t{blockIdx.x} * (kWide ? kWaves : 1) + (kWide ? wave : 0)) * kTokens;
     if (t0 >= g.tokens) return;  // a whole workgroup, or a wave that meets no barrier
     const int32_t id = adapter_of(g.adapter, t0 + (lane & (kTokens - 1)), g.tokens, g.n_adapters);
     const typename T::raw *x[kSub];
@@ -221,7 +225,8 @@ __device__ void shrink(const ShrinkArgs &g, const ShrinkJob &j, uint32_t split, 
                     for (uint32_t e = 0; e < 4; ++e) {
                         const uint32_t row = kTile * s + 4 * q + e;
                         if (mine >> row & 1u && 16 * r + c < g.rank)
-                            j.part[(split * g.tokens + t0 + row) * g.rank + 16 * r + c] = acc[s][r][e];
+                            j.part[(split * g.tokens + t0 + row) * g.rank + 16 * r + c] =
+                                acc[s][r][e];
                     }
         } else {
             __syncthreads();
@@ -292,7 +297,8 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
     int32_t loaded = -1;
     uint4 w[4][kFrags];
     static_assert(kTiles * kTile <= 64, "a lane a token");
-    const int32_t ids = adapter_of(g.adapter, group * kTiles * kTile + lane, g.tokens, g.n_adapters);
+    const int32_t ids =
+        adapter_of(g.adapter, group * kTiles * kTile + lane, g.tokens, g.n_adapters);
 #pragma unroll 1
     for (uint32_t s = 0; s < kTiles; ++s) {
         const uint64_t t0 = (group * kTiles + s) * kTile;
@@ -305,7 +311,8 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
                 const uint32_t row = i * (64 / kLanes) + lane / kLanes;
                 held[i] = zero4();
                 if (base && (mine >> row & 1u) && col < g.len)
-                    held[i] = *reinterpret_cast<const uint4 *>(base + (t0 + row) * g.base_stride + col);
+                    held[i] =
+                        *reinterpret_cast<const uint4 *>(base + (t0 + row) * g.base_stride + col);
             }
             if (a >= 0) {
                 if (a != loaded) {
@@ -356,9 +363,11 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
                 const float *d = mytile + row * kRow + T::kVec * (lane % kLanes);
 #pragma unroll
                 for (uint32_t e = 0; e < T::kVec; e += 4) {
-                    const f32x4 v = a >= 0 ? *reinterpret_cast<const f32x4 *>(d + e) : f32x4{0, 0, 0, 0};
+                    const f32x4 v =
+                        a >= 0 ? *reinterpret_cast<const f32x4 *>(d + e) : f32x4{0, 0, 0, 0};
 #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k) o[e + k] = T::store(T::get(held[i], e + k) + v[k]);
+                    for (uint32_t k = 0; k < 4; ++k)
+                        o[e + k] = T::store(T::get(held[i], e + k) + v[k]);
                 }
                 if ((mine >> row & 1u) && col < g.len)
                     *reinterpret_cast<uint4 *>(out + (t0 + row) * g.out_stride + col) =
@@ -379,12 +388,14 @@ __global__ __launch_bounds__(kThreads) void lora_expand_few_kernel(ExpandArgs g)
     const uint32_t col = blockIdx.x * kThreads + threadIdx.x;
     const bool in = col < g.len;
     float v = 0.0f;
-    if (in && g.base) v = T::load(static_cast<const typename T::raw *>(g.base)[t * g.base_stride + col]);
+    if (in && g.base)
+        v = T::load(static_cast<const typename T::raw *>(g.base)[t * g.base_stride + col]);
     if (a >= 0) {
         if (threadIdx.x < g.rank) {
             float s = 0.0f;
 #pragma unroll 4
-            for (uint32_t p = 0; p < g.splits; ++p) s += g.part[(p * g.tokens + t) * g.rank + threadIdx.x];
+            for (uint32_t p = 0; p < g.splits; ++p)
+                s += g.part[(p * g.tokens + t) * g.rank + threadIdx.x];
             low[threadIdx.x] = s * (g.scale ? g.scale[a] : 1.0f);
         }
         __syncthreads();
@@ -428,14 +439,16 @@ __global__ __launch_bounds__(kThreads) void lora_transpose_kernel(TransposeArgs 
     for (uint32_t i = 0; i < 2; ++i) {
         const uint32_t r = threadIdx.x / 8 + 32 * i, c = threadIdx.x % 8 * 8;
         if (r0 + r < j.rows && c0 + c < j.cols)
-            v[i] = *reinterpret_cast<const uint4 *>(j.from + at + static_cast<uint64_t>(r0 + r) * j.cols + c0 + c);
+            v[i] = *reinterpret_cast<const uint4 *>(
+                j.from + at + static_cast<uint64_t>(r0 + r) * j.cols + c0 + c);
     }
 #pragma unroll
     for (uint32_t i = 0; i < 2; ++i) {
         const uint32_t r = threadIdx.x / 8 + 32 * i, c = threadIdx.x % 8 * 8;
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e)
-            tile[(c + e) * kRow + r] = static_cast<uint16_t>(F32::word(v[i], e / 2) >> 16 * (e & 1u));
+            tile[(c + e) * kRow + r] =
+                static_cast<uint16_t>(F32::word(v[i], e / 2) >> 16 * (e & 1u));
     }
     __syncthreads();
 #pragma unroll
@@ -443,10 +456,11 @@ __global__ __launch_bounds__(kThreads) void lora_transpose_kernel(TransposeArgs 
         const uint32_t c = threadIdx.x / 8 + 32 * i, r = threadIdx.x % 8 * 8;
         uint32_t w[4];
         for (uint32_t e = 0; e < 4; ++e)
-            w[e] = tile[c * kRow + r + 2 * e] | static_cast<uint32_t>(tile[c * kRow + r + 2 * e + 1]) << 16;
+            w[e] = tile[c * kRow + r + 2 * e] |
+                   static_cast<uint32_t>(tile[c * kRow + r + 2 * e + 1]) << 16;
         if (r0 + r < j.rows && c0 + c < j.cols)
-            *reinterpret_cast<uint4 *>(j.to + at + static_cast<uint64_t>(c0 + c) * j.rows + r0 + r) =
-                uint4{w[0], w[1], w[2], w[3]};
+            *reinterpret_cast<uint4 *>(j.to + at + static_cast<uint64_t>(c0 + c) * j.rows + r0 +
+                                       r) = uint4{w[0], w[1], w[2], w[3]};
     }
 }
 
@@ -545,7 +559,8 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
     const uint32_t col = min(c0 + 4 * c, j.len - 4);
     const auto *m = static_cast<const typename T::raw *>(j.m);
     const uint64_t from = uint64_t{blockIdx.y} * g.per, to = std::min(g.tokens, from + g.per);
-    constexpr uint32_t kPieceSteps = kPiece<kRanks> / 32, kTermSize = 16 * kRanks * kPieceRow<kRanks>;
+    constexpr uint32_t kPieceSteps = kPiece<kRanks> / 32;
+    constexpr uint32_t kTermSize = 16 * kRanks * kPieceRow<kRanks>;
     f32x4 acc[4][kRanks];
 #pragma unroll
     for (uint32_t e = 0; e < 4; ++e)
@@ -606,7 +621,8 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
 #pragma unroll
                     for (uint32_t k = 0; k < kBatch && b + k < kLoads; ++k) {
                         const uint32_t i = (b + k) * kThreads + threadIdx.x, row = i / kEach;
-                        *reinterpret_cast<uint4 *>(terms + row * kPieceRow<kRanks> + i % kEach * 8) = v[k];
+                        *reinterpret_cast<uint4 *>(terms + row * kPieceRow<kRanks> +
+                                                   i % kEach * 8) = v[k];
                     }
                 }
                 __syncthreads();
@@ -629,7 +645,8 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
             }
             // column 4c + e of the lane's eight tokens
             const auto w_term = [&](uint32_t r, uint32_t i) {
-                const uint32_t at = (16 * r + c) * kPieceRow<kRanks> + now % kPieceSteps * 32 + 8 * q;
+                const uint32_t at =
+                    (16 * r + c) * kPieceRow<kRanks> + now % kPieceSteps * 32 + 8 * q;
                 uint4 w = *reinterpret_cast<const uint4 *>(terms + i * kTermSize + at);
                 w.x &= keep[0], w.y &= keep[1], w.z &= keep[2], w.w &= keep[3];
                 return w;
@@ -650,7 +667,8 @@ __device__ void outer(const OuterArgs &g, const OuterJob &j, uint32_t block, uin
                             const uint4 w = w_term(r, i);
                             // products of 2^-24 and less of the whole are left out
 #pragma unroll
-                            for (uint32_t p = 0; p + i < kTerms; ++p) acc[e][r] = mfma(t[p], w, acc[e][r]);
+                            for (uint32_t p = 0; p + i < kTerms; ++p)
+                                acc[e][r] = mfma(t[p], w, acc[e][r]);
                         }
                 }
             } else {
@@ -791,7 +809,8 @@ int check_workspace(const void *ws, uint64_t have, uint64_t need) {
 void split_columns(uint32_t len, uint64_t tokens, uint32_t rank, uint32_t n_adapters,
                    ShrinkJob *j) {
     const uint64_t wgs = tokens <= kFewTokens
-                             ? (tokens + kTile - 1) / kTile * std::min<uint64_t>({16, n_adapters, tokens})
+                             ? (tokens + kTile - 1) / kTile *
+                                   std::min<uint64_t>({16, n_adapters, tokens})
                              : (tokens + wide_tokens(rank, false) - 1) / wide_tokens(rank, false);
     const uint32_t most = std::min(32u, std::max(1u, len / 512));
     const uint32_t want = static_cast<uint32_t>(std::min<uint64_t>(most, (1024 + wgs - 1) / wgs));
@@ -831,8 +850,10 @@ int launch_shrink(const ShrinkArgs &s, hipStream_t stream) {
 
 int launch_shrink(const ShrinkArgs &s, uint32_t dtype, hipStream_t stream) {
     if (s.tokens <= kFewTokens)
-        return dtype == DF11_F32 ? launch_shrink<F32, false>(s, stream) : launch_shrink<BF16, false>(s, stream);
-    return dtype == DF11_F32 ? launch_shrink<F32, true>(s, stream) : launch_shrink<BF16, true>(s, stream);
+        return dtype == DF11_F32 ? launch_shrink<F32, false>(s, stream)
+                                 : launch_shrink<BF16, false>(s, stream);
+    return dtype == DF11_F32 ? launch_shrink<F32, true>(s, stream)
+                             : launch_shrink<BF16, true>(s, stream);
 }
 
 int launch_expand_few(const ExpandArgs &e, uint32_t dtype, hipStream_t stream) {
@@ -850,7 +871,7 @@ int launch_expand(ExpandArgs e, hipStream_t stream) {
     const uint64_t wgs = (e.tokens + kTile * kTiles - 1) / (kTile * kTiles) * e.blocks;
     if (wgs > 0xFFFFFFFFull / kThreads) return DF11_E_UNSUPPORTED;
     const dim3 grid(wgs, 1,
-                    kTiles == 1 ? std::min<uint64_t>({16, uint64_t{e.n_adapters} + 1, e.tokens}) : 1);
+                    kTiles == 1 ? std::min<uint64_t>({16, e.n_adapters + 1ull, e.tokens}) : 1);
     const dim3 block(kThreads);
     if (e.rank <= 16)
         hipLaunchKernelGGL((lora_expand_kernel<T, 0, kTiles>), grid, block, 0, stream, e);
@@ -865,8 +886,10 @@ int launch_expand(ExpandArgs e, hipStream_t stream) {
 
 int launch_expand(const ExpandArgs &e, uint32_t dtype, hipStream_t stream) {
     if (e.tokens <= kFewTokens)
-        return dtype == DF11_F32 ? launch_expand<F32, 1>(e, stream) : launch_expand<BF16, 1>(e, stream);
-    return dtype == DF11_F32 ? launch_expand<F32, 4>(e, stream) : launch_expand<BF16, 4>(e, stream);
+        return dtype == DF11_F32 ? launch_expand<F32, 1>(e, stream)
+                                 : launch_expand<BF16, 1>(e, stream);
+    return dtype == DF11_F32 ? launch_expand<F32, 4>(e, stream)
+                             : launch_expand<BF16, 4>(e, stream);
 }
 
 template <class T>
@@ -965,9 +988,10 @@ int df11_lora(const uint16_t *x, uint64_t x_stride, uint64_t tokens, uint32_t co
     const ExpandArgs e{part, scale, terms, b, adapter, base, out, tokens, base_stride,
                        out_stride, rows, rank, n_adapters, s.job[0].splits, 0};
     if (tokens * rank <= kFewValues) return launch_expand_few(e, dtype, stream);
-    const PrepareArgs p{{{part, terms, nullptr, s.job[0].splits}, {}}, scale, adapter, tokens, 0, rank,
-                        n_adapters};
-    hipLaunchKernelGGL(lora_prepare_kernel, dim3((tokens + 31) / 32), dim3(kThreads), 0, stream, p);
+    const PrepareArgs p{{{part, terms, nullptr, s.job[0].splits}, {}},
+                        scale, adapter, tokens, 0, rank, n_adapters};
+    hipLaunchKernelGGL(lora_prepare_kernel, dim3((tokens + 31) / 32), dim3(kThreads), 0, stream,
+                       p);
     if ((rc = launched())) return rc;
     return launch_expand(e, dtype, stream);
 }
@@ -1013,7 +1037,8 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
 
     const Space s = space_of(tokens, cols, rows, rank, n_adapters);
     char *ws = static_cast<char *>(workspace);
-    auto *bt = reinterpret_cast<uint16_t *>(ws + s.bt), *at = reinterpret_cast<uint16_t *>(ws + s.at);
+    auto *bt = reinterpret_cast<uint16_t *>(ws + s.bt);
+    auto *at = reinterpret_cast<uint16_t *>(ws + s.at);
     auto *u = reinterpret_cast<float *>(ws + s.u), *v = reinterpret_cast<float *>(ws + s.v);
     auto *terms = reinterpret_cast<uint16_t *>(ws + s.terms);
 
@@ -1046,7 +1071,8 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
     const PrepareArgs p{{{u, dx ? by_row : nullptr, da ? terms : nullptr, s.ju.splits},
                          {v, nullptr, terms + kTerms * rank * s.padded, s.jv.splits}},
                         scale, adapter, tokens, s.padded, rank, n_adapters};
-    hipLaunchKernelGGL(lora_prepare_kernel, dim3(s.padded / 32, da ? 2 : 1), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(lora_prepare_kernel, dim3(s.padded / 32, da ? 2 : 1), dim3(kThreads), 0,
+                       stream, p);
     if ((rc = launched())) return rc;
 
     if (dx) {
