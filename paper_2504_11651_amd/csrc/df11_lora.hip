@@ -804,14 +804,25 @@ int check_workspace(const void *ws, uint64_t have, uint64_t need) {
     return need && (!ws || misaligned(ws, 16)) ? DF11_E_INVALID_ARG : DF11_OK;
 }
 
+// Whether `shrink` gives each wave tiles of its own.  Its workgroups are fewer and
+// take four times as long, but read w for many more tokens at once: where they are
+// many, or where a read of w for every 16 tokens would come to more than 64 MB.
+// Us, wide and not: 574 tokens x (14336 + 4096) columns, rank 24, fp32 31.6 and
+// 19.6; 1604 x 4096, rank 24 15.8 and 9.9; 6001 x 4096, rank 16 19.8 and 19.7; 8192
+// x (4096 + 4096), rank 64 62 and 85; 1024 x 128,256, rank 16, fp32 111 and 131.
+bool is_wide(uint64_t tokens, uint32_t rank, uint64_t columns) {
+    if (tokens <= kFewTokens) return false;
+    const uint64_t wgs = tokens / wide_tokens(rank, false) * std::min<uint64_t>(32, columns / 512);
+    return wgs >= 512 || tokens / kTile * rank * columns * 2 > (64ull << 20);
+}
+
 // Columns of a split and how many splits: about 1024 workgroups in all, each of
 // at least 512 columns, at most 32 sums to add.
-void split_columns(uint32_t len, uint64_t tokens, uint32_t rank, uint32_t n_adapters,
+void split_columns(uint32_t len, uint64_t tokens, uint32_t rank, uint32_t n_adapters, bool wide,
                    ShrinkJob *j) {
-    const uint64_t wgs = tokens <= kFewTokens
-                             ? (tokens + kTile - 1) / kTile *
-                                   std::min<uint64_t>({16, n_adapters, tokens})
-                             : (tokens + wide_tokens(rank, false) - 1) / wide_tokens(rank, false);
+    uint64_t wgs = (tokens + kTile - 1) / kTile;
+    if (tokens <= kFewTokens) wgs *= std::min<uint64_t>({16, n_adapters, tokens});
+    if (wide) wgs = (tokens + wide_tokens(rank, false) - 1) / wide_tokens(rank, false);
     const uint32_t most = std::min(32u, std::max(1u, len / 512));
     const uint32_t want = static_cast<uint32_t>(std::min<uint64_t>(most, (1024 + wgs - 1) / wgs));
     j->len = len;
@@ -834,7 +845,7 @@ template <class T, bool kWide>
 int launch_shrink(const ShrinkArgs &s, hipStream_t stream) {
     const uint64_t tile = kWide ? wide_tokens(s.rank, T::kVec == 4) : kTile;
     const dim3 grid((s.tokens + tile - 1) / tile, s.job[0].splits + s.job[1].splits,
-                    kWide ? 1 : std::min<uint64_t>({16, s.n_adapters, s.tokens}));
+                    s.tokens <= kFewTokens ? std::min<uint64_t>({16, s.n_adapters, s.tokens}) : 1);
     const dim3 block(kThreads);
     const uint32_t ranks = (s.rank + 15) / 16;
     if (ranks == 1)
@@ -848,12 +859,12 @@ int launch_shrink(const ShrinkArgs &s, hipStream_t stream) {
     return launched();
 }
 
-int launch_shrink(const ShrinkArgs &s, uint32_t dtype, hipStream_t stream) {
-    if (s.tokens <= kFewTokens)
-        return dtype == DF11_F32 ? launch_shrink<F32, false>(s, stream)
-                                 : launch_shrink<BF16, false>(s, stream);
-    return dtype == DF11_F32 ? launch_shrink<F32, true>(s, stream)
-                             : launch_shrink<BF16, true>(s, stream);
+int launch_shrink(const ShrinkArgs &s, uint32_t dtype, bool wide, hipStream_t stream) {
+    if (wide)
+        return dtype == DF11_F32 ? launch_shrink<F32, true>(s, stream)
+                                 : launch_shrink<BF16, true>(s, stream);
+    return dtype == DF11_F32 ? launch_shrink<F32, false>(s, stream)
+                             : launch_shrink<BF16, false>(s, stream);
 }
 
 int launch_expand_few(const ExpandArgs &e, uint32_t dtype, hipStream_t stream) {
@@ -912,12 +923,14 @@ struct Space {
     uint64_t bt, at, u, v, rows, terms, present, db, da, bytes;
     uint64_t padded, per, chunks;
     ShrinkJob ju, jv;
+    bool wide;
 };
 Space space_of(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank, uint32_t n_adapters) {
     Space s{};
     s.padded = up(tokens, 32);
-    split_columns(rows, std::max<uint64_t>(tokens, 1), rank, n_adapters, &s.ju);
-    split_columns(cols, std::max<uint64_t>(tokens, 1), rank, n_adapters, &s.jv);
+    s.wide = is_wide(tokens, rank, uint64_t{rows} + cols);
+    split_columns(rows, std::max<uint64_t>(tokens, 1), rank, n_adapters, s.wide, &s.ju);
+    split_columns(cols, std::max<uint64_t>(tokens, 1), rank, n_adapters, s.wide, &s.jv);
     s.per = std::max<uint64_t>(32, chunk_tokens(tokens, cols, rows, rank, n_adapters));
     s.chunks = std::max<uint64_t>(1, (tokens + s.per - 1) / s.per);
     uint64_t at = 0;
@@ -949,7 +962,8 @@ int df11_lora_workspace_bytes(uint64_t tokens, uint32_t cols, uint32_t rows, uin
     const int rc = check_shapes(tokens, cols, rows, rank, n_adapters);
     if (rc) return rc;
     ShrinkJob j{};
-    if (tokens) split_columns(cols, tokens, rank, n_adapters, &j);
+    if (tokens)
+        split_columns(cols, tokens, rank, n_adapters, is_wide(tokens, rank, cols), &j);
     // the parts, and their sum as three terms where there are more than few values
     *bytes = tokens * rank * (4 * j.splits + (tokens * rank > kFewValues ? 2 * kTerms : 0));
     return DF11_OK;
@@ -977,12 +991,13 @@ int df11_lora(const uint16_t *x, uint64_t x_stride, uint64_t tokens, uint32_t co
     s.job[0].w = a;
     s.job[0].part = static_cast<float *>(workspace);
     s.job[0].stride = x_stride;
-    split_columns(cols, tokens, rank, n_adapters, &s.job[0]);
+    const bool wide = is_wide(tokens, rank, cols);
+    split_columns(cols, tokens, rank, n_adapters, wide, &s.job[0]);
     s.adapter = adapter;
     s.tokens = tokens;
     s.rank = rank;
     s.n_adapters = n_adapters;
-    if ((rc = launch_shrink(s, DF11_BF16, stream))) return rc;
+    if ((rc = launch_shrink(s, DF11_BF16, wide, stream))) return rc;
     const float *part = s.job[0].part;
     auto *terms = reinterpret_cast<uint16_t *>(s.job[0].part + s.job[0].splits * tokens * rank);
     const ExpandArgs e{part, scale, terms, b, adapter, base, out, tokens, base_stride,
@@ -1065,7 +1080,7 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
     h.tokens = tokens;
     h.rank = rank;
     h.n_adapters = n_adapters;
-    if ((rc = launch_shrink(h, dy_dtype, stream))) return rc;
+    if ((rc = launch_shrink(h, dy_dtype, s.wide, stream))) return rc;
 
     auto *by_row = reinterpret_cast<uint16_t *>(ws + s.rows);
     const PrepareArgs p{{{u, dx ? by_row : nullptr, da ? terms : nullptr, s.ju.splits},

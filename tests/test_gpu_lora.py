@@ -161,6 +161,18 @@ def test_many_tokens(kind, rank, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("tokens, rank", [(6001, 16), (8211, 24), (4099, 64), (2131, 128)])
+@pytest.mark.parametrize("scattered", [False, True])
+def test_long_prompts(tokens, rank, scattered, dtype):
+    """So many values that a wave takes tiles of tokens of its own: whole tiles of one
+    adapter, tiles that several share, tokens without."""
+    n = 3
+    g = torch.Generator().manual_seed(tokens)
+    adapter = torch.randint(-1, n, (tokens,), generator=g).int() if scattered else runs(tokens, n, rank)
+    check(tokens, 4096, 48, rank, n, adapter, dtype, rank)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("n", [1, 3, 40])
 def test_chunks_of_tokens(n, dtype):
     """Token counts that the gradients take in several chunks, and in more than one
