@@ -17,19 +17,19 @@
 //     only few are above (about 1.3 top for values in any order).  They go to
 //     the workspace unordered; the join orders the few that are left, by value
 //     and index, which are distinct, so the order they arrived in is gone;
-//   - where more than the workspace's room are above (equal values, ordered
-//     ones), the part is trimmed exactly, over all its values and then over the
-//     indices of the equal ones.
+//   - where more than the workspace has room for are above (equal values, ordered
+//     ones), a higher bound is found by bisection, and equal values are taken in
+//     the order of their indices.
 // Rows that start at any address are read with unaligned 16-byte loads.
 //
 // Kernel times, and what bounds them (4096 rows of 128,256 bf16 values are 1.05 GB:
 // 215 us at the 4.9 TB/s of a device copy):
-//   64 alternatives    parts 270 us, join 44 us: instruction issue, about 19
+//   64 alternatives    parts 270 us, join 41 us: instruction issue, about 19
 //                      vector instructions a value, a third of them for the
 //                      alternatives (the threshold, and the values above it);
 //   distillation       parts 199 us (5.3 TB/s), join 11, gradient 345 us (6.1
 //                      TB/s, reads and writes past the caches): memory;
-//   one row, fp32, 20  parts 6.6 us, join 7.1: loads and barriers after one another.
+//   one row, fp32, 20  parts 6.6 us, join 6.9: loads and barriers after one another.
 // Holding two parts, with the next one's loads under way while one is worked on,
 // takes registers for half the waves and was slower (283 against 240 us); groups of
 // rows whose logits stay in the memory-side cache between the two passes of the
@@ -327,55 +327,69 @@ __device__ uint32_t reached_by(const uint32_t *lane_key, uint32_t top) {
     return cut;
 }
 
-// A part's `top` largest values, exactly, where more than fit reach `cut`: the
-// last of them by bisection over all values (not where `cut` is it already: equal
-// values), then the index up to which values equal to it are taken.  Reads the
-// part again: it is rare, and the registers it would need are not.
+// Where more of a part's values reach `cut` than there is room for: the least
+// bound above that leaves room, by bisection over all values (the next value where
+// those equal to `cut` are the many), or, where equal values are too many for any
+// bound, those above them and the first of them in the order of the indices.
+// Returns how many values it wrote, `top` at least.  Reads the part again: it is
+// rare, and the registers it would need are not.
 template <class T>
-__device__ inline void trim_part(const typename T::raw *z, uint32_t part,
-                                                    uint32_t vocab, uint32_t cut, uint32_t top,
-                                                    uint2 *out, uint32_t *lds) {
-    const uint32_t to = min(kPart, vocab - part);
+__device__ inline uint32_t trim_part(const typename T::raw *z, uint32_t part, uint32_t vocab,
+                                     uint32_t cut, uint32_t top, uint32_t room, uint2 *out,
+                                     uint32_t *lds) {
+    const uint32_t to = min(kPart, vocab - part), wave = threadIdx.x >> 6;
     z += part;
     auto count = [&](auto f) {
         uint32_t n = 0;
 #pragma unroll 4
-        for (uint32_t i = threadIdx.x; i < to; i += kThreads) n += f(T::load(z[i]), i) ? 1u : 0u;
+        for (uint32_t i = threadIdx.x; i < to; i += kThreads) n += f(T::load(z[i])) ? 1u : 0u;
         return wg_sum(n, lds);
     };
+    // values above `last` are taken; `larger` of them
     uint32_t lo = cut, hi = 0xFF800000u;  // ordered bits of +inf
     float last = from_ordered(lo);
-    uint32_t larger = count([&](float v, uint32_t) { return v > last; });
-    while (lo < hi && larger >= top) {
+    uint32_t larger = count([&](float v) { return v > last; });
+    while (larger > room && lo < hi) {
         const uint32_t mid = hi - (hi - lo) / 2;
         const float at = from_ordered(mid);
-        if (count([&](float v, uint32_t) { return v >= at; }) >= top) {
+        if (count([&](float v) { return v >= at; }) >= top) {
             lo = mid;
             last = at;
-            larger = count([&](float v, uint32_t) { return v > last; });
+            larger = count([&](float v) { return v > at; });
         } else {
             hi = mid - 1;
         }
     }
-    uint32_t from = 0, until = kPart - 1;
-    while (from < until) {
-        const uint32_t mid = from + (until - from) / 2;
-        if (larger + count([&](float v, uint32_t i) { return v == last && i <= mid; }) >= top)
-            until = mid;
-        else
-            from = mid + 1;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) lds[0] = 0;
-    __syncthreads();
-#pragma unroll 1
-    for (uint32_t i = threadIdx.x; i < to; i += kThreads) {
-        const float v = T::load(z[i]);
-        if (v > last || (v == last && i <= until)) {
-            const uint32_t slot = atomicAdd(&lds[0], 1u);
-            if (slot < top) out[slot] = uint2{ordered(v), part + i};
+    if (larger) {
+        __syncthreads();
+        if (threadIdx.x == 0) lds[0] = 0;
+        __syncthreads();
+#pragma unroll 4
+        for (uint32_t i = threadIdx.x; i < to; i += kThreads) {
+            const float v = T::load(z[i]);
+            if (v > last) {
+                const uint32_t slot = atomicAdd(&lds[0], 1u);
+                if (slot < room) out[slot] = uint2{ordered(v), part + i};
+            }
         }
     }
+    uint32_t n = larger;
+    for (uint32_t i0 = 0; i0 < to && n < top; i0 += kThreads) {
+        const uint32_t i = i0 + threadIdx.x;
+        const bool equal = i < to && T::load(z[min(i, to - 1)]) == last;
+        const uint64_t all = __ballot(equal);
+        __syncthreads();
+        if ((threadIdx.x & 63u) == 0) lds[wave] = __popcll(all);
+        __syncthreads();
+        uint32_t slot = n + before(all), here = 0;
+        for (uint32_t w = 0; w < kWaves; ++w) {
+            slot += w < wave ? lds[w] : 0;
+            here += lds[w];
+        }
+        if (equal && slot < top) out[slot] = uint2{ordered(last), part + i};
+        n = min(n + here, max(top, n));
+    }
+    return n;
 }
 
 template <class T, bool kTop>
@@ -487,8 +501,7 @@ __device__ void logprob_part(const LogprobArgs &g) {
                 out[at + i] = uint2{ordered(__uint_as_float(v.x)), v.y};
             }
         } else {
-            trim_part<T>(z, part, g.vocab, cut, g.top, out, counts);
-            total = g.top;
+            total = trim_part<T>(z, part, g.vocab, cut, g.top, g.room, out, counts);
         }
         if (threadIdx.x == 0) g.count[blockIdx.x] = total;
     }
@@ -662,10 +675,19 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
         const uint32_t lo = wave * n / kWaves, hi = (wave + 1) * n / kWaves;
         for (uint32_t c = lane; c < n; c += 64) {
             const uint32_t k = list_key[c], i = list_idx[c];
-            uint32_t larger = 0;
+            uint32_t larger = 0, same = c >= lo && c < hi ? ~0u : 0;
 #pragma unroll 4
-            for (uint32_t d = lo; d < hi; ++d)
-                larger += list_key[d] > k || (list_key[d] == k && list_idx[d] < i) ? 1u : 0u;
+            for (uint32_t d = lo; d < hi; ++d) {
+                larger += list_key[d] > k ? 1u : 0u;
+                same += list_key[d] == k ? 1u : 0u;
+            }
+            if (__any(same != 0)) {  // equal keys: by their indices
+#pragma unroll 4
+                for (uint32_t d = lo; d < hi; ++d) {
+                    const bool first = (list_key[d] == k) & (list_idx[d] < i);
+                    larger += first ? 1u : 0u;
+                }
+            }
             atomicAdd(&place[c], larger);
         }
         __syncthreads();
