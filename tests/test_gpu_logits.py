@@ -146,6 +146,25 @@ def test_alternatives_among_equal_and_ordered_values(kind, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("top", [1, 20, 64, 128])
+def test_alternatives_that_crowd_in_few_lanes(top, dtype):
+    """Sorted rows, and rows in which a run of places holds all that is not masked,
+    by -inf or by the lowest finite value."""
+    z = torch.randn((6, 24600), generator=torch.Generator().manual_seed(top)) * 2
+    z[0] = z[0].sort(descending=True).values
+    z[1] = z[1].sort().values
+    z[2, :9000] = torch.finfo(dtype).min
+    z[2, 9300:] = torch.finfo(dtype).min
+    z[3, :9000] = -INF
+    z[3, 9300:] = -INF
+    z[4, 300:] = torch.finfo(dtype).min
+    z[5] = torch.where(torch.arange(24600) % 8200 < 300, 4.0, z[5].clamp(max=3.0))
+    tokens = torch.tensor([0, 24599, 9100, 9100, 20000, 8300])
+    check_logprobs(place(z, dtype), tokens, top, 1.0)
+    check_logprobs(place(z, dtype, 3), tokens, top, 0.8)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("best", [-0.0, 0.0, -1.0, -2.0 ** -14])
 def test_few_alternatives_above_negative_values(best, dtype):
     """The bound of the alternatives is 0 or negative, in either half of a word."""
