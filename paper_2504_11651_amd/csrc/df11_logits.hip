@@ -183,8 +183,10 @@ struct PartStat {
 
 // x = (v - m) log2e / tau for the values of a wave with the wave's maximum m, up
 // to a shift that is the same for all of them: v c - m c, fused, with m c rounded.
-// Where m c leaves the range (masks of the lowest finite value, logits of 10^37)
-// the differences are taken first.
+// The shift, that rounding and (with the second part of c) m times it, goes through
+// exp2 and is taken out of the sums again, so it must be small: below 1 for |m c| up
+// to 2^22.  Beyond (waves of masks of -1e9 or the lowest finite value, logits of
+// millions) the differences are taken first.
 struct Exponent {
     float m, c, rest, mc, two_over_tau;
     bool near;
@@ -192,11 +194,11 @@ struct Exponent {
     __device__ Exponent(float most, const Tau &tau)
         : m(fmaxf(most, kLowest)), c(tau.c), rest(tau.rest),
           mc(most == -INFINITY ? 0.0f : m * c), two_over_tau(tau.two_over),
-          near(fabsf(mc) < 1e38f) {}
+          near(fabsf(mc) < 4194304.0f) {}
     // what is to be taken from x: m c, with the second part of c if x has it, is mc
     // plus this
     __device__ float shift(bool whole) const {
-        if (!near || m == kLowest) return 0.0f;
+        if (!near || mc == 0.0f) return 0.0f;
         return whole ? fmaf(m, rest, fmaf(m, c, -mc)) : fmaf(m, c, -mc);
     }
     // Without the second part each x is short of a 2^-24th, so that sum e is short of
