@@ -36,6 +36,8 @@
 // distillation end too many launches early (656 against 600 us at 192 MB).
 #include "df11_ops_common.h"
 
+#include <limits>
+
 namespace {
 
 using namespace df11ops;
@@ -61,6 +63,8 @@ struct Tau {
         c = static_cast<float>(M_LOG2E / tau);
         if (c >= M_LOG2E / tau) c = std::nextafterf(c, 0.0f);
         rest = static_cast<float>(M_LOG2E / tau - c);
+        // not 0 where that is below the float range (tau of 10^37 and more): 0 * -inf
+        if (rest == 0.0f) rest = std::numeric_limits<float>::denorm_min();
     }
 };
 

@@ -1,15 +1,16 @@
 """Finite masks and far-off values on the GPU: rows whose masked places fill whole
 waves and parts with a large negative number instead of -inf, rows of such a number
-alone, and rows with a large common offset.  Oracle and tolerances are those of
-test_gpu_logits."""
+alone, rows with a large common offset, and very large temperatures.  Oracle and
+tolerances are those of test_gpu_logits."""
+import math
+
 import pytest
 import torch
 
 from paper_2504_11651_amd import ops
 
 from conftest import gpu_available
-from test_gpu_logits import (INF, Rows, check_distill, check_grad, check_logprobs, grad_logprobs,
-                             place)
+from test_gpu_logits import (INF, check_distill, check_grad, check_logprobs, grad_logprobs, place)
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs an MI355X")]
 
@@ -83,3 +84,18 @@ def test_common_offset(dtype, offset, tau):
     index = torch.stack([torch.zeros(3, dtype=torch.int64), tokens], 1)
     for tail in (True, False):
         check_distill(place(z, dtype), index, torch.tensor([[-0.5, -2.0]]).repeat(3, 1), tail, tau, gl)
+
+
+@pytest.mark.parametrize("tau", [1e20, 1e30, 1e37, 1e38, 3e38])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_very_large_temperatures(dtype, tau):
+    """All that is not masked is alike; what is masked stays so."""
+    z, tokens = masked_rows(-INF, 9)
+    z[4] = -INF
+    check_logprobs(place(z, dtype), tokens, 5, tau)
+    index = torch.tensor([[3, 9000, 8]]).repeat(6, 1)
+    logp = torch.log(torch.tensor([[0.5, 0.3, 0.0]])).repeat(6, 1)
+    index[1:4] = torch.tensor([[17500, 17599, 0], [0, 2, 4], [5, 8199, 1]])
+    index[5] = torch.tensor([0, 3000, 6000])
+    for tail in (True, False):
+        check_distill(place(z, dtype), index, logp, tail, tau, torch.full((6,), math.sqrt(tau)))
