@@ -869,8 +869,11 @@ __global__ __launch_bounds__(kThreads, 8) void distill_part_kernel(DistillArgs g
 }
 
 // One wave per row: the loss from the parts and the student's values at the
-// named places, and what the gradient needs: m, ln S, the factor of q where no
-// place is named, and that of the teacher's probability (below 0: no gradient).
+// named places, and what the gradient needs: m, ln S (+inf: no gradient) and, with
+// the tail, the factor of q where no place is named, without it what scales the
+// teacher's probabilities exp(lt - top) / sum.  They are taken relative to the
+// largest, so that their sum to divide by is between 1 and `top` however little
+// the teacher gives the named places.
 template <class T>
 __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     const uint64_t row = blockIdx.x;
@@ -878,7 +881,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
     const PartStat first = lane < g.parts ? g.stat[row * g.parts + lane] : kNoStat;
     constexpr uint32_t kMost = DF11_MAX_TOP / 64;
-    float lt[kMost], v[kMost];
+    float lt[kMost], v[kMost], top = -INFINITY;
     double p[kMost], mass = 0.0;
     bool some = false, bad = false;
 #pragma unroll
@@ -888,8 +891,14 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
         lt[e] = k < g.top ? g.teacher[row * g.top + k] : 0.0f;
         some |= named(at);
         bad |= bad_entry(at, lt[e], g.vocab);
-        p[e] = named(at) ? exp(static_cast<double>(lt[e])) : 0.0;
+        if (!named(at)) lt[e] = -INFINITY;
         v[e] = named(at) && at < g.vocab ? T::load(z[at]) : 0.0f;
+        top = fmaxf(top, lt[e]);
+    }
+    top = g.tail ? 0.0f : wave_max(top);
+#pragma unroll
+    for (uint32_t e = 0; e < kMost; ++e) {
+        p[e] = lt[e] > -INFINITY ? exp(static_cast<double>(lt[e]) - top) : 0.0;
         mass += p[e];
     }
     some = __any(some);
@@ -900,7 +909,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
         join_parts(first, g.stat + row * g.parts, g.parts, g.tau.two_over, false, &none);
     // a row's few terms in 64 bits: the loss is a difference of larger ones
     const double ln_s = log(static_cast<double>(st.s));
-    const double scale = g.tail ? 1.0 : 1.0 / mass, ln_mass = g.tail ? 0.0 : log(mass);
+    const double scale = g.tail ? 1.0 : 1.0 / mass, ln_mass = g.tail ? 0.0 : top + log(mass);
     double sum = 0.0;
 #pragma unroll
     for (uint32_t e = 0; e < kMost; ++e)
@@ -910,25 +919,25 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     if (lane) return;
     const double left = static_cast<double>(st.t) / st.s, r = fmax(0.0, 1.0 - mass);
     const float nan = __builtin_nanf("");
-    float other = 1.0f, factor = static_cast<float>(scale);
+    float other = 1.0f, out_ln_s = static_cast<float>(ln_s);
     if (g.tail && r > 0.0) {
         sum += r * (log(r) - log(left));
         other = left > 0.0 ? static_cast<float>(1.0 - r / left) : 0.0f;
     }
     float loss = static_cast<float>(sum);
     if (st.s == 0.0f) {
-        factor = -1.0f;
+        out_ln_s = INFINITY;
         loss = INFINITY;
     }
-    if (!(st.s >= 0.0f) || st.s == INFINITY) loss = other = nan;
+    if (!(st.s >= 0.0f) || st.s == INFINITY) loss = out_ln_s = nan;
     if (!some || (!g.tail && mass == 0.0)) {
         loss = 0.0f;
-        factor = -1.0f;
+        out_ln_s = INFINITY;
     }
-    if (bad) loss = other = factor = nan;
+    if (bad) loss = out_ln_s = nan;
     g.loss[row] = loss;
-    *reinterpret_cast<float4 *>(g.stats + 4 * row) = 
-        float4{st.m, static_cast<float>(ln_s), other, factor};
+    *reinterpret_cast<float4 *>(g.stats + 4 * row) =
+        float4{st.m, out_ln_s, g.tail ? other : top, g.tail ? 0.0f : static_cast<float>(scale)};
 }
 
 // q times its factor everywhere, then the few named places of the part once
@@ -944,10 +953,11 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g
     Held<T> h;
     h.load(z, part, g.vocab, g.once);
     const float4 st = *reinterpret_cast<const float4 *>(g.stats + 4 * row);
-    const float m = st.x, log2_s = st.y * kLog2e, other = st.z, factor = st.w;
+    const float m = st.x, log2_s = st.y * kLog2e, other = g.tail ? st.z : 1.0f;
+    const float top = g.tail ? 0.0f : st.z, scale = g.tail ? 1.0f : st.w;
     const float w = (g.weight ? g.weight[row] : 1.0f) * (0.5f * g.tau.two_over);
-    const bool none = factor < 0.0f;  // not for a NaN
-    const float every = factor != factor ? factor : other * w;
+    const bool none = st.y == INFINITY;
+    const float every = other * w;
 
     // a thread an entry; the places of this part go to LDS, so that an entry
     // sees whether its place is named again
@@ -961,13 +971,13 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g
     float value = 0.0f, target = 0.0f;
     if (mine) {
         value = T::load(z[at]);
-        target = expf(g.teacher[row * g.top + threadIdx.x]);
+        target = expf(g.teacher[row * g.top + threadIdx.x] - top);
         uint32_t same = 0;
         for (uint32_t k = 0; k < many; ++k) same += place[k] == at ? 1u : 0u;
         if (same > 1) {  // all its entries, in their order: each of them writes the same
             target = 0.0f;
             for (uint32_t k = 0; k < g.top; ++k)
-                if (g.index[row * g.top + k] == at) target += expf(g.teacher[row * g.top + k]);
+                if (g.index[row * g.top + k] == at) target += expf(g.teacher[row * g.top + k] - top);
         }
     }
     __syncthreads();
@@ -978,7 +988,7 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g
     __syncthreads();
     if (mine && !none) {
         const float y = fmaf(scaled(value, m, g.tau.two_over), kLog2e, -log2_s);
-        out[at] = T::store((__builtin_amdgcn_exp2f(y) - target * factor) * w);
+        out[at] = T::store((__builtin_amdgcn_exp2f(y) - target * scale) * w);
     }
 }
 
