@@ -177,12 +177,17 @@ __device__ double scaled64(float v, float m, const Tau &tau) {
 }
 
 // What a part, or several, says about its row: maximum (at least the lowest
-// finite value, so that masked values give exp(-inf)), sum e, and a second sum:
-// e x in powers of two for the entropy, or e over the places a teacher does
-// not name.
+// finite value, so that masked values give exp(-inf)), sum e, sum e x in powers of
+// two for the entropy, and how many values are above the token's.
 struct PartStat {
     float m, s, t;
     uint32_t above;
+};
+// The same for the distillation: maximum and sum e of all values, and of those at
+// places that the teacher does not name, which may be less than 32 bits hold
+// beside the first.  The second maximum may be larger than the values are.
+struct PairStat {
+    float m, s, other_m, other_s;
 };
 
 // x = (v - m) log2e / tau for the values of a wave with the wave's maximum m, up
@@ -228,49 +233,75 @@ struct Exponent {
 
 // Sums with maximum m scaled to the larger maximum M: the factor, and for the
 // sum of e x the shift of x.
-__device__ void rescale(const PartStat &p, float M, float two_over_tau, bool xsum, float *s,
-                        float *t) {
+__device__ void rescale(const PartStat &p, float M, float two_over_tau, float *s, float *t) {
     const float d = fmaxf(scaled(p.m, M, two_over_tau) * kLog2e, -300.0f);
     const float f = d <= -300.0f ? 0.0f : __builtin_amdgcn_exp2f(d);
     *s += p.s * f;
-    *t += f * (xsum ? fmaf(d, p.s, p.t) : p.t);
+    *t += f * fmaf(d, p.s, p.t);
+}
+// One sum, scaled so.
+__device__ float rescaled(float s, float m, float M, float two_over_tau) {
+    const float d = fmaxf(scaled(m, M, two_over_tau) * kLog2e, -300.0f);
+    return s * (d <= -300.0f ? 0.0f : __builtin_amdgcn_exp2f(d));
 }
 
 // The waves' statistics as one, by every thread, after a barrier.
-__device__ PartStat join_waves(const PartStat *w, float two_over_tau, bool xsum) {
+__device__ PartStat join_waves(const PartStat *w, float two_over_tau) {
     PartStat p{w[0].m, 0.0f, 0.0f, 0};
     for (uint32_t i = 1; i < kWaves; ++i) p.m = fmaxf(p.m, w[i].m);
     for (uint32_t i = 0; i < kWaves; ++i) {
-        rescale(w[i], p.m, two_over_tau, xsum, &p.s, &p.t);
+        rescale(w[i], p.m, two_over_tau, &p.s, &p.t);
         p.above += w[i].above;
     }
     return p;
 }
+__device__ PairStat join_two(const PairStat &a, const PairStat &b, float two_over_tau) {
+    PairStat p{fmaxf(a.m, b.m), 0.0f, fmaxf(a.other_m, b.other_m), 0.0f};
+    p.s = rescaled(a.s, a.m, p.m, two_over_tau) + rescaled(b.s, b.m, p.m, two_over_tau);
+    p.other_s = rescaled(a.other_s, a.other_m, p.other_m, two_over_tau) +
+                rescaled(b.other_s, b.other_m, p.other_m, two_over_tau);
+    return p;
+}
+__device__ PairStat join_waves(const PairStat *w, float two_over_tau) {
+    return join_two(join_two(w[0], w[1], two_over_tau), join_two(w[2], w[3], two_over_tau),
+                    two_over_tau);
+}
+static_assert(kWaves == 4, "two pairs of waves");
 
 constexpr PartStat kNoStat{kLowest, 0.0f, 0.0f, 0};
+constexpr PairStat kNoPair{kLowest, 0.0f, kLowest, 0.0f};
 
 // The parts' statistics of a row as one, by a wave.  `mine`: this lane's, of the
 // first 64.
 __device__ PartStat join_parts(PartStat mine, const PartStat *stat, uint32_t parts,
-                               float two_over_tau, bool xsum, uint64_t *above) {
+                               float two_over_tau, uint64_t *above) {
     const uint32_t lane = threadIdx.x & 63u;
     uint64_t count = mine.above;
     for (uint32_t i = lane + 64; i < parts; i += 64) {  // past 524,288 values
         const PartStat p = stat[i];
         const float M = fmaxf(mine.m, p.m);
         PartStat both{M, 0.0f, 0.0f, 0};
-        rescale(mine, M, two_over_tau, xsum, &both.s, &both.t);
-        rescale(p, M, two_over_tau, xsum, &both.s, &both.t);
+        rescale(mine, M, two_over_tau, &both.s, &both.t);
+        rescale(p, M, two_over_tau, &both.s, &both.t);
         count += p.above;
         mine = both;
     }
     PartStat row{wave_max(mine.m), 0.0f, 0.0f, 0};
     float s = 0.0f, t = 0.0f;
-    rescale(mine, row.m, two_over_tau, xsum, &s, &t);
+    rescale(mine, row.m, two_over_tau, &s, &t);
     row.s = wave_sum(s);
     row.t = wave_sum(t);
     *above = static_cast<uint64_t>(wave_sum(static_cast<uint32_t>(count >> 16))) * 65536u +
              wave_sum(static_cast<uint32_t>(count & 0xFFFFu));
+    return row;
+}
+__device__ PairStat join_parts(PairStat mine, const PairStat *stat, uint32_t parts,
+                               float two_over_tau) {
+    for (uint32_t i = (threadIdx.x & 63u) + 64; i < parts; i += 64)
+        mine = join_two(mine, stat[i], two_over_tau);
+    PairStat row{wave_max(mine.m), 0.0f, wave_max(mine.other_m), 0.0f};
+    row.s = wave_sum(rescaled(mine.s, mine.m, row.m, two_over_tau));
+    row.other_s = wave_sum(rescaled(mine.other_s, mine.other_m, row.other_m, two_over_tau));
     return row;
 }
 
@@ -466,7 +497,7 @@ __device__ void logprob_part(const LogprobArgs &g) {
     }
     if constexpr (kTop) lane_key[threadIdx.x] = ordered(lane_max);
     __syncthreads();
-    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.tau.two_over, true);
+    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.tau.two_over);
     if constexpr (kTop) {
         if (wave_of == (blockIdx.x & 3u)) {
             const uint32_t c = reached_by(lane_key, g.top);
@@ -577,7 +608,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
     const float zt = asked ? T::load(z[token]) : 0.0f;
     if (wave == 0) {
         uint64_t above;
-        const PartStat p = join_parts(mine, g.stat + first, g.parts, g.tau.two_over, true, &above);
+        const PartStat p = join_parts(mine, g.stat + first, g.parts, g.tau.two_over, &above);
         const bool broken = !(p.s >= 0.0f) || p.s == INFINITY;
         const bool empty = p.s == 0.0f;
         const float nan = __builtin_nanf("");
@@ -798,7 +829,7 @@ struct DistillArgs {
     void *grad;
     const int64_t *index;
     const float *teacher, *weight;
-    PartStat *stat;
+    PairStat *stat;
     float *loss, *stats;
     uint64_t stride, grad_stride;
     uint32_t vocab, parts, top, tail;
@@ -816,9 +847,10 @@ __device__ bool bad_entry(int64_t place, float logprob, uint32_t vocab) {
 // a bit for each value of the part in LDS (1 KB), a lane reads its vector's.
 // The second sum is kept beside the first, not taken from it by subtraction:
 // where the named places have nearly all the probability nothing would be left.
+// Where they have more than that, it is taken relative to its own maximum.
 template <class T>
 __global__ __launch_bounds__(kThreads, 8) void distill_part_kernel(DistillArgs g) {
-    __shared__ PartStat wave_stat[kWaves];
+    __shared__ PairStat wave_stat[kWaves];
     __shared__ uint32_t bits[kPart / 32];
     const uint64_t row = blockIdx.x / g.parts;
     const uint32_t part = (blockIdx.x % g.parts) * kPart;
@@ -860,26 +892,46 @@ __global__ __launch_bounds__(kThreads, 8) void distill_part_kernel(DistillArgs g
     }
     s = wave_sum(s);
     t = wave_sum(t);
-    if ((threadIdx.x & 63u) == 0) {
-        const float f = __builtin_amdgcn_exp2f(-x_of.shift(true));
-        wave_stat[threadIdx.x >> 6] = PartStat{x_of.m, s * f, t * f, 0};
+    const float f = __builtin_amdgcn_exp2f(-x_of.shift(true));
+    PairStat mine{x_of.m, s * f, x_of.m, t * f};
+    if (t < s * 0x1p-64f) {
+        // next to nothing beside the named places: from its own maximum.  The values
+        // are read again: it is rare, and the registers it would need are not
+        const auto each_other = [&](auto use) {
+#pragma unroll 1
+            for (uint32_t i = 0; i < kVecs<T>; ++i)
+#pragma unroll 1
+                for (uint32_t k = 0; k < T::kVec; ++k) {
+                    const uint32_t j = h.first(0, i) + k;
+                    if (part + j < g.vocab && !(bits[j >> 5] >> (j & 31u) & 1u))
+                        use(T::load(z[part + j]));
+                }
+        };
+        float most = kLowest, sum = 0.0f;
+        each_other([&](float v) { most = fmaxf(most, v); });
+        mine.other_m = wave_max(most);
+        each_other([&](float v) {
+            sum += __builtin_amdgcn_exp2f(scaled(v, mine.other_m, g.tau.two_over) * kLog2e);
+        });
+        mine.other_s = wave_sum(sum);
     }
+    if ((threadIdx.x & 63u) == 0) wave_stat[threadIdx.x >> 6] = mine;
     __syncthreads();
-    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.tau.two_over, false);
+    if (threadIdx.x == 0) g.stat[blockIdx.x] = join_waves(wave_stat, g.tau.two_over);
 }
 
 // One wave per row: the loss from the parts and the student's values at the
 // named places, and what the gradient needs: m, ln S (+inf: no gradient) and, with
-// the tail, the factor of q where no place is named, without it what scales the
-// teacher's probabilities exp(lt - top) / sum.  They are taken relative to the
-// largest, so that their sum to divide by is between 1 and `top` however little
-// the teacher gives the named places.
+// the tail, the maximum and the factor of the exponentials where no place is named,
+// without it what scales the teacher's probabilities exp(lt - top) / sum.  They are
+// taken relative to the largest, so that their sum to divide by is between 1 and
+// `top` however little the teacher gives the named places.
 template <class T>
 __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     const uint64_t row = blockIdx.x;
     const uint32_t lane = threadIdx.x;
     const auto *z = static_cast<const typename T::raw *>(g.logits) + row * g.stride;
-    const PartStat first = lane < g.parts ? g.stat[row * g.parts + lane] : kNoStat;
+    const PairStat first = lane < g.parts ? g.stat[row * g.parts + lane] : kNoPair;
     constexpr uint32_t kMost = DF11_MAX_TOP / 64;
     float lt[kMost], v[kMost], top = -INFINITY;
     double p[kMost], mass = 0.0;
@@ -904,9 +956,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     some = __any(some);
     bad = __any(bad);
     mass = wave_sum(mass);
-    uint64_t none;
-    const PartStat st =
-        join_parts(first, g.stat + row * g.parts, g.parts, g.tau.two_over, false, &none);
+    const PairStat st = join_parts(first, g.stat + row * g.parts, g.parts, g.tau.two_over);
     // a row's few terms in 64 bits: the loss is a difference of larger ones
     const double ln_s = log(static_cast<double>(st.s));
     const double scale = g.tail ? 1.0 : 1.0 / mass, ln_mass = g.tail ? 0.0 : top + log(mass);
@@ -917,31 +967,33 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
             sum += p[e] * scale * (lt[e] - ln_mass - (scaled64(v[e], st.m, g.tau) - ln_s));
     sum = wave_sum(sum);
     if (lane) return;
-    const double left = static_cast<double>(st.t) / st.s, r = fmax(0.0, 1.0 - mass);
+    // what is left to the others, by the teacher and (its logarithm) by the student
+    const double r = fmax(0.0, 1.0 - mass);
+    const double ln_left = scaled64(st.other_m, st.m, g.tau) + log(double{st.other_s}) - ln_s;
     const float nan = __builtin_nanf("");
-    float other = 1.0f, out_ln_s = static_cast<float>(ln_s);
-    if (g.tail && r > 0.0) {
-        sum += r * (log(r) - log(left));
-        other = left > 0.0 ? static_cast<float>(1.0 - r / left) : 0.0f;
-    }
+    float out_ln_s = static_cast<float>(ln_s);
+    if (g.tail && r > 0.0) sum += r * (log(r) - ln_left);
+    // q (1 - r/Q) of a place is exp((z - other_m) / tau) times this
+    float other = st.other_s > 0.0f ? static_cast<float>((exp(ln_left) - r) / st.other_s) : 0.0f;
     float loss = static_cast<float>(sum);
     if (st.s == 0.0f) {
         out_ln_s = INFINITY;
         loss = INFINITY;
     }
-    if (!(st.s >= 0.0f) || st.s == INFINITY) loss = out_ln_s = nan;
+    if (!(st.s >= 0.0f) || st.s == INFINITY) loss = out_ln_s = other = nan;
     if (!some || (!g.tail && mass == 0.0)) {
         loss = 0.0f;
         out_ln_s = INFINITY;
     }
-    if (bad) loss = out_ln_s = nan;
+    if (bad) loss = out_ln_s = other = nan;
     g.loss[row] = loss;
     *reinterpret_cast<float4 *>(g.stats + 4 * row) =
-        float4{st.m, out_ln_s, g.tail ? other : top, g.tail ? 0.0f : static_cast<float>(scale)};
+        float4{st.m, out_ln_s, g.tail ? st.other_m : top,
+               g.tail ? other : static_cast<float>(scale)};
 }
 
-// q times its factor everywhere, then the few named places of the part once
-// more, q minus the teacher's probability.  Their logits are read before the
+// An exponential times its factor everywhere, then the few named places of the part
+// once more, q minus the teacher's probability.  Their logits are read before the
 // first store, so that the gradient may replace the logits.
 template <class T>
 __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g) {
@@ -953,11 +1005,12 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g
     Held<T> h;
     h.load(z, part, g.vocab, g.once);
     const float4 st = *reinterpret_cast<const float4 *>(g.stats + 4 * row);
-    const float m = st.x, log2_s = st.y * kLog2e, other = g.tail ? st.z : 1.0f;
+    const float m = st.x, log2_s = st.y * kLog2e;
+    const float other_m = g.tail ? st.z : m, other_log2_s = g.tail ? 0.0f : log2_s;
     const float top = g.tail ? 0.0f : st.z, scale = g.tail ? 1.0f : st.w;
     const float w = (g.weight ? g.weight[row] : 1.0f) * (0.5f * g.tau.two_over);
     const bool none = st.y == INFINITY;
-    const float every = other * w;
+    const float every = (g.tail ? st.w : 1.0f) * w;
 
     // a thread an entry; the places of this part go to LDS, so that an entry
     // sees whether its place is named again
@@ -982,7 +1035,7 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g
     }
     __syncthreads();
     store_part(h, out, part, g.vocab, g.once, [&](float v, uint32_t) {
-        const float y = fmaf(scaled(v, m, g.tau.two_over), kLog2e, -log2_s);
+        const float y = fmaf(scaled(v, other_m, g.tau.two_over), kLog2e, -other_log2_s);
         return none ? 0.0f : __builtin_amdgcn_exp2f(y) * every;
     });
     __syncthreads();
@@ -1132,7 +1185,7 @@ int df11_distill_workspace_bytes(uint32_t dtype, uint64_t rows, uint32_t vocab, 
     static const float some = 0.0f;
     const int rc = check_logits(&some, dtype, rows, vocab, vocab);
     if (rc) return rc;
-    *bytes = sizeof(PartStat) * rows * parts_of(vocab);
+    *bytes = sizeof(PairStat) * rows * parts_of(vocab);
     return DF11_OK;
 }
 
@@ -1152,10 +1205,10 @@ int df11_distill(const void *logits, uint32_t dtype, uint64_t rows, uint32_t voc
         misaligned(loss, 4) || misaligned(stats, 16))
         return DF11_E_INVALID_ARG;
     const uint32_t parts = parts_of(vocab);
-    rc = check_workspace(workspace, workspace_bytes, sizeof(PartStat) * rows * parts);
+    rc = check_workspace(workspace, workspace_bytes, sizeof(PairStat) * rows * parts);
     if (rc) return rc;
     DistillArgs g{logits, grad, teacher_index, teacher_logprob, weight,
-                  static_cast<PartStat *>(workspace), loss, stats, row_stride, grad_stride, vocab,
+                  static_cast<PairStat *>(workspace), loss, stats, row_stride, grad_stride, vocab,
                   parts, top, tail, Tau(temperature), streams(dtype, rows, vocab)};
     DF11_BY_DTYPE(dtype, distill_part_kernel, rows * parts, kThreads, stream, g);
     if ((rc = launched())) return rc;

@@ -106,3 +106,21 @@ def test_teachers_of_little_mass_without_the_tail(level, dtype):
         index[2, 1::2] = -1
         got = check(place(z, dtype), index, logp, False, 1.0, torch.tensor([1.0, -2.0, 0.5]))
         assert torch.isfinite(got.loss).all() and torch.isfinite(got.grad).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("ahead", [30.0, 60.0, 90.0, 110.0, 300.0, 2000.0])
+def test_students_that_leave_the_others_next_to_nothing(ahead, dtype):
+    """The places that are not named have less probability than 32 bits can say:
+    all in one wave's values, in some, or everywhere behind one named place."""
+    vocab = 20011
+    for tau in (1.0, 0.5, 3.0):
+        z = student(5, vocab, 8)
+        index = torch.tensor([[3, 7000, 19000], [0, 1, 2], [8191, 8192, 16384], [5, 2050, 20010], [12, 13, 14]])
+        top = z.amax(1, keepdim=True) + ahead
+        z.scatter_(1, index.clamp(min=0), top + torch.tensor([[0.0, -1.0, -0.5]]))
+        z[3, 6:2050] = -INF                      # waves in which all the others are masked
+        z[3, 2051:20010] = -INF
+        z[4, :] -= 1e3                           # and rows far from zero
+        logp = torch.log(torch.tensor([[0.6, 0.2, 0.1]])).repeat(5, 1)
+        check(place(z, dtype, 1), index, logp, True, tau, torch.linspace(0.5, 1.5, 5))
