@@ -96,6 +96,8 @@ int df11_logprobs_backward(const void *logits, uint32_t dtype, uint64_t rows, ui
  * the gradient with respect to z times weight[r] / tau (weight null: 1).
  *   - A term with p_k = 0 (or r = 0) counts 0.  A place named more than once
  *     counts each of its entries.
+ *   - Where all places but the named ones are masked (Q = 0), an r of up to
+ *     2^-18 counts as 0: that much the logarithms' 32 bits may leave of 1.
  *   - A row whose teacher names no place, or (tail == 0) gives none of them
  *     a probability above 0, has loss 0 and gradient 0.
  *   - A student's row of masked values alone has gradient 0 (and the loss

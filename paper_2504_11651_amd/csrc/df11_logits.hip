@@ -968,7 +968,10 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     sum = wave_sum(sum);
     if (lane) return;
     // what is left to the others, by the teacher and (its logarithm) by the student
-    const double r = fmax(0.0, 1.0 - mass);
+    double r = fmax(0.0, 1.0 - mass);
+    // 32-bit logarithms, each right to 2^-21 (1 + |lt|), leave sum p (1 + |lt|) 2^-21 of 1,
+    // 2.8e-6 for 128 places: no probability where there is no place to have it
+    if (st.other_s == 0.0f && r <= 0x1p-18) r = 0.0;
     const double ln_left = scaled64(st.other_m, st.m, g.tau) + log(double{st.other_s}) - ln_s;
     const float nan = __builtin_nanf("");
     float out_ln_s = static_cast<float>(ln_s);

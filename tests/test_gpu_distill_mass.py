@@ -124,3 +124,39 @@ def test_students_that_leave_the_others_next_to_nothing(ahead, dtype):
         z[4, :] -= 1e3                           # and rows far from zero
         logp = torch.log(torch.tensor([[0.6, 0.2, 0.1]])).repeat(5, 1)
         check(place(z, dtype, 1), index, logp, True, tau, torch.linspace(0.5, 1.5, 5))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("live", [1, 2, 10, 19])
+def test_a_grammar_leaves_fewer_places_than_the_teacher_may_name(live, dtype):
+    """The teacher's alternatives of a masked row are all there is: what its 32-bit
+    values leave of 1 is no probability, for the row itself or for a student's."""
+    rows, vocab = 64, 9001
+    g = torch.Generator().manual_seed(live)
+    mask = torch.full((rows, vocab), -INF)
+    for r in range(rows):
+        mask[r, torch.randperm(vocab, generator=g)[:live]] = 0.0
+    z = student(rows, vocab, 6) * 2
+    for tau in (1.0, 0.7):
+        t = place(z + mask, dtype)
+        teacher = ops.logprobs(t, top=20, temperature=tau)
+        same = ops.distill(t, teacher.top_index, teacher.top_logprob, temperature=tau,
+                           weight=torch.ones(rows, device="cuda"))
+        # p = q up to what 32 bits hold: ln p and ln q agree to about |x| U
+        x = (z.amax(1) - z.amin(1)).max() / tau
+        assert same.loss.abs().max() <= (x + 16) * 2 * U and same.grad.abs().max() <= (x + 16) * 2 * U / tau
+        t = place(student(rows, vocab, 7) + mask, dtype)
+        got = check(t, teacher.top_index.cpu(), teacher.top_logprob.cpu(), True, tau)
+        assert torch.isfinite(got.loss).all()
+
+
+@pytest.mark.parametrize("short", [2.0 ** -10, 2.0 ** -16])
+def test_probability_that_meets_no_place_is_infinite(short):
+    """More than rounding is missing from the named places: the formula's loss."""
+    z = torch.full((2, 5000), -INF)
+    z[:, 100:110] = 1.0
+    index = torch.arange(100, 110).repeat(2, 1)
+    logp = torch.full((2, 10), math.log((1 - short) / 10))
+    got = ops.distill(place(z, torch.float32), index.cuda(), logp.cuda(), weight=torch.ones(2, device="cuda"))
+    assert (got.loss == INF).all() and torch.isfinite(got.grad).all()
+    assert (got.grad[:, :100] == 0).all() and (got.grad[:, 110:] == 0).all()
