@@ -46,7 +46,7 @@ extern "C" {
  *   top_logprob, top_index (rows x top): the `top` largest, largest first,
  *                  equal ones by ascending index;
  *   stats          rows x 4 floats for the backward pass: m, ln S, the
- *                  entropy, logprob.
+ *                  entropy, 1/S.
  * tokens may be null (then logprob and rank must be); each output may be
  * null, top_logprob and top_index with top = 0 only.
  *   - A masked value (-inf) has probability 0.  Where fewer than `top`

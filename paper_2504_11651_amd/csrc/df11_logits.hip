@@ -36,6 +36,7 @@
 // distillation end too many launches early (656 against 600 us at 192 MB).
 #include "df11_ops_common.h"
 
+#include <algorithm>
 #include <limits>
 
 namespace {
@@ -56,6 +57,7 @@ struct Tau {
     float two_over;  // 2/tau: differences of halves are multiplied by it
     float c, rest;   // log2e/tau in two parts: one would be off by |x| 2^-25 in x, the
                      // same way in every value, and so in the sum
+    float two_c, two_rest;  // the same for differences of halves
     double over;     // 1/tau
     explicit Tau(float tau) : two_over(2.0f / tau), over(1.0 / tau) {
         // the first part from below, so that the second is positive and a masked
@@ -65,12 +67,20 @@ struct Tau {
         rest = static_cast<float>(M_LOG2E / tau - c);
         // not 0 where that is below the float range (tau of 10^37 and more): 0 * -inf
         if (rest == 0.0f) rest = std::numeric_limits<float>::denorm_min();
+        two_c = std::min(2.0f * c, std::numeric_limits<float>::max());  // not 0 * inf
+        two_rest = 2.0f * rest;
     }
 };
 
 // (v - m) / tau, of halves so that the difference of two finite values is finite
 __device__ float scaled(float v, float m, float two_over_tau) {
     return fmaf(v, 0.5f, -0.5f * m) * two_over_tau;
+}
+
+// (v - m) log2e / tau, to 2^-23 of itself and no worse however large m is
+__device__ float exponent(float v, float m, const Tau &tau) {
+    const float d = fmaf(v, 0.5f, -0.5f * m);
+    return fmaf(d, tau.two_rest, d * tau.two_c);
 }
 
 // Bits in the order of the values: unsigned comparison.  -0 is +0.
@@ -625,7 +635,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
             if (g.entropy) g.entropy[row] = h;
             if (g.stats)
                 *reinterpret_cast<float4 *>(g.stats + 4 * row) =
-                    float4{p.m, static_cast<float>(ln_s), h, lp};
+                    float4{p.m, static_cast<float>(ln_s), h, broken ? nan : 1.0f / p.s};
             row_m = p.m;
             row_ln_s = ln_s;
             row_s = broken ? -1.0f : p.s;
@@ -796,7 +806,8 @@ __device__ void store_part(const Held<T> &h, typename T::raw *out, uint32_t part
     }
 }
 
-// grad = p (A + B y), y = log2 p: the formula with its factors drawn together.
+// grad = p (A + B x), p = exp2(x) / S: the formula with its factors drawn together.
+// S comes as 1/S: of ln S, which is about 10, 32 bits leave 5e-7 of every p.
 // The token's value, the only other one, is written by the lane that holds it.
 template <class T>
 __global__ __launch_bounds__(kThreads, 8) void logprob_grad_kernel(LogprobGradArgs g) {
@@ -813,12 +824,13 @@ __global__ __launch_bounds__(kThreads, 8) void logprob_grad_kernel(LogprobGradAr
     if (token >= static_cast<int64_t>(g.vocab)) gl = __builtin_nanf("");
     const float ge = g.grad_entropy ? g.grad_entropy[row] : 0.0f;
     const bool empty = ln_s == -INFINITY;
-    const float A = -over_tau * fmaf(ge, entropy, gl), B = -over_tau * ge * kLn2;
-    const float hit = over_tau * gl, log2_s = ln_s * kLog2e;
+    const float over = over_tau * st.w;
+    const float A = -over * fmaf(ge, entropy - ln_s, gl), B = -over * ge * kLn2;
+    const float hit = over_tau * gl;
     const uint32_t tok = token >= 0 && token < g.vocab ? static_cast<uint32_t>(token) : ~0u;
     store_part(h, out, part, g.vocab, g.once, [&](float v, uint32_t j) {
-        const float y = fmaf(scaled(v, m, g.tau.two_over), kLog2e, -log2_s);
-        const float d = __builtin_amdgcn_exp2f(y) * fmaf(B, fmaxf(y, -300.0f), A);
+        const float x = exponent(v, m, g.tau);
+        const float d = __builtin_amdgcn_exp2f(x) * fmaf(B, fmaxf(x, -300.0f), A);
         return empty ? 0.0f : j == tok ? d + hit : d;
     });
 }
@@ -921,7 +933,7 @@ __global__ __launch_bounds__(kThreads, 8) void distill_part_kernel(DistillArgs g
 }
 
 // One wave per row: the loss from the parts and the student's values at the
-// named places, and what the gradient needs: m, ln S (+inf: no gradient) and, with
+// named places, and what the gradient needs: m, 1/S (0: no gradient) and, with
 // the tail, the maximum and the factor of the exponentials where no place is named,
 // without it what scales the teacher's probabilities exp(lt - top) / sum.  They are
 // taken relative to the largest, so that their sum to divide by is between 1 and
@@ -974,24 +986,23 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillArgs g) {
     if (st.other_s == 0.0f && r <= 0x1p-18) r = 0.0;
     const double ln_left = scaled64(st.other_m, st.m, g.tau) + log(double{st.other_s}) - ln_s;
     const float nan = __builtin_nanf("");
-    float out_ln_s = static_cast<float>(ln_s);
+    float over_s = 1.0f / st.s;
     if (g.tail && r > 0.0) sum += r * (log(r) - ln_left);
     // q (1 - r/Q) of a place is exp((z - other_m) / tau) times this
     float other = st.other_s > 0.0f ? static_cast<float>((exp(ln_left) - r) / st.other_s) : 0.0f;
     float loss = static_cast<float>(sum);
     if (st.s == 0.0f) {
-        out_ln_s = INFINITY;
+        over_s = 0.0f;
         loss = INFINITY;
     }
-    if (!(st.s >= 0.0f) || st.s == INFINITY) loss = out_ln_s = other = nan;
+    if (!(st.s >= 0.0f) || st.s == INFINITY) loss = over_s = other = nan;
     if (!some || (!g.tail && mass == 0.0)) {
-        loss = 0.0f;
-        out_ln_s = INFINITY;
+        loss = over_s = 0.0f;
     }
-    if (bad) loss = out_ln_s = other = nan;
+    if (bad) loss = over_s = other = nan;
     g.loss[row] = loss;
     *reinterpret_cast<float4 *>(g.stats + 4 * row) =
-        float4{st.m, out_ln_s, g.tail ? st.other_m : top,
+        float4{st.m, over_s, g.tail ? st.other_m : top,
                g.tail ? other : static_cast<float>(scale)};
 }
 
@@ -1008,12 +1019,11 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g
     Held<T> h;
     h.load(z, part, g.vocab, g.once);
     const float4 st = *reinterpret_cast<const float4 *>(g.stats + 4 * row);
-    const float m = st.x, log2_s = st.y * kLog2e;
-    const float other_m = g.tail ? st.z : m, other_log2_s = g.tail ? 0.0f : log2_s;
+    const float m = st.x, over_s = st.y, other_m = g.tail ? st.z : m;
     const float top = g.tail ? 0.0f : st.z, scale = g.tail ? 1.0f : st.w;
     const float w = (g.weight ? g.weight[row] : 1.0f) * (0.5f * g.tau.two_over);
-    const bool none = st.y == INFINITY;
-    const float every = (g.tail ? st.w : 1.0f) * w;
+    const bool none = over_s == 0.0f;
+    const float every = (g.tail ? st.w : over_s) * w;
 
     // a thread an entry; the places of this part go to LDS, so that an entry
     // sees whether its place is named again
@@ -1038,13 +1048,13 @@ __global__ __launch_bounds__(kThreads, 8) void distill_grad_kernel(DistillArgs g
     }
     __syncthreads();
     store_part(h, out, part, g.vocab, g.once, [&](float v, uint32_t) {
-        const float y = fmaf(scaled(v, other_m, g.tau.two_over), kLog2e, -other_log2_s);
-        return none ? 0.0f : __builtin_amdgcn_exp2f(y) * every;
+        const float x = exponent(v, other_m, g.tau);
+        return none ? 0.0f : __builtin_amdgcn_exp2f(x) * every;
     });
     __syncthreads();
     if (mine && !none) {
-        const float y = fmaf(scaled(value, m, g.tau.two_over), kLog2e, -log2_s);
-        out[at] = T::store((__builtin_amdgcn_exp2f(y) - target * scale) * w);
+        const float q = __builtin_amdgcn_exp2f(exponent(value, m, g.tau)) * over_s;
+        out[at] = T::store((q - target * scale) * w);
     }
 }
 
