@@ -290,8 +290,8 @@ __device__ void wave_lds_sync() {
 }
 
 // kSteps products of 32 ranks a term; 0: up to 16 ranks, where one product holds two
-// terms.  A BF16 out takes two terms (2^-16 of the adapter's part, where out itself
-// is rounded to 2^-9), an fp32 one all three.
+// terms.  A BF16 out takes all three too: where base and the adapter's part cancel,
+// its own rounding hides nothing.
 template <class T, uint32_t kSteps, uint32_t kTiles>
 __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
     constexpr uint32_t kFrags = kSteps ? kSteps : 1, kCols = 64, kRow = kCols + 4;
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
                                                  : zero4();
                         }
                 }
-                constexpr uint32_t kUse = T::kVec == 4 ? 3 : 2, kProducts = kSteps ? kUse : 2;
+                constexpr uint32_t kProducts = kSteps ? kTerms : 2;
                 uint4 t[kProducts][kFrags];
 #pragma unroll
                 for (uint32_t k = 0; k < kFrags; ++k)
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
                         const uint32_t r = kSteps ? 32 * k + 8 * q : 8 * (q & 1u);
                         // up to 16 ranks lane groups 2 and 3 hold the next term
                         const uint32_t term = kSteps ? i : 2 * i + q / 2;
-                        const bool in = r < g.rank && (mine >> c & 1u) && term < kUse;
+                        const bool in = r < g.rank && (mine >> c & 1u) && term < kTerms;
                         t[i][k] = in ? *reinterpret_cast<const uint4 *>(
                                            g.terms + (term * g.tokens + t0 + c) * g.rank + r)
                                      : zero4();
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(kThreads) void lora_expand_kernel(ExpandArgs g) {
 #pragma unroll
                     for (uint32_t k = 0; k < kFrags; ++k)
 #pragma unroll
-                        for (uint32_t i = 0; i < (kSteps || kUse > 2 ? kProducts : 1); ++i)
+                        for (uint32_t i = 0; i < kProducts; ++i)
                             acc = mfma(w[f][k], t[i][k], acc);
                     *reinterpret_cast<f32x4 *>(mytile + c * kRow + 16 * f + 4 * q) = acc;
                 }
