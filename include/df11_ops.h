@@ -141,7 +141,8 @@ int df11_distill_backward(const void *logits, uint32_t dtype, uint64_t rows, uin
  * rank a multiple of 8, 8 <= rank <= DF11_MAX_RANK; cols a multiple of 64 and
  * rows of 16 (as df11_matrix); tokens <= 2^24; rows of every tensor 16-byte
  * aligned (strides: multiples of 8 BF16 or 4 floats).  tokens = 0 launches
- * nothing.
+ * nothing.  DF11_E_UNSUPPORTED for more than 2^24 - 1 pieces of 64 tokens times
+ * pieces of 256 of the rows, or of the cols (2^38 values).
  *
  * Backward, for the gradient dy of out (tokens x rows, DF11_F32 or DF11_BF16),
  * with u[t] = scale[i] * B_i^T dy[t] and v[t] = A_i x[t]:

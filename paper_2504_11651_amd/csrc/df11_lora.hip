@@ -50,6 +50,7 @@ constexpr uint32_t kThreads = 256;
 constexpr uint32_t kWaves = kThreads / 64;
 constexpr uint32_t kTile = 16;        // tokens of a matrix product
 constexpr uint32_t kFewTokens = 256;  // up to these, a workgroup an adapter of a tile
+constexpr uint32_t kManyTiles = 4;    // tiles that a workgroup of `expand` takes above them
 constexpr uint32_t kFewValues = 1024; // tokens x rank up to which `expand` takes single tokens
 
 __device__ f32x4 mfma(const uint4 &a, const uint4 &b, f32x4 c) {
@@ -790,7 +791,10 @@ int check_shapes(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank,
     if (cols % 64 || rows % 16 || rank % 8 || rank > DF11_MAX_RANK || tokens > (1ull << 24) ||
         n_adapters > 65535u || cols > (1u << 23) || rows > (1u << 23))
         return DF11_E_UNSUPPORTED;
-    return DF11_OK;
+    // `expand` over out or dx: a launch holds 2^32 threads
+    const uint64_t blocks = (std::max(rows, cols) + 255) / 256;
+    const uint64_t groups = (tokens + kTile * kManyTiles - 1) / (kTile * kManyTiles);
+    return groups * blocks > 0xFFFFFFFFull / kThreads ? DF11_E_UNSUPPORTED : DF11_OK;
 }
 
 int check_rows(const void *p, uint64_t stride, uint32_t len, uint64_t tokens, uint32_t bytes) {
@@ -892,7 +896,6 @@ template <class T, uint32_t kTiles>
 int launch_expand(ExpandArgs e, hipStream_t stream) {
     e.blocks = (e.len + 255) / 256;
     const uint64_t wgs = (e.tokens + kTile * kTiles - 1) / (kTile * kTiles) * e.blocks;
-    if (wgs > 0xFFFFFFFFull / kThreads) return DF11_E_UNSUPPORTED;
     const dim3 grid(wgs, 1,
                     kTiles == 1 ? std::min<uint64_t>({16, e.n_adapters + 1ull, e.tokens}) : 1);
     const dim3 block(kThreads);
@@ -911,8 +914,8 @@ int launch_expand(const ExpandArgs &e, uint32_t dtype, hipStream_t stream) {
     if (e.tokens <= kFewTokens)
         return dtype == DF11_F32 ? launch_expand<F32, 1>(e, stream)
                                  : launch_expand<BF16, 1>(e, stream);
-    return dtype == DF11_F32 ? launch_expand<F32, 4>(e, stream)
-                             : launch_expand<BF16, 4>(e, stream);
+    return dtype == DF11_F32 ? launch_expand<F32, kManyTiles>(e, stream)
+                             : launch_expand<BF16, kManyTiles>(e, stream);
 }
 
 template <class T>
