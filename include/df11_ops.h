@@ -150,7 +150,8 @@ int df11_distill_backward(const void *logits, uint32_t dtype, uint64_t rows, uin
  *   da[i] = sum_{t of i} u[t] x[t]^T     n_adapters x rank x cols floats;
  *   db[i] = sum_{t of i} scale[i] dy[t] v[t]^T   n_adapters x rows x rank floats;
  * an adapter without tokens gets zeros.  dx, or da and db together, may be
- * null. */
+ * null; with da and db, dx must not be x or dy, which are read after it is
+ * written. */
 int df11_lora_workspace_bytes(uint64_t tokens, uint32_t cols, uint32_t rows, uint32_t rank,
                               uint32_t n_adapters, uint64_t *bytes);
 int df11_lora(const uint16_t *x, uint64_t x_stride, uint64_t tokens, uint32_t cols, uint32_t rows,

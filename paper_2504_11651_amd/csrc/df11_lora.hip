@@ -1063,6 +1063,8 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
     if (!rc && dx_base && dx_base == dx && tokens > 1 && dx_base_stride != dx_stride)
         rc = DF11_E_INVALID_ARG;
     if (!rc) rc = check_workspace(workspace, workspace_bytes, need);
+    // dA and dB are made of x and dy after dx is written
+    if (!rc && da && dx && (dx == x || dx == dy)) rc = DF11_E_INVALID_ARG;
     if (rc) return rc;
 
     const Space s = space_of(tokens, cols, rows, rank, n_adapters);

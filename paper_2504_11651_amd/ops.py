@@ -348,7 +348,7 @@ def lora_backward(x, a, b, scale, adapter, dy, dx_base=None, dx=None, da=None, d
     or bfloat16, (tokens, rows)): dx (bfloat16, added to ``dx_base`` where that
     is given; it may be ``dx_base`` itself), da and db (float32).  ``dx``,
     ``da``, ``db``: tensors to fill; ``need_dx`` or ``need_ab`` False leaves
-    out dx, or da and db."""
+    out dx, or da and db.  With da and db, ``dx`` must not be x or dy."""
     device, x_stride, shapes = _adapters(x, a, b, scale, adapter)
     tokens, cols, rows, rank, n = shapes
     dy_stride = _rows(dy, _Y, device, "dy", (tokens, rows))

@@ -20,3 +20,9 @@ def test_more_products_than_a_grid_holds(tokens, rows):
         with pytest.raises(ops.codec.DF11Error):
             ops.lora_backward_workspace_bytes(*sizes)
     assert ops.lora_workspace_bytes(tokens, 128, 64, 8, 2) > 0
+
+
+@pytest.mark.parametrize("change", [dict(x=3 * A), dict(dy=3 * A), dict(x=3 * A, dx_base=3 * A)])
+def test_dx_in_place_of_what_the_adapters_gradients_still_read(change):
+    """da and db are made of x and dy after dx is written."""
+    assert lora_backward(dx=3 * A, **change) == INVALID
