@@ -7,9 +7,11 @@ gradients of all three.
 Argument marshalling only, as in ``codec``: every value is computed by the
 library's HIP kernels, on ``stream`` (default: torch's current stream), and a
 call returns without waiting.  Outputs and workspaces that are not given are
-allocated by torch; a workspace holds nothing between calls, so calls that
-overlap in time need one each.  ValueError for tensors that do not fit each
-other, ``codec.DF11Error`` for what the library refuses.
+allocated by torch, in ``stream``'s memory; tensors that are given are the
+caller's to keep, and to have ready on ``stream``.  A workspace holds nothing
+between calls, so calls that overlap in time need one each.  ValueError for
+tensors that do not fit each other, ``codec.DF11Error`` for what the library
+refuses.
 """
 from __future__ import annotations
 
@@ -119,6 +121,22 @@ def _gpu(t, what):
     return t.device
 
 
+def _new(shape, dtype, device, stream):
+    """A tensor that the kernels on ``stream`` write: of that stream's memory, so
+    that nothing the current stream still does with memory it gave back meets
+    them, nor they what it allocates when the tensor is dropped early."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    here = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if stream.cuda_stream != here.cuda_stream:
+        t.record_stream(here)  # which reads it later, and may when it is dropped
+    return t
+
+
 @functools.lru_cache(maxsize=1024)
 def _bytes(size, *sizes):
     """What the library's size function says for these sizes."""
@@ -135,16 +153,7 @@ def _workspace(given, size, sizes, device, stream):
             raise ValueError("workspace must be contiguous")
         return given, given.numel() * given.element_size()
     n = _bytes(size, *sizes)
-    if n == 0:
-        return None, 0
-    ws = torch.empty(n, dtype=torch.uint8, device=device)
-    if stream is not None:
-        # the kernels run on `stream`: the caching allocator must not hand this
-        # memory out again before that stream has finished with it
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream), device=device)
-        ws.record_stream(stream)
-    return ws, n
+    return (_new((n,), torch.uint8, device, stream), n) if n else (None, 0)
 
 
 def _handle(stream, device):
@@ -171,11 +180,12 @@ def logprobs(logits, tokens=None, top: int = 0, temperature: float = 1.0, out=No
     rows, vocab = logits.shape
     _want(tokens, (rows,), torch.int64, device, "tokens")
     if out is None:
-        def new(shape, dtype=torch.float32):
-            return torch.empty(shape, dtype=dtype, device=device)
+        def new(*shape, dtype=torch.float32):
+            return _new(shape, dtype, device, stream)
         asked = tokens is not None
-        out = Logprobs(new(rows) if asked else None, new(rows, torch.int64) if asked else None,
-                       new(rows), new((rows, top)), new((rows, top), torch.int64), new((rows, 4)))
+        out = Logprobs(new(rows) if asked else None,
+                       new(rows, dtype=torch.int64) if asked else None, new(rows), new(rows, top),
+                       new(rows, top, dtype=torch.int64), new(rows, 4))
     else:
         out = Logprobs(*out)
         _want(out.logprob, (rows,), torch.float32, device, "out.logprob")
@@ -209,7 +219,7 @@ def logprobs_backward(logits, tokens, stats, grad_logprob=None, grad_entropy=Non
     _want(grad_logprob, (rows,), torch.float32, device, "grad_logprob")
     _want(grad_entropy, (rows,), torch.float32, device, "grad_entropy")
     if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=device)
+        out = _new((rows, vocab), logits.dtype, device, stream)
     grad_stride = _rows(out, (logits.dtype,), device, "out", logits.shape)
     codec._check(lib().df11_logprobs_backward(
         logits.data_ptr(), DTYPES[logits.dtype], rows, vocab, stride, _ptr(tokens),
@@ -251,10 +261,10 @@ def distill(logits, teacher_index, teacher_logprob, tail: bool = True, temperatu
     _want(loss, (rows,), torch.float32, device, "loss")
     _want(stats, (rows, 4), torch.float32, device, "stats")
     if weight is not None and grad is None:
-        grad = torch.empty((rows, vocab), dtype=logits.dtype, device=device)
+        grad = _new((rows, vocab), logits.dtype, device, stream)
     grad_stride = 0 if grad is None else _rows(grad, (logits.dtype,), device, "grad", logits.shape)
-    loss = torch.empty(rows, dtype=torch.float32, device=device) if loss is None else loss
-    stats = torch.empty((rows, 4), dtype=torch.float32, device=device) if stats is None else stats
+    loss = _new((rows,), torch.float32, device, stream) if loss is None else loss
+    stats = _new((rows, 4), torch.float32, device, stream) if stats is None else stats
     dt = DTYPES[logits.dtype]
     ws, ws_bytes = _workspace(workspace, "df11_distill_workspace_bytes", (dt, rows, vocab), device,
                               stream)
@@ -278,7 +288,7 @@ def distill_backward(logits, teacher_index, teacher_logprob, stats, grad_loss=No
     _want(stats, (rows, 4), torch.float32, device, "stats")
     _want(grad_loss, (rows,), torch.float32, device, "grad_loss")
     if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=device)
+        out = _new((rows, vocab), logits.dtype, device, stream)
     grad_stride = _rows(out, (logits.dtype,), device, "out", logits.shape)
     codec._check(lib().df11_distill_backward(
         logits.data_ptr(), DTYPES[logits.dtype], rows, vocab, stride, teacher_index.data_ptr(),
@@ -325,7 +335,7 @@ def lora(x, a, b, scale, adapter, base=None, out=None, workspace=None, stream=No
     device, x_stride, shapes = _adapters(x, a, b, scale, adapter)
     shape = (shapes[0], shapes[2])
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32 if base is None else base.dtype, device=device)
+        out = _new(shape, torch.float32 if base is None else base.dtype, device, stream)
     out_stride = _rows(out, _Y, device, "out", shape)
     base_stride = 0 if base is None else _rows(base, (out.dtype,), device, "base", shape)
     ws, ws_bytes = _workspace(workspace, "df11_lora_workspace_bytes", shapes, device, stream)
@@ -357,15 +367,15 @@ def lora_backward(x, a, b, scale, adapter, dy, dx_base=None, dx=None, da=None, d
         dx = dx_base = None
     else:
         if dx is None:
-            dx = torch.empty((tokens, cols), dtype=torch.bfloat16, device=device)
+            dx = _new((tokens, cols), torch.bfloat16, device, stream)
         dx_stride = _rows(dx, _BF16, device, "dx", x.shape)
         if dx_base is not None:
             dxb_stride = _rows(dx_base, _BF16, device, "dx_base", x.shape)
     if not need_ab:
         da = db = None
     else:
-        da = torch.empty((n, rank, cols), dtype=torch.float32, device=device) if da is None else da
-        db = torch.empty((n, rows, rank), dtype=torch.float32, device=device) if db is None else db
+        da = _new((n, rank, cols), torch.float32, device, stream) if da is None else da
+        db = _new((n, rows, rank), torch.float32, device, stream) if db is None else db
         _want(da, (n, rank, cols), torch.float32, device, "da")
         _want(db, (n, rows, rank), torch.float32, device, "db")
     ws, ws_bytes = _workspace(workspace, "df11_lora_backward_workspace_bytes", shapes, device,
