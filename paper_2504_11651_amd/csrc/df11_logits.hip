@@ -273,10 +273,17 @@ __device__ PairStat join_two(const PairStat &a, const PairStat &b, float two_ove
     return p;
 }
 __device__ PairStat join_waves(const PairStat *w, float two_over_tau) {
-    return join_two(join_two(w[0], w[1], two_over_tau), join_two(w[2], w[3], two_over_tau),
-                    two_over_tau);
+    PairStat p{w[0].m, 0.0f, w[0].other_m, 0.0f};
+    for (uint32_t i = 1; i < kWaves; ++i) {
+        p.m = fmaxf(p.m, w[i].m);
+        p.other_m = fmaxf(p.other_m, w[i].other_m);
+    }
+    for (uint32_t i = 0; i < kWaves; ++i) {
+        p.s += rescaled(w[i].s, w[i].m, p.m, two_over_tau);
+        p.other_s += rescaled(w[i].other_s, w[i].other_m, p.other_m, two_over_tau);
+    }
+    return p;
 }
-static_assert(kWaves == 4, "two pairs of waves");
 
 constexpr PartStat kNoStat{kLowest, 0.0f, 0.0f, 0};
 constexpr PairStat kNoPair{kLowest, 0.0f, kLowest, 0.0f};
