@@ -138,6 +138,8 @@ int df11_distill_backward(const void *logits, uint32_t dtype, uint64_t rows, uin
  * Any order of adapters is right; tokens of one adapter side by side share
  * its loads.  The low-rank intermediate (and an fp32 dy below) meets the matrix
  * cores as three BF16 terms, which hold all its bits, whatever the type of out.
+ * (An infinity in an operand that meets such terms may come out as a NaN: a
+ * term can be 0.  It stays with the tokens, rows or adapters it belongs to.)
  * rank a multiple of 8, 8 <= rank <= DF11_MAX_RANK; cols a multiple of 64 and
  * rows of 16 (as df11_matrix); tokens <= 2^24; rows of every tensor 16-byte
  * aligned (strides: multiples of 8 BF16 or 4 floats).  tokens = 0 launches

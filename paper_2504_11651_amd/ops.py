@@ -12,6 +12,11 @@ caller's to keep, and to have ready on ``stream``.  A workspace holds nothing
 between calls, so calls that overlap in time need one each.  ValueError for
 tensors that do not fit each other, ``codec.DF11Error`` for what the library
 refuses.
+
+The calls know nothing of autograd: results are detached also where an input
+requires a gradient, and a tensor that is filled or replaced is written
+without its version being counted.  A program that differentiates through them
+calls the ``_backward`` functions from its own ``torch.autograd.Function``.
 """
 from __future__ import annotations
 
