@@ -144,3 +144,38 @@ def test_a_lost_term_would_show():
         for t in range(40):
             less = b[adapter[t]] @ (cut[adapter[t]] @ x[t])
             assert adapter[t] < 0 or (less != add[t]).all()
+
+
+@gpu
+@pytest.mark.parametrize("tokens, rank", [(5, 8), (50, 40), (300, 16), (5000, 64)])
+def test_infinite_weights_stay_with_their_adapter(tokens, rank):
+    """An infinity or a NaN in one adapter's A or B, in a row of B that others' rows of
+    the same tile pass by, reaches its own tokens, and of these its own row, alone."""
+    n, cols, rows = 3, 128, 256
+    g = torch.Generator().manual_seed(tokens)
+    x = torch.randn((tokens, cols), generator=g).bfloat16().cuda()
+    a = torch.randn((n, rank, cols), generator=g).bfloat16().cuda()
+    b = torch.randn((n, rows, rank), generator=g).bfloat16().cuda()
+    dy = torch.randn((tokens, rows), generator=g).cuda()
+    adapter = (torch.arange(tokens) % (n + 1) - 1).int().cuda()
+    own, others = adapter == 1, adapter != 1
+    for dtype in DTYPES:
+        base = dy.to(dtype)
+        out = ops.lora(x, a, b, None, adapter, base=base)
+        back = ops.lora_backward(x, a, b, None, adapter, base)
+        for value in (float("inf"), float("nan")):
+            bad = b.clone()
+            bad[1, 77, 3] = value
+            got = ops.lora(x, a, bad, None, adapter, base=base)
+            row = torch.arange(rows, device="cuda") == 77
+            assert torch.equal(got[others], out[others]) and torch.equal(got[own][:, ~row], out[own][:, ~row])
+            assert not torch.isfinite(got[own][:, row]).any()
+            bad = a.clone()
+            bad[1, 2, 5] = value
+            assert torch.equal(ops.lora(x, bad, b, None, adapter, base=base)[others], out[others])
+            got = ops.lora_backward(x, bad, b, None, adapter, base)
+            col = torch.arange(cols, device="cuda") == 5
+            assert torch.equal(got.dx[others], back.dx[others])
+            assert torch.equal(got.dx[own][:, ~col], back.dx[own][:, ~col])
+            for i in (0, 2):
+                assert torch.equal(got.da[i], back.da[i]) and torch.equal(got.db[i], back.db[i])
