@@ -27,7 +27,7 @@
 //   64 alternatives    parts 270 us, join 41 us: instruction issue, about 19
 //                      vector instructions a value, a third of them for the
 //                      alternatives (the threshold, and the values above it);
-//   distillation       parts 199 us (5.3 TB/s), join 11, gradient 345 us (6.1
+//   distillation       parts 202 us (5.2 TB/s), join 11, gradient 346 us (6.1
 //                      TB/s, reads and writes past the caches): memory;
 //   one row, fp32, 20  parts 6.6 us, join 6.9: loads and barriers after one another.
 // Holding two parts, with the next one's loads under way while one is worked on,

@@ -27,11 +27,12 @@
 //   1 token, 4096 -> 4096, rank 16: shrink 3.4 us, expand 3.0: loads after one another;
 //   64 tokens of 32 adapters, 4096 -> 14336, fp32: 5.5 and 6.7 (22 MB of adapters, base
 //     and out): the same, and the adapters' rows from the L2 cache;
-//   6001 tokens, 4096 -> 14336, bf16: shrink 19.7, prepare 4.7, expand 70 (344 MB: 4.9
-//     TB/s): memory;
+//   6001 tokens, 4096 -> 14336, bf16: shrink 19.7, prepare 4.8, expand 73 (344 MB: 4.7
+//     TB/s; 70 with two of the three terms): memory;
 //   gradients, 8192 tokens, 4096 x 4096, rank 64: transpose 5, shrink 62, prepare 8,
-//     expand 44, outer 60, join 13 for 67 MB each of dy, x, dx_base and dx: the loads of
-//     A, B and of the terms, which at this rank are as many as those of the tokens;
+//     expand 51 (44 with two terms), outer 61, join 13 for 67 MB each of dy, x, dx_base
+//     and dx: the loads of A, B and of the terms, which at this rank are as many as those
+//     of the tokens;
 //   of an LM head of 128,256 rows, 1024 tokens, fp32 dy (525 MB): shrink 111, outer 104:
 //     memory (4.8 and 5.1 TB/s), dy is read twice.
 #include "df11_ops_common.h"

@@ -11,7 +11,7 @@ allocated by torch, in ``stream``'s memory; tensors that are given are the
 caller's to keep, and to have ready on ``stream``.  A workspace holds nothing
 between calls, so calls that overlap in time need one each.  ValueError for
 tensors that do not fit each other, ``codec.DF11Error`` for what the library
-refuses.
+refuses.  As for ``codec``'s calls, the tensors' GPU is to be the current one.
 
 The calls know nothing of autograd: results are detached also where an input
 requires a gradient, and a tensor that is filled or replaced is written
