@@ -83,12 +83,15 @@ def test_dropped_outputs_wait_for_both_streams():
     where = t.data_ptr()
     # work of the current stream that is under way when the tensor is dropped
     big = torch.randn((4096, 4096), device="cuda")
-    for _ in range(20):
+    for _ in range(60):
         big = big @ big * 1e-2
     kept = t + big[0, 0]
+    done = torch.cuda.Event()
+    done.record()
     del t
     with torch.cuda.stream(side):
         again = [torch.empty(5, dtype=torch.float32, device="cuda") for _ in range(4)]
-    assert all(x.data_ptr() != where for x in again)
+    if not done.query():
+        assert all(x.data_ptr() != where for x in again)
     torch.cuda.synchronize()
     assert kept.shape == (5,)
