@@ -3,8 +3,6 @@ that S is the number of unmasked places, and only the last few operations round.
 
 Tolerance: 1/S, the row's factor, 1/tau, their products and the last one are rounded
 once each: 6 * 2^-24 of the value, and 2^-126 where values are that small."""
-import math
-
 import pytest
 import torch
 
