@@ -4,7 +4,10 @@
  *     the adapters' and the activations' gradients;
  *   - log probabilities of given tokens with their rank, the entropy and the
  *     top alternatives, with the logits' gradient;
- *   - distillation from a teacher's top log probabilities, loss and gradient.
+ *   - distillation from a teacher's top log probabilities, loss and gradient;
+ *   - a paged cache of keys and values: appending to it with the position
+ *     rotation, and attention of a batch to a prefix that it shares and to
+ *     each sequence's own tokens.
  *
  * The conventions are those of df11.h: the caller owns every buffer, device
  * pointers except where a size is returned, work is enqueued on `stream` and
@@ -32,6 +35,8 @@ extern "C" {
 
 #define DF11_MAX_TOP 128  /* alternatives of a row */
 #define DF11_MAX_RANK 128 /* of an adapter */
+#define DF11_MIN_PAGE 16  /* tokens of a cache's page, a power of two */
+#define DF11_MAX_PAGE 1024
 
 /* ---- Log probabilities of given tokens.
  *
@@ -170,6 +175,104 @@ int df11_lora_backward(const uint16_t *x, uint64_t x_stride, uint64_t tokens, ui
                        const uint16_t *dx_base, uint64_t dx_base_stride, uint16_t *dx,
                        uint64_t dx_stride, float *da, float *db, void *workspace,
                        uint64_t workspace_bytes, hipStream_t stream);
+
+/* ---- A paged cache of keys and values.
+ *
+ * df11_kv_cache: `pages` pages of page_size tokens for each of `heads` heads of
+ * `dim` values, k and v alike: token i of page p and head h is the dim values at
+ * k + p * k_stride + (h * page_size + i) * dim (elements; v with v_stride).
+ *   dtype      DF11_BF16 or DF11_F16;
+ *   page_size  a power of two, DF11_MIN_PAGE .. DF11_MAX_PAGE;
+ *   dim        64 or 128;  heads * page_size * dim < 2^31;
+ *   k_stride, v_stride  at least heads * page_size * dim, multiples of 8; k and v
+ *              16-byte aligned.  (Layers side by side, or k and v, are strides.)
+ *
+ * df11_kv_batch: the batch's sequences, in device memory but for the sizes, so
+ * that a captured call follows the values:
+ *   start      sequences + 1 row numbers, ascending from 0: sequence s has rows
+ *              start[s] .. start[s + 1] - 1 of the call's tensors, its last tokens
+ *              in their order (none, one, or a prompt's).  Rows from
+ *              start[sequences] on belong to no sequence: they are not read, and
+ *              what a call writes is left as it was there;
+ *   length     per sequence, the tokens of its own cache with this call's rows:
+ *              row r has the place length[s] - (start[s + 1] - r) in it;
+ *   table      sequences x width page numbers, row s at table + s * table_stride:
+ *              place i of sequence s is token i % page_size of page
+ *              table[s][i / page_size].  Entries that no place needs are not looked at;
+ *   prefix_table, prefix_pages, prefix_len   the pages of the prefix that all
+ *              sequences share, and its tokens (0: none).  A row's position is
+ *              prefix_len + its place.
+ * What the library reads in device memory leads to no access out of range: see
+ * each call for page numbers outside the cache.  Two rows that share a page and a
+ * token of it write over one another in any order.
+ *
+ * df11_kv_append: for each row r of a sequence, with place i >= 0 and position p,
+ *   q_out[r] = R_p q[r],  cache.k <- R_p k[r],  cache.v <- v[r]   (at place i)
+ * where R_p turns, in every head, pair j of `rotary` values by the angle
+ * p * inv_freq[j] (a, b -> a cos - b sin, b cos + a sin).  Pair j is values j and
+ * j + rotary / 2, or 2 j and 2 j + 1 where `interleaved`; values from rotary on
+ * stay.  The angle is a product of 64 bits, taken to a turn's fraction before it is
+ * rounded: as exact at the far end of a long context as at its beginning.
+ *   q, k, v    rows of `dtype` (DF11_F32, as df11_block_gemm gives its products,
+ *              DF11_BF16 or DF11_F16), heads * dim values in q, cache.heads * dim
+ *              in k and v, strides in elements, rows 16-byte aligned;
+ *   inv_freq   rotary / 2 floats (rotary = 0: no rotation, inv_freq may be null);
+ *   rotary     a multiple of 16, at most dim;
+ *   q_out      tokens x heads * dim of the cache's type; it may be q itself where
+ *              the types are the same (with its stride).
+ * A row whose place is negative, lies past the table's width or on a page outside
+ * the cache is not appended; its q_out is written as any other's.  Of the batch's
+ * prefix only prefix_len is looked at (prefix_table may be null).  tokens <= 2^24 - 1
+ * (DF11_E_UNSUPPORTED for 2^24). */
+typedef struct {
+    void *k, *v;
+    uint32_t dtype, pages, heads, page_size, dim;
+    uint64_t k_stride, v_stride;
+} df11_kv_cache;
+
+typedef struct {
+    const int32_t *start, *length, *table;
+    uint32_t sequences, width;
+    uint64_t table_stride;
+    const int32_t *prefix_table;
+    uint32_t prefix_pages, prefix_len;
+} df11_kv_batch;
+
+int df11_kv_append(const void *q, uint64_t q_stride, const void *k, uint64_t k_stride,
+                   const void *v, uint64_t v_stride, uint32_t dtype, uint64_t tokens,
+                   uint32_t heads, const float *inv_freq, uint32_t rotary, uint32_t interleaved,
+                   const df11_kv_cache *cache, const df11_kv_batch *batch, void *q_out,
+                   uint64_t q_out_stride, hipStream_t stream);
+
+/* ---- Attention to a shared prefix and to each sequence's own tokens.
+ *
+ * For each row r of a sequence and each of `heads` query heads h, head
+ * h / (heads / cache.heads) of the cache, over the prefix_len tokens of the prefix
+ * and the sequence's places up to the row's own:
+ *   s_j = scale q . k_j,  lse = ln sum_j exp s_j,  out = sum_j exp(s_j - lse) v_j.
+ *   q, out     tokens x heads * dim of the cache's type, strides in elements, rows
+ *              16-byte aligned; out may be q itself (with its stride);
+ *   lse        tokens x heads floats, may be null;
+ *   heads      a multiple of cache.heads; tokens * heads < 2^31; scale > 0.
+ * The rows of all sequences read the prefix together, once.  Products are summed in
+ * 32 bits on the matrix cores, the softmax is held in 32 bits; exp(s_j - m) is
+ * rounded to the cache's type where it meets v.
+ *   - A row that sees nothing (no prefix and a negative place), or scores of -inf
+ *     alone: out 0, lse -inf.
+ *   - What lies behind a row's place (in pages, or later rows' keys and values) has
+ *     no effect on it, NaN and infinities included.
+ *   - A row that sees a place past the table's width or a page outside the cache has
+ *     no result: out and lse NaN.
+ * tokens = 0 launches nothing.  DF11_E_UNSUPPORTED for more workgroups than a launch
+ * holds: (tokens * heads / 128 + sequences * cache.heads) or tokens * heads / 4 of 2^24,
+ * the latter where the workspace has a size. */
+int df11_prefix_attention_workspace_bytes(uint64_t tokens, uint32_t heads,
+                                          const df11_kv_cache *cache, const df11_kv_batch *batch,
+                                          uint64_t *bytes);
+int df11_prefix_attention(const void *q, uint64_t q_stride, uint64_t tokens, uint32_t heads,
+                          float scale, const df11_kv_cache *cache, const df11_kv_batch *batch,
+                          void *out, uint64_t out_stride, float *lse, void *workspace,
+                          uint64_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

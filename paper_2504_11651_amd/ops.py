@@ -2,7 +2,9 @@
 C ABI declared in include/df11_ops.h): low-rank adapters beside a shared
 projection, log probabilities of given tokens with rank, entropy and top
 alternatives, distillation from a teacher's top log probabilities, and the
-gradients of all three.
+gradients of all three; and, between a block's products, a paged cache of keys
+and values, appended to with the position rotation and read by attention to a
+prefix that the batch shares and to each sequence's own tokens.
 
 Argument marshalling only, as in ``codec``: every value is computed by the
 library's HIP kernels, on ``stream`` (default: torch's current stream), and a
@@ -33,14 +35,29 @@ EXPORTS = (
     "df11_logprobs_workspace_bytes", "df11_logprobs", "df11_logprobs_backward",
     "df11_distill_workspace_bytes", "df11_distill", "df11_distill_backward",
     "df11_lora_workspace_bytes", "df11_lora", "df11_lora_backward_workspace_bytes",
-    "df11_lora_backward",
+    "df11_lora_backward", "df11_kv_append", "df11_prefix_attention_workspace_bytes",
+    "df11_prefix_attention",
 )
 
 MAX_TOP = 128   # DF11_MAX_TOP
 MAX_RANK = 128  # DF11_MAX_RANK
+MIN_PAGE, MAX_PAGE = 16, 1024  # DF11_MIN_PAGE, DF11_MAX_PAGE
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 _lib = None
+
+
+class _Cache(ctypes.Structure):  # df11_kv_cache
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v")] + [
+        (n, ctypes.c_uint32) for n in ("dtype", "pages", "heads", "page_size", "dim")] + [
+        (n, ctypes.c_uint64) for n in ("k_stride", "v_stride")]
+
+
+class _Batch(ctypes.Structure):  # df11_kv_batch
+    _fields_ = [(n, ctypes.c_void_p) for n in ("start", "length", "table")] + [
+        ("sequences", ctypes.c_uint32), ("width", ctypes.c_uint32),
+        ("table_stride", ctypes.c_uint64), ("prefix_table", ctypes.c_void_p),
+        ("prefix_pages", ctypes.c_uint32), ("prefix_len", ctypes.c_uint32)]
 
 
 def lib():
@@ -64,6 +81,13 @@ def lib():
             "df11_lora": [*adapters, vp, u64, vp, u64, u32, vp, u64, vp],
             "df11_lora_backward_workspace_bytes": [*shapes, size],
             "df11_lora_backward": [*adapters, vp, u64, u32, vp, u64, vp, u64, vp, vp, vp, u64, vp],
+        }
+        cache, batch = ctypes.POINTER(_Cache), ctypes.POINTER(_Batch)
+        sig |= {
+            "df11_kv_append": [vp, u64, vp, u64, vp, u64, u32, u64, u32, vp, u32, u32, cache, batch,
+                               vp, u64, vp],
+            "df11_prefix_attention_workspace_bytes": [u64, u32, cache, batch, size],
+            "df11_prefix_attention": [vp, u64, u64, u32, f32, cache, batch, vp, u64, vp, vp, u64, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -94,6 +118,28 @@ class LoraGrads(NamedTuple):
     dx: Optional[torch.Tensor]  # bfloat16 (tokens, cols)
     da: Optional[torch.Tensor]  # float32 (adapters, rank, cols)
     db: Optional[torch.Tensor]  # float32 (adapters, rows, rank)
+
+
+class KVCache(NamedTuple):
+    """A paged cache: page p holds page_size tokens of every head.  Any stride
+    between pages (layers or k and v side by side), each page contiguous."""
+    k: torch.Tensor  # bfloat16 or float16 (pages, kv_heads, page_size, head_dim)
+    v: torch.Tensor  # as k
+
+
+class KVBatch(NamedTuple):
+    """The sequences that a call works on, and where their tokens lie."""
+    start: torch.Tensor   # int32 (sequences + 1,): first row of each, ascending from 0, and the end
+    length: torch.Tensor  # int32 (sequences,): own tokens of each, the call's rows (its last) included
+    table: torch.Tensor   # int32 (sequences, width): pages of each sequence's own tokens
+    prefix_table: Optional[torch.Tensor] = None  # int32 (n,): pages of the shared prefix
+    prefix_len: int = 0                          # its tokens
+
+
+class Attention(NamedTuple):
+    """What ``prefix_attention`` gives."""
+    out: torch.Tensor            # as q
+    lse: Optional[torch.Tensor]  # float32 (tokens, heads), None where none was asked for
 
 
 def _ptr(t):
@@ -391,3 +437,136 @@ def lora_backward(x, a, b, scale, adapter, dy, dx_base=None, dx=None, da=None, d
         _ptr(dx), dx_stride, _ptr(da), _ptr(db), _ptr(ws), ws_bytes,
         _handle(stream, device)), "df11_lora_backward")
     return LoraGrads(dx, da, db)
+
+
+# ------------------------------------------------- a paged cache of keys and values
+def _kv_cache(cache, device):
+    """df11_kv_cache of a KVCache on this GPU."""
+    k, v = cache
+    if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("cache.k must be (pages, kv_heads, page_size, head_dim), bfloat16 or "
+                         f"float16, not {k.dtype} {tuple(k.shape)}")
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError(f"cache.v must be as cache.k: {k.dtype} {tuple(k.shape)}, not {v.dtype} "
+                         f"{tuple(v.shape)}")
+    pages, heads, page, dim = k.shape
+    for t, what in ((k, "cache.k"), (v, "cache.v")):
+        if t.device != device:
+            raise ValueError(f"{what} must be on {device}, not {t.device}")
+        if t.stride()[1:] != (page * dim, dim, 1) and pages and not t[0].is_contiguous():
+            raise ValueError(f"each page of {what} must be contiguous")
+    return _Cache(k.data_ptr(), v.data_ptr(), DTYPES[k.dtype], pages, heads, page, dim,
+                  k.stride(0), v.stride(0))
+
+
+def _kv_batch(batch, device):
+    """df11_kv_batch of a KVBatch on this GPU."""
+    start, length, table, prefix_table, prefix_len = batch
+    n = length.shape[0] if length.dim() == 1 else -1
+    _want(length, (n,), torch.int32, device, "batch.length")
+    _want(start, (n + 1,), torch.int32, device, "batch.start")
+    stride = _rows(table, (torch.int32,), device, "batch.table")
+    if table.shape[0] != n:
+        raise ValueError(f"batch.table must have a row for each of {n} sequences")
+    pages = 0
+    if prefix_table is not None:
+        pages = prefix_table.numel()
+        _want(prefix_table, (pages,), torch.int32, device, "batch.prefix_table")
+    if not 0 <= prefix_len < 2 ** 31:
+        raise ValueError(f"batch.prefix_len must be from 0 to 2^31 - 1, not {prefix_len}")
+    return _Batch(start.data_ptr(), length.data_ptr(), table.data_ptr(), n, table.shape[1], stride,
+                  _ptr(prefix_table), pages, prefix_len)
+
+
+def _heads(t, dim, what):
+    """Heads of `dim` values in the rows of a 2-d tensor."""
+    heads, rest = divmod(t.shape[1], dim)
+    if rest or not heads:
+        raise ValueError(f"{what}'s rows must be heads of {dim} values, not {t.shape[1]}")
+    return heads
+
+
+def kv_append(q, k, v, inv_freq, cache: KVCache, batch: KVBatch, interleaved: bool = False,
+              q_out=None, stream=None):
+    """Rotates the rows of q and k by their positions and appends k and v to the
+    cache; returns q_out, the rotated q of the cache's type.
+
+    q: (tokens, heads * head_dim), k and v: (tokens, kv_heads * head_dim), float32
+    as ``codec.block_gemm`` gives its products, bfloat16 or float16, rows
+    contiguous.  A row's position is batch.prefix_len + its place among its
+    sequence's own tokens; pair j of a head turns by position * inv_freq[j]
+    (float32, half as many as values that turn; None: none do).  Pairs are j and
+    j + len(inv_freq), or neighbours where ``interleaved``.  ``q_out`` may be q
+    itself where the types are the same.  Rows behind the last sequence's are left
+    as they are in q_out; a row without a place in its sequence's pages, or whose
+    page is not one of the cache, is not appended.  Two rows must not share a
+    token of a page."""
+    device = _gpu(q, "q")
+    c, b = _kv_cache(cache, device), _kv_batch(batch, device)
+    tokens = q.shape[0]
+    q_stride = _rows(q, DTYPES, device, "q")
+    heads = _heads(q, c.dim, "q")
+    shape = (tokens, c.heads * c.dim)
+    k_stride = _rows(k, (q.dtype,), device, "k", shape)
+    v_stride = _rows(v, (q.dtype,), device, "v", shape)
+    rotary = 0
+    if inv_freq is not None:
+        rotary = 2 * inv_freq.numel()
+        _want(inv_freq, (rotary // 2,), torch.float32, device, "inv_freq")
+    if q_out is None:
+        q_out = _new(q.shape, cache.k.dtype, device, stream)
+    out_stride = _rows(q_out, (cache.k.dtype,), device, "q_out", q.shape)
+    codec._check(lib().df11_kv_append(
+        q.data_ptr(), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, DTYPES[q.dtype],
+        tokens, heads, _ptr(inv_freq), rotary, bool(interleaved), c, b, q_out.data_ptr(),
+        out_stride, _handle(stream, device)), "df11_kv_append")
+    return q_out
+
+
+def _attention_bytes(tokens, heads, c, b):
+    n = ctypes.c_uint64()
+    codec._check(lib().df11_prefix_attention_workspace_bytes(tokens, heads, c, b, ctypes.byref(n)),
+                 "df11_prefix_attention_workspace_bytes")
+    return int(n.value)
+
+
+def prefix_attention_workspace_bytes(tokens: int, heads: int, cache: KVCache,
+                                     batch: KVBatch) -> int:
+    """For this many rows of q; of cache and batch only the sizes count."""
+    device = cache.k.device
+    return _attention_bytes(tokens, heads, _kv_cache(cache, device), _kv_batch(batch, device))
+
+
+def prefix_attention(q, cache: KVCache, batch: KVBatch, scale: Optional[float] = None, out=None,
+                     lse=None, need_lse: bool = False, workspace=None, stream=None) -> Attention:
+    """Attention of q's rows (tokens, heads * head_dim, the cache's type, rows
+    contiguous, as ``kv_append`` gives them) to the prefix that the batch's
+    sequences share and to their own sequence's tokens up to themselves, which the
+    cache already holds: the prefix is read once for all rows.  Consecutive
+    heads / kv_heads query heads share a head of the cache.
+
+    scale: of the products q k before the softmax (None: head_dim ** -0.5).
+    ``out`` may be q itself; ``lse`` (float32 (tokens, heads), given or with
+    ``need_lse`` new) is the log of the sum of the exponentials.  Rows behind the
+    last sequence's are left as they are in both.  A row that sees nothing has out
+    0 and lse -inf; one that sees a page which is not of the cache has NaN."""
+    device = _gpu(q, "q")
+    c, b = _kv_cache(cache, device), _kv_batch(batch, device)
+    q_stride = _rows(q, (cache.k.dtype,), device, "q")
+    heads, tokens = _heads(q, c.dim, "q"), q.shape[0]
+    if out is None:
+        out = _new(q.shape, q.dtype, device, stream)
+    out_stride = _rows(out, (q.dtype,), device, "out", q.shape)
+    if lse is None and need_lse:
+        lse = _new((tokens, heads), torch.float32, device, stream)
+    _want(lse, (tokens, heads), torch.float32, device, "lse")
+    if workspace is None:
+        ws_bytes = _attention_bytes(tokens, heads, c, b)
+        workspace = _new((ws_bytes,), torch.uint8, device, stream) if ws_bytes else None
+    else:
+        workspace, ws_bytes = _workspace(workspace, None, None, device, stream)
+    codec._check(lib().df11_prefix_attention(
+        q.data_ptr(), q_stride, tokens, heads, c.dim ** -0.5 if scale is None else scale, c, b,
+        out.data_ptr(), out_stride, _ptr(lse), _ptr(workspace), ws_bytes,
+        _handle(stream, device)), "df11_prefix_attention")
+    return Attention(out, lse)

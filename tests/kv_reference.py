@@ -1,0 +1,135 @@
+"""What the tests of the paged cache share: caches whose unused places hold NaN, and
+the operators' definitions in 64 bits."""
+import math
+
+import torch
+
+from paper_2504_11651_amd import ops
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def half_step(t):
+    return torch.finfo(t).eps / 2
+
+
+class Case:
+    """Sequences with `new` rows of `own` tokens each behind a prefix; `spare` rows
+    behind the last.  Pages are in random order, entries and places that nothing needs
+    hold what must not be looked at."""
+
+    def __init__(self, new, own, prefix=0, heads=8, kv_heads=2, dim=128, page=64, dtype=BF16, seed=0,
+                 spare=0, width=None, device="cuda", filled=True):
+        self.new, self.own, self.prefix = list(new), list(own), prefix
+        self.heads, self.kv_heads, self.dim, self.page, self.dtype = heads, kv_heads, dim, page, dtype
+        self.group, self.tokens, self.device = heads // kv_heads, sum(new) + spare, device
+        self.g = torch.Generator(device=device).manual_seed(seed)
+        n = len(self.new)
+        used = [max(0, -(-x // page)) for x in self.own]
+        front = -(-prefix // page)
+        total = sum(used) + front + 3
+        order = torch.randperm(total, generator=self.g, device=device).int()
+        width = max([1, *used]) if width is None else width
+        self.table = torch.full((n, width), -7, dtype=torch.int32, device=device)
+        at = front
+        self.pages = []
+        for i, u in enumerate(used):
+            self.pages.append(order[at:at + u].long())
+            self.table[i, :min(u, width)] = order[at:at + min(u, width)]
+            at += u
+        self.prefix_table = order[:front].contiguous()
+        self.start = torch.tensor([0, *torch.tensor(self.new, dtype=torch.int64).cumsum(0).tolist()], dtype=torch.int32,
+                                  device=device)
+        self.length = torch.tensor(self.own, dtype=torch.int32, device=device)
+        self.k, self.v = (torch.full((total, kv_heads, page, dim), math.nan, dtype=dtype, device=device)
+                          for _ in range(2))
+        # what every sequence sees, as it stands in the pages
+        self.sets = []
+        for pages, count in [(self.prefix_table.long(), prefix), *zip(self.pages, self.own)]:
+            count = max(count, 0)
+            kv = []
+            for cache, size in ((self.k, 0.5), (self.v, 1.0)):
+                x = (size * self.normal(count, kv_heads, dim)).to(dtype)
+                if filled and count:
+                    i = torch.arange(count, device=device)
+                    cache[pages[i // page], :, i % page] = x
+                kv.append(x)
+            self.sets.append(kv)
+        self.q = self.normal(self.tokens, heads * dim).to(dtype)
+
+    def normal(self, *shape):
+        return torch.randn(shape, generator=self.g, device=self.device)
+
+    @property
+    def cache(self):
+        return ops.KVCache(self.k, self.v)
+
+    @property
+    def batch(self):
+        return ops.KVBatch(self.start, self.length, self.table, self.prefix_table if self.prefix else None, self.prefix)
+
+    def expected(self, scale=None, q=None):
+        """out, lse in 64 bits and how far a result may be off: {name: (want, tolerance)}
+        for the rows of sequences.
+
+        A score's products are exact and summed in 32 bits: dim 2^-24 sum |q k| at most
+        (any order), its multiple by scale log2 e and the exponential add 2^-22 of the
+        score and 2^-22.  A p is off by half a step of its type (a half float below 2^-14
+        by 2^-25, of a sum that is at least 1), sums over n tokens by n 2^-24, and the
+        result by half a step once more."""
+        scale = self.dim ** -0.5 if scale is None else scale
+        q = (self.q if q is None else q).double().view(self.tokens, self.kv_heads, self.group, self.dim)
+        u = half_step(self.dtype)
+        outs, lses, out_tol, lse_tol = [], [], [], []
+        for b, (n, own) in enumerate(zip(self.new, self.own)):
+            if not n:
+                continue
+            k, v = (torch.cat((self.sets[0][i], self.sets[b + 1][i])).double().transpose(0, 1) for i in (0, 1))
+            lo = sum(self.new[:b])
+            x = q[lo:lo + n].permute(1, 2, 0, 3)  # kv heads, group, n, dim
+            ends = torch.arange(own - n, own, device=self.device).clamp(min=-1) + self.prefix + 1
+            hidden = torch.arange(k.shape[1], device=self.device) >= ends[:, None]
+            s = (x.flatten(1, 2) @ k.transpose(1, 2).contiguous()).view(*x.shape[:3], -1) * scale
+            size = (x.abs().flatten(1, 2) @ k.abs().transpose(1, 2).contiguous()).view(s.shape) * scale
+            off = torch.where(hidden, 0.0, size * self.dim * 2 ** -24 + s.abs() * 2 ** -22 + 2 ** -22)
+            off = off.amax(-1) if k.shape[1] else s.new_zeros(s.shape[:3])
+            s.masked_fill_(hidden, -math.inf)
+            lse = torch.logsumexp(s, -1) if k.shape[1] else s.new_full(s.shape[:3], -math.inf)
+            p = torch.where(hidden, 0.0, (s - torch.where(lse.isfinite(), lse, 0.0)[..., None]).exp())
+            v = torch.where(v.isfinite(), v, 0.0)[:, None]
+            out, weight = p @ v, p @ v.abs()
+            count = k.shape[1]
+            tol = weight * (u + 3 * off[..., None] + 2 * count * 2 ** -24) + out.abs() * u
+            if self.dtype == F16:
+                tol = tol + 2 ** -24 + count * 2 ** -25 * v.abs().amax(-2, keepdim=True) / p.amax(
+                    -1, keepdim=True).clamp(min=1e-30) * p.amax(-1, keepdim=True) if count else tol
+            outs.append(out.permute(2, 0, 1, 3).reshape(n, -1))
+            out_tol.append(tol.expand_as(out).permute(2, 0, 1, 3).reshape(n, -1))
+            lses.append(lse.permute(2, 0, 1).reshape(n, -1))
+            lse_tol.append((off + count * 2 ** -24 + lse.nan_to_num(0, 0, 0).abs() * 2 ** -22).permute(
+                2, 0, 1).reshape(n, -1))
+        return {"out": (torch.cat(outs), torch.cat(out_tol) + 1e-30),
+                "lse": (torch.cat(lses), torch.cat(lse_tol) + 1e-30)}
+
+    def attend(self, **more):
+        """Result of the operator, into tensors whose spare rows must stay as they are."""
+        out = torch.full_like(self.q, 77.0)
+        lse = torch.full((self.tokens, self.heads), 77.0, device=self.device)
+        return ops.prefix_attention(self.q, self.cache, self.batch, out=out, lse=lse, **more)
+
+    def check(self, got=None, **more):
+        got = self.attend(**more) if got is None else got
+        rows = sum(self.new)
+        for name, (want, tol) in self.expected(more.get("scale")).items():
+            near(getattr(got, name)[:rows], want, tol, name)
+            assert (getattr(got, name)[rows:] == 77.0).all(), f"{name}: rows behind the last were written"
+        return got
+
+
+def near(got, want, tol, what=""):
+    got = got.double()
+    same = (got == want) | (got.isnan() & want.isnan())
+    bad = ~same & ~((got - want).abs() <= tol)
+    worst = ((got - want).abs() / tol)[bad]
+    assert not bad.any(), (f"{what}: {int(bad.sum())} of {bad.numel()} off, first at {bad.nonzero()[0].tolist()}: "
+                           f"{got[bad][0]} for {want[bad][0]}, up to {worst.max()} tolerances")
