@@ -29,6 +29,7 @@ using namespace df11ops;
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kTile = 64;   // tokens of a tile
 constexpr uint32_t kRows = 128;  // rows of a tile: 32 a wave
+constexpr uint32_t kMaxParts = 256;  // of the prefix, and of a sequence's own tokens
 // How far c s may rise above m before O is taken down: p stays below 2^8, far from
 // the largest fp16, and what is summed in 32 bits loses nothing.
 constexpr float kSlack = 8.0f;
@@ -70,23 +71,48 @@ struct AttendArgs {
     Batch batch;
     float c;  // scale log2 e
     uint32_t pages, page_shift, heads, kv_heads, group;
-    // the prefix: row tiles, parts and their tokens, workgroups; none if it is read
-    // with a sequence's own tokens
-    uint32_t front_tiles, front_parts, front_step, front_grid;
-    // the own tokens: tile numbers, most parts, groups of tiles that share an XCD
-    uint32_t own_tiles, own_parts, own_groups;
-    uint32_t whole;  // a workgroup reads the prefix and all own tokens of its rows
+    uint32_t own_tiles, own_groups;  // `whole`: tile numbers; groups of them that share an XCD
+    // `shares`: tiles of rows and of tokens of the prefix, most parts of a row's prefix and
+    // of its own tokens, and for the join the share's size, the tiles of all sequences'
+    // own tokens, and those in front of every sequence
+    uint32_t row_tiles, front_tiles, front_parts, own_parts;
+    uint32_t *sums;
 };
 
-// Parts that a sequence's `length` own tokens are cut into, and their tokens: at
-// least four tiles each, and no more parts than there is room for.
-struct Cut {
-    uint32_t parts, step;
+// Tokens that a table row has pages for: what lies beyond is not read, and rows that
+// see it have no result.
+__device__ inline uint32_t room(const Batch &b, uint32_t page_shift) {
+    return min(uint64_t{b.width} << page_shift, uint64_t{INT32_MAX});
+}
+// A sequence's rows, in tiles of kRows, and the tokens of its own that they see.
+struct Sequence {
+    uint32_t from, to;  // rows of the call
+    int32_t before;     // a row r sees before + r
+    __device__ uint32_t tiles(const AttendArgs &a) const {
+        return to > from ? ((to - from) * a.group + kRows - 1) / kRows : 0;
+    }
+    __device__ uint32_t first_row(const AttendArgs &a, uint32_t i) const {
+        return from * a.group + i * kRows;
+    }
+    __device__ uint32_t rows(const AttendArgs &a, uint32_t i) const {
+        return min(kRows, to * a.group - first_row(a, i));
+    }
+    // what the first and the last row of a tile see
+    __device__ int32_t least(const AttendArgs &a, uint32_t i) const {
+        return before + static_cast<int32_t>(first_row(a, i) / a.group);
+    }
+    __device__ uint32_t end(const AttendArgs &a, uint32_t i) const {
+        const uint32_t last = first_row(a, i) + rows(a, i) - 1;
+        return min(static_cast<uint32_t>(max(before + static_cast<int32_t>(last / a.group), 0)),
+                   room(a.batch, a.page_shift));
+    }
+    __device__ uint32_t token_tiles(const AttendArgs &a, uint32_t i) const {
+        return (end(a, i) + kTile - 1) / kTile;
+    }
 };
-__device__ inline Cut cut(uint32_t length, uint32_t most) {
-    const uint32_t tiles = (length + kTile - 1) / kTile;
-    const uint32_t step = max(4u, (tiles + most - 1) / most);
-    return {(tiles + step - 1) / step, step * kTile};
+__device__ inline Sequence sequence(const Batch &b, uint32_t s) {
+    const uint32_t to = b.first(s + 1);
+    return {b.first(s), to, max(b.length[s], 0) - static_cast<int32_t>(to) + 1};
 }
 
 __device__ inline uint32_t swizzle64(uint32_t t) { return 2 * ((t >> 1) & 3) | ((t >> 3) & 1); }
@@ -113,10 +139,11 @@ struct Places {
     static constexpr uint32_t kSteps = D / 16;   // of K Q^T
     static constexpr uint32_t kBlocks = D / 32;  // of O
     uint32_t k[kSteps], v[kBlocks][2];
-    __device__ Places(uint32_t lane) {
+    // `first`: of the tile's tokens that the wave looks at
+    __device__ Places(uint32_t lane, uint32_t first) {
         const uint32_t half = lane >> 5, t = lane & 31;
         for (uint32_t s = 0; s < kSteps; s++)
-            k[s] = t * kRowBytes + (((2 * s + half) ^ swizzle<D>(t & 15)) << 4);
+            k[s] = (first + t) * kRowBytes + (((2 * s + half) ^ swizzle<D>(t & 15)) << 4);
         // groups of 16 lanes read 4 tokens x 16 values: lane i the 8 bytes i % 4 of token i / 4
         const uint32_t i = lane & 15, tok = 4 * half + (i >> 2);
 #pragma unroll
@@ -124,7 +151,7 @@ struct Places {
 #pragma unroll
             for (uint32_t e = 0; e < 2; e++) {
                 const uint32_t piece = 4 * b + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-                v[b][e] = (tok + 8 * e) * kRowBytes + ((piece ^ swizzle<D>(tok + 8 * e)) << 4) +
+                v[b][e] = (first + tok + 8 * e) * kRowBytes + ((piece ^ swizzle<D>(tok + 8 * e)) << 4) +
                           (i & 1) * 8;
             }
     }
@@ -144,10 +171,10 @@ struct Worker {
     uint32_t from[kLoads];  // a lane's bytes from its 16 tokens' first
     s8 q[P::kSteps];
     acc16 o[P::kBlocks];
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, base = 0.0f, l = 0.0f;  // base: m where it is a number
 
-    __device__ Worker(const AttendArgs &args, uint32_t kvh_)
-        : a(args), at(threadIdx.x & 63), lane(threadIdx.x & 63),
+    __device__ Worker(const AttendArgs &args, uint32_t kvh_, bool split)
+        : a(args), at(threadIdx.x & 63, split ? threadIdx.x >> 1 & 32 : 0), lane(threadIdx.x & 63),
           wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), kvh(kvh_) {
         head_off = (uint64_t{kvh} * D) << a.page_shift;
 #pragma unroll
@@ -162,20 +189,18 @@ struct Worker {
             for (uint32_t e = 0; e < 16; e++) x[e] = 0.0f;
     }
 
+    // The page numbers of a tile's tokens, asked for a tile ahead of its loads: lanes
+    // 4 i + j have that of tokens 16 j.. (16 tokens lie on one page, also at the end).
+    __device__ uint32_t pages(const Range &r, uint32_t tile) const {
+        const uint32_t at = min(tile + 16 * (lane & 3), r.end - 1) >> a.page_shift;
+        return at < r.width ? static_cast<uint32_t>(r.table[at]) : ~0u;
+    }
     // Loads this wave's 16 tokens of a tile into LDS, past the registers.  True: the
     // tile's tokens lie on pages of the cache; where they do not, those of another page
     // are loaded in their place.
-    __device__ bool load(const Range &r, uint32_t tile, uint8_t *k, uint8_t *v) const {
-        uint32_t page = 0;
-        bool fine = true;
-        // (16 tokens lie on one page, and 64 do from that page size on)
-        for (uint32_t i = 0; i < (a.page_shift >= 6 ? 1u : 4u); i++) {
-            const uint32_t at = min(tile + 16 * i, r.end - 1) >> a.page_shift;
-            uint32_t p = ~0u;
-            if (at < r.width) p = __builtin_amdgcn_readfirstlane(r.table[at]);
-            fine = fine && p < a.pages;
-            if (i == wave || a.page_shift >= 6) page = p;
-        }
+    __device__ bool load(const Range &r, uint32_t tile, uint32_t numbers, uint8_t *k,
+                         uint8_t *v) const {
+        uint32_t page = __builtin_amdgcn_readlane(numbers, wave);
         if (page >= a.pages) page = 0;
         const uint32_t t = min(tile + 16 * wave, (r.end - 1) & ~15u);  // behind: of no effect
         const uint64_t in = (uint64_t{t & ((1u << a.page_shift) - 1)} * D + head_off) * 2;
@@ -190,18 +215,20 @@ struct Worker {
             __builtin_amdgcn_global_load_lds((mem_void *)(vp + from[i]), (lds_void *)(v + i * 1024),
                                              16, 0, 0);
         }
-        return fine;
+        return !__any(numbers >= a.pages);
     }
     // Waits for them, and clears the values of tokens behind the range: they meet a
     // p of 0, and what memory holds there may be an infinity.
     __device__ void landed(const Range &r, uint32_t tile, uint8_t *v) const {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (tile + kTile <= r.end) return;
+        if (__builtin_expect(tile + kTile <= r.end, 1)) return;
+        uint32_t mine = lane;
+        asm volatile("" : "+v"(mine));  // nothing of this rare loop is kept in registers
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; i++) {
             constexpr uint32_t kLanes = 64 / kEach;
-            if (tile + 16 * wave + i * kEach + lane / kLanes >= r.end)
-                *reinterpret_cast<uint4 *>(v + 16 * wave * P::kRowBytes + i * 1024 + lane * 16) =
+            if (tile + 16 * wave + i * kEach + mine / kLanes >= r.end)
+                *reinterpret_cast<uint4 *>(v + 16 * wave * P::kRowBytes + i * 1024 + mine * 16) =
                     uint4{0, 0, 0, 0};
         }
     }
@@ -212,45 +239,35 @@ struct Worker {
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     }
 
-    // Tokens 32 kFirst .. 32 (kFirst + kCount) of a tile.  `end`: the tokens that the
-    // lane's row sees, from the tile's first; `masked`: not all rows see all.
+    // Scores of tokens `first` .. first + 32 kCount of a tile.
     template <uint32_t kCount>
-    __device__ void tokens(const uint8_t *k, const uint8_t *v, uint32_t first, bool masked,
-                           int32_t end, bool lost, bool uneven) {
-        k += first * P::kRowBytes;
-        v += first * P::kRowBytes;
-        acc16 s[kCount];
+    __device__ void scores(const uint8_t *k, acc16 (&s)[kCount]) const {
 #pragma unroll
-        for (uint32_t b = 0; b < kCount; b++) {
+        for (uint32_t b = 0; b < kCount; b++)
 #pragma unroll
             for (uint32_t e = 0; e < 16; e++) s[b][e] = 0.0f;
 #pragma unroll
-            for (uint32_t i = 0; i < P::kSteps; i++)
-                s[b] = Mat<C>::product(
-                    *reinterpret_cast<const s8 *>(k + at.k[i] + b * 32 * P::kRowBytes), q[i], s[b]);
-        }
-        if (lost)  // a page outside the cache
-#pragma unroll
-            for (auto &x : s)
-#pragma unroll
-                for (uint32_t e = 0; e < 16; e++) x[e] = NAN;
-        const int32_t seen = end - static_cast<int32_t>(first + 4 * (lane >> 5));
-        if (masked)
+        for (uint32_t i = 0; i < P::kSteps; i++)
 #pragma unroll
             for (uint32_t b = 0; b < kCount; b++)
-#pragma unroll
-                for (uint32_t e = 0; e < 16; e++)
-                    if (static_cast<int32_t>(32 * b + 8 * (e / 4) + e % 4) >= seen)
-                        s[b][e] = -INFINITY;
+                s[b] = Mat<C>::product(
+                    *reinterpret_cast<const s8 *>(k + at.k[i] + b * 32 * P::kRowBytes), q[i], s[b]);
+    }
+    // The softmax' step: p of them, in the order in which they meet the values.
+    template <uint32_t kCount>
+    __device__ void weigh(const acc16 (&s)[kCount], s8 (&p)[2 * kCount]) {
         float top = s[0][0];
 #pragma unroll
         for (uint32_t b = 0; b < kCount; b++)
 #pragma unroll
             for (uint32_t e = 0; e < 16; e++) top = fmaxf(top, s[b][e]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * a.c;
-        if (__any(top > m + kSlack)) {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top),
+                                                           __float_as_uint(top), false, false);
+        top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.c;
+        if (__builtin_expect(__any(top > m + kSlack), 0)) {
             const float rise = fmaxf(m, top);
-            const float down = __builtin_amdgcn_exp2f(m - (rise == -INFINITY ? 0.0f : rise));
+            base = rise == -INFINITY ? 0.0f : rise;
+            const float down = __builtin_amdgcn_exp2f(m - base);
             m = rise;
             l *= down;
 #pragma unroll
@@ -258,8 +275,6 @@ struct Worker {
 #pragma unroll
                 for (uint32_t e = 0; e < 16; e++) x[e] *= down;
         }
-        const float base = m == -INFINITY ? 0.0f : m;
-        s8 p[2 * kCount];
 #pragma unroll
         for (uint32_t b = 0; b < kCount; b++)
 #pragma unroll
@@ -268,22 +283,45 @@ struct Worker {
                 l += x;
                 p[2 * b + e / 8][e % 8] = static_cast<short>(C::store(x));
             }
-        if (uneven) {
-            // rows see different tokens: a value that is an infinity or a NaN must not
-            // meet the p of 0 of a row that does not see it
-            u4 worst = {0, 0, 0, 0};
+    }
+
+    // Tokens of a tile that every row sees.
+    template <uint32_t kCount>
+    __device__ void tokens(const uint8_t *k, const uint8_t *v) {
+        acc16 s[kCount];
+        s8 p[2 * kCount];
+        scores<kCount>(k, s);
+        weigh<kCount>(s, p);
+        products<kCount>(v, p);
+    }
+
+    // 32 tokens of which the lane's row sees the first `seen`, or of a page outside the
+    // cache (not `fine`).  A value that is an infinity or a NaN must not meet the p of 0 of
+    // a row that does not see it: those are left out, and true comes back if there are any.
+    __device__ bool tokens_of_some(const uint8_t *k, const uint8_t *v, int32_t seen, bool fine) {
+        acc16 s[1];
+        s8 p[2];
+        scores<1>(k, s);
+        seen -= 4 * static_cast<int32_t>(lane >> 5);
 #pragma unroll
-            for (uint32_t i = 0; i < 2 * kCount; i++)
-#pragma unroll
-                for (uint32_t b = 0; b < P::kBlocks; b++)
-                    worst |= not_finite(read_v(v + i * 16 * P::kRowBytes, at.v[b][0], at.v[b][1]));
-            if (__any((worst[0] | worst[1] | worst[2] | worst[3]) != 0)) {
-                products<kCount, true>(v, p);
-                add_not_finite<kCount>(v, end - static_cast<int32_t>(first));
-                return;
-            }
+        for (uint32_t e = 0; e < 16; e++) {
+            const int32_t t = 8 * (e / 4) + e % 4;
+            s[0][e] = t >= seen ? -INFINITY : fine ? s[0][e] : NAN;
         }
-        products<kCount, false>(v, p);
+        weigh<1>(s, p);
+        u4 bad = {0, 0, 0, 0};
+#pragma unroll
+        for (uint32_t i = 0; i < 2; i++)
+#pragma unroll
+            for (uint32_t b = 0; b < P::kBlocks; b++) {
+                const s8 x = read_v(v + i * 16 * P::kRowBytes, at.v[b][0], at.v[b][1]);
+                const u4 lost = not_finite(x);
+                bad |= lost;
+                // 0 for 1, all bits for 0
+                const us8 keep = __builtin_bit_cast(us8, lost) - static_cast<unsigned short>(1);
+                o[b] = Mat<C>::product(x & __builtin_bit_cast(s8, keep), p[i], o[b]);
+            }
+        return __any((bad[0] | bad[1] | bad[2] | bad[3]) != 0);
     }
 
     // Of each half of a word: 1 if it holds an infinity or a NaN.
@@ -292,112 +330,124 @@ struct Worker {
         const us8 t = __builtin_bit_cast(us8, x) & static_cast<unsigned short>(0x7FFF);
         return __builtin_bit_cast(u4, (t + static_cast<unsigned short>(0x8000 - Mat<C>::kInf)) >> 15);
     }
-    template <uint32_t kCount, bool kFinite>
+    template <uint32_t kCount>
     __device__ void products(const uint8_t *v, const s8 (&p)[2 * kCount]) {
 #pragma unroll
         for (uint32_t i = 0; i < 2 * kCount; i++)
 #pragma unroll
-            for (uint32_t b = 0; b < P::kBlocks; b++) {
-                s8 x = read_v(v + i * 16 * P::kRowBytes, at.v[b][0], at.v[b][1]);
-                if constexpr (kFinite)  // the others as 0
-                    x &= __builtin_bit_cast(s8, __builtin_bit_cast(us8, not_finite(x)) -
-                                                    static_cast<unsigned short>(1));
-                o[b] = Mat<C>::product(x, p[i], o[b]);
-            }
-    }
-    // What the products left out, token after token: the sum becomes the infinity or the
-    // NaN of every value that the lane's row sees.
-    template <uint32_t kCount>
-    __device__ void add_not_finite(const uint8_t *v, int32_t seen) {
-        typedef unsigned short us4 __attribute__((ext_vector_type(4)));
-#pragma nounroll
-        for (uint32_t t = 0; t < 32 * kCount; t++) {
-            const uint32_t sees = static_cast<int32_t>(t) < seen ? ~0u : 0u;
-#pragma unroll
             for (uint32_t b = 0; b < P::kBlocks; b++)
-#pragma unroll
-                for (uint32_t e = 0; e < 4; e++) {
-                    const us4 x = *reinterpret_cast<const us4 *>(
-                        v + t * P::kRowBytes + (((4 * b + e) ^ swizzle<D>(t & 15)) << 4) +
-                        8 * (lane >> 5));
-                    const us4 bad = ((x & static_cast<unsigned short>(0x7FFF)) +
-                                     static_cast<unsigned short>(0x8000 - Mat<C>::kInf)) >> 15;
-                    const us4 y = x & -bad & static_cast<unsigned short>(sees);
-#pragma unroll
-                    for (uint32_t j = 0; j < 4; j++) o[b][4 * e + j] += C::load(y[j]);
-                }
-        }
-    }
-
-    // One tile of a range.  `sees`: tokens of the range that the lane's row sees (every
-    // row of the workgroup at least `least`, at most r.end).
-    template <bool kSplit>
-    __device__ void tile(const Range &r, uint32_t tile, const uint8_t *k, const uint8_t *v,
-                         int32_t sees, int32_t least, bool fine) {
-        const int32_t at = static_cast<int32_t>(tile);
-        const bool masked = at + static_cast<int32_t>(kTile) > least;
-        const bool uneven = masked && least < static_cast<int32_t>(r.end);
-        if constexpr (kSplit)
-            tokens<1>(k, v, 32 * (wave & 1), masked, sees - at, !fine, uneven);
-        else
-            tokens<2>(k, v, 0, masked, sees - at, !fine, uneven);
+                o[b] = Mat<C>::product(
+                    read_v(v + i * 16 * P::kRowBytes, at.v[b][0], at.v[b][1]), p[i], o[b]);
     }
 };
 
-// kSplit: the rows are at most 64, waves 2 i and 2 i + 1 take rows 32 i.. and share
-// the tokens of a tile.
-template <class C, uint32_t D, bool kSplit>
+// Adds to x the infinities and NaN among eight values of the tokens [from, to) of a
+// range: what tokens_of_some left out.
+template <class C, uint32_t D>
+__device__ void add_left_out(const AttendArgs &a, const Range &r, uint32_t from, uint32_t to,
+                             uint32_t kvh, uint32_t piece, float (&x)[8]) {
+    for (uint32_t t = from; t < to; t++) {
+        const uint32_t i = t >> a.page_shift;
+        if (i >= r.width) return;  // the row has no result
+        const uint32_t page = r.table[i];
+        if (page >= a.pages) return;
+        const uint64_t in = (uint64_t{kvh * D} << a.page_shift) + (t & ((1u << a.page_shift) - 1)) * D;
+        const uint4 y = load16(a.v + page * a.page_v + in + 8 * piece);
+        for (uint32_t e = 0; e < 8; e++) {
+            const float z = C::get(y, e);
+            if (!(fabsf(z) < INFINITY)) x[e] += z;
+        }
+    }
+}
+
+// A tile of rows against a part of the prefix or of own tokens, or both after one
+// another.  `places`: own tokens that the first row sees.
+template <class C, uint32_t D, bool kWhole>
 __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32_t row0,
                                        uint32_t rows, uint32_t part, const Range &front,
                                        const Range &own, int32_t places, uint8_t *k0, uint8_t *v0,
-                                       uint8_t *k1, uint8_t *v1, float2 *stats) {
+                                       uint8_t *k1, uint8_t *v1, float2 *stats,
+                                       uint32_t *left_out) {
     using W = Worker<C, D>;
     using P = Places<D>;
-    W w(a, kvh);
+    // up to 64 rows: waves 2 i and 2 i + 1 take rows 32 i.. and share the tokens of a tile
+    const bool split = rows <= 64;
+    W w(a, kvh, split);
     const uint32_t half = w.lane >> 5, n = w.lane & 31;
-    const uint32_t mine = 32 * (kSplit ? w.wave >> 1 : w.wave);
+    const uint32_t mine = 32 * (split ? w.wave >> 1 : w.wave);
     const bool busy = mine < rows;
     const uint32_t row = row0 + min(mine + n, rows - 1);
     const uint32_t token = row / a.group;
     const uint32_t head = kvh * a.group + row % a.group;
+    const int32_t later = static_cast<int32_t>(token - row0 / a.group);
     if (busy) {
         const uint16_t *p = a.q + token * a.q_stride + uint64_t{head} * D + 8 * half;
 #pragma unroll
         for (uint32_t i = 0; i < P::kSteps; i++)
             w.q[i] = __builtin_bit_cast(s8, load16(p + 16 * i));
     }
+    bool lost = false;  // a page outside the cache, among tokens that all rows see
     for (uint32_t i = 0; i < 2; i++) {
         const Range r = i ? own : front;
         if (r.begin >= r.end) continue;
-        // own tokens that the rows see: `places` the workgroup's first row
+        // what every row sees, and the lane's row
         const int32_t end = static_cast<int32_t>(r.end);
-        const int32_t least = i ? min(places, end) : end;
-        const int32_t sees =
-            i ? min(places + static_cast<int32_t>(token - row0 / a.group), end) : end;
-        bool fine0 = w.load(r, r.begin, k0, v0), fine1 = true;
-        w.landed(r, r.begin, v0);
+        const uint32_t least = i ? max(min(places, end), 0) : end;
+        const int32_t sees = i ? min(places + later, end) : end;
+        const uint32_t plain = least & ~(kTile - 1);  // tiles before it: no row is masked
+        // (page numbers behind the last tile: its own once more)
+        bool fine = w.load(r, r.begin, w.pages(r, r.begin), k0, v0), odd = false;
+        uint32_t next = w.pages(r, r.begin + kTile), t = r.begin;
+        w.landed(r, t, v0);
         __syncthreads();
-        for (uint32_t t = r.begin;; t += 2 * kTile) {
+        // one tile is looked at while the next one is loaded
+        const auto step = [&](uint8_t *k, uint8_t *v, uint8_t *to_k, uint8_t *to_v) {
+            lost = lost || !fine;
             const bool more = t + kTile < r.end;
-            if (more) fine1 = w.load(r, t + kTile, k1, v1);
-            if (busy) w.template tile<kSplit>(r, t, k0, v0, sees, least, fine0);
-            if (!more) break;
-            w.landed(r, t + kTile, v1);
+            if (more) fine = w.load(r, t + kTile, next, to_k, to_v);
+            next = w.pages(r, t + 2 * kTile);
+            if (busy) {
+                if (split)
+                    w.template tokens<1>(k, v);
+                else
+                    w.template tokens<2>(k, v);
+            }
+            t += kTile;
+            odd = !odd;
+            if (more) w.landed(r, t, to_v);
             __syncthreads();
-            const bool again = t + 2 * kTile < r.end;
-            if (again) fine0 = w.load(r, t + 2 * kTile, k0, v0);
-            if (busy) w.template tile<kSplit>(r, t + kTile, k1, v1, sees, least, fine1);
-            if (!again) break;
-            w.landed(r, t + 2 * kTile, v0);
-            __syncthreads();
+        };
+        while (t < plain) {
+            step(k0, v0, k1, v1);
+            if (t >= plain) break;
+            step(k1, v1, k0, v0);
         }
-        __syncthreads();
+        while (t < r.end) {
+            if (busy) {
+                const uint8_t *k = odd ? k1 : k0, *v = odd ? v1 : v0;
+                const int32_t first = split ? 32 * (w.wave & 1) : 0;
+#pragma nounroll
+                for (uint32_t j = 0; j < (split ? 1 : 2); j++)
+                    if (w.tokens_of_some(k + 32 * j * P::kRowBytes, v + 32 * j * P::kRowBytes,
+                                         sees - static_cast<int32_t>(t + 32 * j) - first, fine))
+                        *left_out = 1;
+            }
+            t += kTile;
+            __syncthreads();
+            if (t >= r.end) break;
+            fine = w.load(r, t, next, k0, v0);
+            next = w.pages(r, t + kTile);
+            w.landed(r, t, v0);
+            __syncthreads();
+            odd = false;
+        }
     }
     // Rows through LDS: a wave's 32 x D floats in a buffer, 16-byte pieces of row n at
     // piece ^ n.  Waves that shared tokens bring theirs to the larger bound first.
     float l = w.l + __shfl_xor(w.l, 32), m = w.m;
+    if (lost || places + later > static_cast<int32_t>(room(a.batch, a.page_shift))) l = NAN;
     float *slice = reinterpret_cast<float *>(w.wave == 0 ? k0 : w.wave == 1 ? v0 : w.wave == 2 ? k1 : v1);
-    if constexpr (kSplit) {
+    if (split) {
         if (half == 0) stats[w.wave * 32 + n] = float2{m, l};
         __syncthreads();
         const float2 other = stats[(w.wave ^ 1) * 32 + n];
@@ -422,25 +472,37 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
         }
     __syncthreads();
     constexpr uint32_t kPieces = D / 8;  // of a row: 8 values each
+#pragma nounroll
     for (uint32_t i = threadIdx.x; i < rows * kPieces; i += kThreads) {
         const uint32_t r = i / kPieces, piece = i % kPieces;
-        const uint32_t src = kSplit ? 2 * (r / 32) : r / 32, nn = r % 32;
+        const uint32_t src = split ? 2 * (r / 32) : r / 32, nn = r % 32;
         const float2 ml = stats[src * 32 + nn];
-        float x[8];
-        for (uint32_t s = 0; s < (kSplit ? 2 : 1); s++) {
-            const uint32_t from = src + s;
+        float x[8] = {};
+#pragma nounroll
+        for (uint32_t from = src; from < src + (split ? 2 : 1); from++) {
             const float *p = reinterpret_cast<const float *>(
                                  from == 0 ? k0 : from == 1 ? v0 : from == 2 ? k1 : v1) + nn * D;
 #pragma unroll
             for (uint32_t e = 0; e < 2; e++) {
                 const float4 y = *reinterpret_cast<const float4 *>(
                     p + (((2 * piece + e) ^ (nn & (D / 4 - 1))) << 2));
-                const float z[4] = {y.x, y.y, y.z, y.w};
-                for (uint32_t j = 0; j < 4; j++) x[4 * e + j] = s ? x[4 * e + j] + z[j] : z[j];
+                x[4 * e] += y.x, x[4 * e + 1] += y.y, x[4 * e + 2] += y.z, x[4 * e + 3] += y.w;
             }
         }
         const uint32_t at = row0 + r, tok = at / a.group, hd = kvh * a.group + at % a.group;
-        if (a.whole) {
+        if (*left_out) {
+            // the tiles that not all rows see to their end
+            const int32_t sees = places + static_cast<int32_t>(tok - row0 / a.group);
+            for (uint32_t j = 0; j < 2; j++) {
+                const Range y = j ? own : front;
+                const uint32_t least = j ? max(places, 0) : y.end;
+                if (y.begin < y.end)
+                    add_left_out<C, D>(a, y, max(y.begin, least & ~(kTile - 1)),
+                                       j ? min(y.end, static_cast<uint32_t>(max(sees, 0))) : y.end,
+                                       kvh, piece, x);
+            }
+        }
+        if constexpr (kWhole) {
             const float inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
             uint32_t word[4];
 #pragma unroll
@@ -462,116 +524,300 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
     }
 }
 
+#define DF11_ATTEND_LDS                                                                       \
+    constexpr uint32_t kBytes = kTile * 2 * D;                                                \
+    __shared__ __attribute__((aligned(1024))) uint8_t k0[kBytes], v0[kBytes], k1[kBytes],     \
+        v1[kBytes];                                                                           \
+    __shared__ float2 stats[4 * 32];                                                          \
+    __shared__ uint32_t left_out
+
+// A workgroup reads the prefix and all own tokens of a tile of a sequence's rows.
 template <class C, uint32_t D>
-__global__ __launch_bounds__(kThreads, 2) void attend_kernel(AttendArgs a) {
-    constexpr uint32_t kBytes = kTile * 2 * D;
-    __shared__ __attribute__((aligned(1024))) uint8_t k0[kBytes], v0[kBytes], k1[kBytes], v1[kBytes];
-    __shared__ float2 stats[4 * 32];
-    const uint32_t x = blockIdx.x & 7;
+__global__ __launch_bounds__(kThreads, 2) void attend_whole_kernel(AttendArgs a) {
+    DF11_ATTEND_LDS;
     const Batch &b = a.batch;
-    Range front{}, own{};
-    uint32_t kvh, row0, rows, part;
-    int32_t first = 0;
-    if (blockIdx.x < a.front_grid) {
-        // a part of the prefix for rows of all sequences; the tiles of a part and head
-        // have numbers that one XCD takes, whose L2 then holds its K and V
-        const uint32_t y = blockIdx.x >> 3, pair = y / a.front_tiles * 8 + x;
-        kvh = pair % a.kv_heads;
-        part = pair / a.kv_heads;
-        if (part >= a.front_parts) return;
-        const uint32_t all = b.first(b.sequences) * a.group;
-        row0 = y % a.front_tiles * kRows;
-        if (row0 >= all) return;
-        rows = min(kRows, all - row0);
-        const uint32_t begin = part * a.front_step;
-        front = {b.prefix_table, b.prefix_pages, begin, min(b.prefix_len, begin + a.front_step)};
-    } else {
-        // a sequence's rows: tile numbers ascend over the sequences, and the last, which
-        // see the most, come first; an XCD takes whole heads or every own_groups-th tile
-        const uint32_t z = (blockIdx.x - a.front_grid) >> 3;
-        const uint32_t per = (a.own_tiles + a.own_groups - 1) / a.own_groups * a.own_parts;
-        const uint32_t combo = z / per * 8 + x, rest = z % per;
-        kvh = combo / a.own_groups;
-        if (kvh >= a.kv_heads) return;
-        const uint32_t cut_part = rest % a.own_parts;
-        const uint32_t number = rest / a.own_parts * a.own_groups + combo % a.own_groups;
-        if (number >= a.own_tiles) return;
-        const uint32_t id = a.own_tiles - 1 - number;
-        // sequence s has the numbers from (its first row) / kRows + s on: never fewer
-        // than its tiles
-        const auto base = [&](uint32_t s) { return b.first(s) * a.group / kRows + s; };
-        const uint32_t s = __builtin_amdgcn_readfirstlane(wave_search(b.sequences, id, base));
-        if (s == ~0u) return;
-        const uint32_t from = b.first(s), to = b.first(s + 1);
-        row0 = from * a.group + (id - base(s)) * kRows;
-        if (to <= from || row0 >= to * a.group) return;
-        rows = min(kRows, to * a.group - row0);
-        // tokens that the tile's first and last rows see
-        const int32_t length = max(b.length[s], 0);
-        const int32_t before = length - static_cast<int32_t>(to) + 1;
-        first = before + static_cast<int32_t>(row0 / a.group);
-        const int32_t last = before + static_cast<int32_t>((row0 + rows - 1) / a.group);
-        const uint32_t end = max(last, 0);
-        const int32_t *table = b.table + s * b.table_stride;
-        if (a.whole) {
-            part = 0;
-            front = {b.prefix_table, b.prefix_pages, 0, b.prefix_len};
-            own = {table, b.width, 0, end};
-        } else {
-            const Cut c = cut(length, a.own_parts);
-            if (cut_part >= c.parts) return;
-            part = a.front_parts + cut_part;
-            own = {table, b.width, cut_part * c.step, min(end, (cut_part + 1) * c.step)};
-        }
-    }
-    if (rows <= 64)
-        attend<C, D, true>(a, kvh, row0, rows, part, front, own, first, k0, v0, k1, v1, stats);
-    else
-        attend<C, D, false>(a, kvh, row0, rows, part, front, own, first, k0, v0, k1, v1, stats);
+    // tile numbers ascend over the sequences, and the last, which see the most, come first;
+    // an XCD takes whole heads or every own_groups-th tile of one, so that its L2 holds
+    // their keys and values
+    const uint32_t x = blockIdx.x & 7, z = blockIdx.x >> 3;
+    const uint32_t per = (a.own_tiles + a.own_groups - 1) / a.own_groups;
+    const uint32_t combo = z / per * 8 + x, kvh = combo / a.own_groups;
+    const uint32_t number = z % per * a.own_groups + combo % a.own_groups;
+    if (kvh >= a.kv_heads || number >= a.own_tiles) return;
+    const uint32_t id = a.own_tiles - 1 - number;
+    // sequence s has the numbers from (its first row) / kRows + s on: never fewer than its
+    // tiles
+    const auto base = [&](uint32_t s) { return b.first(s) * a.group / kRows + s; };
+    const uint32_t s = __builtin_amdgcn_readfirstlane(wave_search(b.sequences, id, base));
+    if (s == ~0u) return;
+    const Sequence q = sequence(b, s);
+    const uint32_t i = id - base(s);
+    if (i >= q.tiles(a)) return;
+    if (threadIdx.x == 0) left_out = 0;  // (barriers follow before it is set or read)
+    const Range front{b.prefix_table, b.prefix_pages, 0, b.prefix_len};
+    const Range own{b.table + s * b.table_stride, b.width, 0, q.end(a, i)};
+    const uint32_t row0 = q.first_row(a, i), rows = q.rows(a, i);
+    attend<C, D, true>(a, kvh, row0, rows, 0, front, own, q.least(a, i), k0, v0, k1, v1, stats,
+                       &left_out);
 }
 
-// Joins the parts of a row and head: a wave for each.  A lane has one part's bound
-// and sum, then D / 64 of the values.
-template <class C, uint32_t D>
-__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+// All the work in a row, cut into equal shares: the prefix' tokens for each head and tile
+// of rows, then every sequence's own tokens for each head and tile of its rows.  The unit
+// is a tile of kTile tokens; kStart units before an item's tiles stand for what it costs to
+// begin and end one (about 7 us of loads after one another, where a tile takes 2).
+constexpr uint32_t kStart = 4;
+struct Shares {
+    uint32_t front, own, size;  // units of the prefix, of own tokens (one head), of a share
+};
+__device__ inline uint32_t cost(uint32_t tiles) { return tiles ? kStart + tiles : 0; }
+__device__ inline uint32_t pieces(uint32_t n, uint32_t of) { return (n + of - 1) / of; }
+
+// Calls f(first sequence, this lane's units, units in front of this lane's) for 64
+// sequences after the other until it returns true.  All units, where it never does.
+template <class F>
+__device__ inline uint64_t each_64(const AttendArgs &a, F f) {
     const uint32_t lane = threadIdx.x & 63;
-    const uint32_t at = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-    const uint32_t token = at / a.heads, head = at % a.heads;
-    if (token >= a.batch.rows) return;
-    const Owner o = owner(a.batch, token);
-    if (o.s == ~0u) return;
-    const uint32_t parts = a.front_parts + cut(max(a.batch.length[o.s], 0), a.own_parts).parts;
-    const uint64_t each = uint64_t{a.batch.rows} * a.heads;
-    const float2 ml = lane < parts ? a.part_ml[lane * each + at] : float2{-INFINITY, 0.0f};
-    const float m = wave_max(ml.x), base = m == -INFINITY ? 0.0f : m;
-    const float part = __builtin_amdgcn_exp2f(ml.x - base);
-    const float l = wave_sum(part * ml.y);
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    constexpr uint32_t kEach = D / 64;
-    float x[kEach] = {};
-    const float *p = a.part_o + uint64_t{at} * D + lane * kEach;
-    for (uint32_t i = 0; i < parts; i++) {
-        const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(part), i));
-        for (uint32_t e = 0; e < kEach; e++) x[e] += f * p[i * each * D + e];
+    uint64_t all = 0;
+    for (uint32_t s0 = 0; s0 < a.batch.sequences; s0 += 64) {
+        const uint32_t before = all;
+        uint32_t n = 0;
+        if (s0 + lane < a.batch.sequences) {
+            const Sequence q = sequence(a.batch, s0 + lane);
+            for (uint32_t i = 0; i < q.tiles(a); i++) n += cost(q.token_tiles(a, i));
+        }
+        uint32_t sum = n;
+        for (uint32_t d = 1; d < 64; d *= 2) {
+            const uint32_t y = __shfl_up(sum, d);
+            if (lane >= d) sum += y;
+        }
+        if (f(s0, n, before + sum - n)) break;
+        all += __builtin_amdgcn_readlane(sum, 63);
     }
-    uint16_t *out = a.out + token * a.out_stride + uint64_t{head} * D + lane * kEach;
-    if constexpr (kEach == 2)
-        *reinterpret_cast<uint32_t *>(out) =
-            C::store(x[0] * inv) | static_cast<uint32_t>(C::store(x[1] * inv)) << 16;
-    else
-        *out = C::store(x[0] * inv);
+    return all;
+}
+
+// A workgroup takes one share.  It holds as many tiles as any other whatever the
+// sequences' lengths are; a row's parts are the shares that its tiles lie in.
+template <class C, uint32_t D>
+__global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a) {
+    DF11_ATTEND_LDS;
+    const Batch &b = a.batch;
+    const uint32_t lane = threadIdx.x & 63;
+    // the units of all sequences, and the most tiles of a row
+    Shares w{a.kv_heads * a.row_tiles * cost(a.front_tiles), 0, 0};
+    uint32_t most = 0;
+    const uint64_t own_tiles = each_64(a, [&](uint32_t s0, uint32_t n, uint32_t before) {
+        if (s0 + lane < b.sequences) {
+            const Sequence q = sequence(b, s0 + lane);
+            if (n) most = max(most, q.token_tiles(a, q.tiles(a) - 1));
+            if (blockIdx.x == 0 && threadIdx.x < 64) a.sums[2 + s0 + lane] = before;
+        }
+        return false;
+    });
+    most = wave_max(most);
+    // (more than 32 bits only where the sequences' starts do not ascend: no result)
+    w.own = (w.front + a.kv_heads * own_tiles) >> 32 ? 0 : own_tiles;
+    // no row has more parts than there is room for
+    w.size = pieces(w.front + a.kv_heads * w.own, gridDim.x);
+    if (a.front_parts > 1) w.size = max(w.size, pieces(a.front_tiles - 1, a.front_parts - 1));
+    if (a.own_parts > 1) w.size = max(w.size, pieces(most - min(most, 1u), a.own_parts - 1));
+    w.size = max(w.size, 1u);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.sums[0] = w.size, a.sums[1] = w.own;
+    // A CU has the workgroups i and i + 256: one takes its share from the front of the row
+    // (the prefix, which the matrix cores bound), the other from its end (own tokens, which
+    // memory bounds).
+    const uint32_t half = gridDim.x / 2;
+    const uint32_t share = blockIdx.x < half ? blockIdx.x : gridDim.x - 1 - (blockIdx.x - half);
+    uint32_t at = share * w.size;
+    const uint32_t end = min(at + w.size, w.front + a.kv_heads * w.own);
+    if (at >= end) return;
+    uint32_t s = ~0u, i = 0, unit = 0, kvh = 0;  // own tokens: where `at` is
+    Sequence q{};
+    while (at < end) {
+        uint32_t row0, rows, part, head, n, tiles;
+        int32_t least = INT32_MIN / 2;  // own tokens that the first row sees: none
+        Range front{}, own{};
+        if (at < w.front) {
+            tiles = a.front_tiles;
+            const uint32_t item = at / cost(tiles);
+            unit = at % cost(tiles);
+            head = item / a.row_tiles;
+            row0 = item % a.row_tiles * kRows;
+            const uint32_t all = b.first(b.sequences) * a.group;
+            rows = row0 < all ? min(kRows, all - row0) : 0;
+        } else {
+            if (s == ~0u) {
+                kvh = (at - w.front) / w.own;
+                const uint32_t to = (at - w.front) % w.own;
+                each_64(a, [&](uint32_t s0, uint32_t n, uint32_t before) {
+                    const uint64_t here = __ballot(before <= to && to < before + n);
+                    if (!here) return false;
+                    const uint32_t at = __builtin_ctzll(here);
+                    s = s0 + at;
+                    unit = to - __builtin_amdgcn_readlane(before, at);
+                    return true;
+                });
+                s = __builtin_amdgcn_readfirstlane(s);
+                if (s == ~0u) return;
+                q = sequence(b, s);
+                for (i = 0; unit >= cost(q.token_tiles(a, i)); i++)
+                    unit -= cost(q.token_tiles(a, i));
+            }
+            tiles = q.token_tiles(a, i);
+            head = kvh;
+            row0 = q.first_row(a, i);
+            rows = q.rows(a, i);
+            least = q.least(a, i);
+        }
+        n = min(cost(tiles) - unit, end - at);
+        const uint32_t first = max(unit, kStart) - kStart, last = max(unit + n, kStart) - kStart;
+        part = share - (at - unit + kStart) / w.size;
+        if (at < w.front) {
+            front = {b.prefix_table, b.prefix_pages, first * kTile,
+                     min(b.prefix_len, last * kTile)};
+        } else {
+            part += a.front_parts;
+            own = {b.table + s * b.table_stride, b.width, first * kTile,
+                   min(q.end(a, i), last * kTile)};
+        }
+        if (first == last) rows = 0;
+        if (rows) {
+            __syncthreads();  // LDS is read
+            if (threadIdx.x == 0) left_out = 0;
+            attend<C, D, false>(a, head, row0, rows, part, front, own, least, k0, v0, k1, v1,
+                                stats, &left_out);
+        }
+        at += n;
+        if (s == ~0u || at >= end) continue;
+        // on to the next tile of rows that sees something
+        unit = 0;
+        do i++;
+        while (i < q.tiles(a) && !q.token_tiles(a, i));
+        if (i < q.tiles(a)) continue;
+        i = 0;
+        for (uint32_t from = s + 1;; from += 64) {
+            if (from >= b.sequences) from = 0, kvh++;
+            const uint32_t next = from + lane;
+            bool some = false;
+            if (next < b.sequences) {
+                const Sequence y = sequence(b, next);
+                some = y.tiles(a) && y.token_tiles(a, y.tiles(a) - 1);
+            }
+            if (const uint64_t here = __ballot(some)) {
+                s = __builtin_amdgcn_readfirstlane(from + __builtin_ctzll(here));
+                break;
+            }
+        }
+        q = sequence(b, s);
+        while (!q.token_tiles(a, i)) i++;
+    }
+}
+
+// The parts of the prefix and of own tokens that a row's head has: those of the prefix
+// are 0.., of own tokens front_parts...
+struct Parts {
+    uint32_t front, own;
+};
+__device__ inline Parts parts_of(const AttendArgs &a, uint32_t token, uint32_t head, uint32_t s) {
+    const uint32_t kvh = head / a.group, row = token * a.group + head % a.group;
+    const uint32_t size = a.sums[0], own = a.sums[1];
+    const uint32_t each = cost(a.front_tiles);
+    Parts p{0, 0};
+    if (each) {
+        const uint32_t at = (kvh * a.row_tiles + row / kRows) * each + kStart;
+        p.front = (at + a.front_tiles - 1) / size - at / size + 1;
+    }
+    const Sequence q = sequence(a.batch, s);
+    const uint32_t i = (row - q.from * a.group) / kRows, n = q.token_tiles(a, i);
+    if (n) {
+        uint32_t at = a.kv_heads * a.row_tiles * each + kvh * own + a.sums[2 + s] + kStart;
+        for (uint32_t j = 0; j < i; j++) at += cost(q.token_tiles(a, j));
+        p.own = (at + n - 1) / size - at / size + 1;
+    }
+    p.front = min(p.front, a.front_parts);
+    p.own = min(p.own, a.own_parts);
+    return p;
+}
+
+// Joins the parts of a row and head: kWaves waves for each, several parts at a time.
+template <class C, uint32_t D, uint32_t kWaves>
+__global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
+    constexpr uint32_t kLanes = D / 4, kAtOnce = 64 / kLanes;  // lanes of a part
+    constexpr uint32_t kRounds = 2 * kMaxParts / 64;
+    __shared__ float weights[4 / kWaves][2 * kMaxParts];
+    __shared__ float4 sums[4][kLanes];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = wave / kWaves;
+    const uint32_t at = __builtin_amdgcn_readfirstlane(blockIdx.x * (4 / kWaves) + mine);
+    const uint32_t token = at / a.heads, head = at % a.heads;
+    const Owner o = token < a.batch.rows ? owner(a.batch, token) : Owner{~0u, 0};
+    if (o.s == ~0u) return;  // (with kWaves = 4 all waves)
+    const Parts n = parts_of(a, token, head, o.s);
+    const uint32_t parts = n.front + n.own, skip = a.front_parts - n.front;
+    const uint64_t each = uint64_t{a.batch.rows} * a.heads;
+    const auto slot = [&](uint32_t i) { return (i < n.front ? i : i + skip) * each + at; };
+    float2 ml[kRounds];
+    float m = -INFINITY, l = 0.0f;
+    for (uint32_t i = 0; i < kRounds && 64 * i < parts; i++) {
+        const uint32_t p = 64 * i + lane;
+        ml[i] = p < parts ? a.part_ml[slot(p)] : float2{-INFINITY, 0.0f};
+        m = fmaxf(m, ml[i].x);
+    }
+    m = wave_max(m);
+    const float base = m == -INFINITY ? 0.0f : m;
+    for (uint32_t i = 0; i < kRounds && 64 * i < parts; i++) {
+        const float w = __builtin_amdgcn_exp2f(ml[i].x - base);
+        l += w * ml[i].y;
+        weights[mine][64 * i + lane] = w;  // kWaves = 4: each wave writes the same
+    }
+    l = wave_sum(l);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const uint32_t sub = wave % kWaves * kAtOnce + lane / kLanes, col = lane % kLanes * 4;
+    constexpr uint32_t kStep = kWaves * kAtOnce;
+    const auto value = [&](uint32_t i) {
+        return *reinterpret_cast<const float4 *>(a.part_o + slot(i) * D + col);
+    };
+    float4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    const auto add = [&](float w, const float4 &y) {
+        x.x += w * y.x, x.y += w * y.y, x.z += w * y.z, x.w += w * y.w;
+    };
+    uint32_t i = sub;
+    for (; i + 3 * kStep < parts; i += 4 * kStep) {
+        float4 y[4];
+        for (uint32_t e = 0; e < 4; e++) y[e] = value(i + e * kStep);
+        for (uint32_t e = 0; e < 4; e++) add(weights[mine][i + e * kStep], y[e]);
+    }
+    for (; i < parts; i += kStep) add(weights[mine][i], value(i));
+    for (uint32_t d = kLanes; d < 64; d *= 2) {
+        x.x += __shfl_xor(x.x, d), x.y += __shfl_xor(x.y, d);
+        x.z += __shfl_xor(x.z, d), x.w += __shfl_xor(x.w, d);
+    }
+    if constexpr (kWaves == 4) {
+        if (lane < kLanes) sums[wave][lane] = x;
+        __syncthreads();
+        if (wave) return;
+        for (uint32_t j = 1; j < 4; j++) add(1.0f, sums[j][lane % kLanes]);
+    }
+    if (lane < kLanes) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        *reinterpret_cast<uint2 *>(a.out + token * a.out_stride + uint64_t{head} * D + col) =
+            uint2{C::store(x.x * inv) | static_cast<uint32_t>(C::store(x.y * inv)) << 16,
+                  C::store(x.z * inv) | static_cast<uint32_t>(C::store(x.w * inv)) << 16};
+    }
     if (a.lse && lane == 0) a.lse[at] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-constexpr uint32_t kMaxParts = 32;  // of the prefix, and of a sequence's own tokens
-constexpr uint32_t kSlots = 512;    // workgroups that the GPU holds at once: two a CU
+constexpr uint32_t kSlots = 512;  // workgroups that the GPU holds at once: two a CU
+constexpr uint32_t kFewJoins = 1024;
 
 struct Plan {
-    uint32_t front_tiles, front_parts, front_step, own_tiles, own_parts, own_groups, whole;
-    uint64_t front_grid, own_grid, bytes;
+    uint32_t own_tiles, own_groups, row_tiles, front_tiles, front_parts, own_parts;
+    bool whole;
+    uint64_t grid, joins, bytes;
 };
 
-uint64_t up(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
+uint64_t up(uint64_t n, uint64_t of) { return (n + of - 1) / of; }
 
 int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_kv_batch &b,
             Plan *p) {
@@ -579,44 +825,51 @@ int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_
     if (!heads || heads >> 20 || heads % c.heads || tokens > kMaxSequences || tokens * heads >> 31)
         return DF11_E_INVALID_ARG;
     if (!tokens || !b.sequences) return DF11_OK;
-    const uint64_t group = heads / c.heads, rows = tokens * group;
-    const uint64_t tiles = (rows + kRows - 1) / kRows;
+    const uint64_t rows = tokens * (heads / c.heads), tiles = up(rows, kRows);
     const uint64_t own_tiles = rows / kRows + b.sequences;
-    const uint64_t capacity = uint64_t{b.width} * c.page_size;
-    p->own_tiles = own_tiles;
-    p->own_groups = 8 / std::__gcd(c.heads, 8u);
-    p->own_parts = 1;
     // Rows that fill tiles by themselves, enough of them to fill the GPU: the prefix is
     // read with the own tokens, and nothing has to be joined.
     const uint64_t each = rows / std::min<uint64_t>(tokens, b.sequences);
     p->whole = each >= 64 && tiles * c.heads >= kSlots / 2;
-    if (!p->whole) {
-        if (b.prefix_len) {
-            const uint64_t parts = std::max<uint64_t>(
-                1, std::min<uint64_t>(kMaxParts, kSlots / (tiles * c.heads)));
-            p->front_tiles = tiles;
-            p->front_step = std::max<uint64_t>(4 * kTile, up((b.prefix_len + parts - 1) / parts, kTile));
-            p->front_parts = (b.prefix_len + p->front_step - 1) / p->front_step;
-            p->front_grid = 8 * tiles * up(uint64_t{c.heads} * p->front_parts, 8) / 8;
-        }
-        p->own_parts = std::max<uint64_t>(
-            1, std::min<uint64_t>({kMaxParts, (capacity + 4 * kTile - 1) / (4 * kTile),
-                                   4 * kSlots / (own_tiles * c.heads)}));
-        p->bytes = (p->front_parts + p->own_parts) * tokens * heads * (4ull * c.dim + 8);
+    if (p->whole) {
+        p->own_tiles = own_tiles;
+        p->own_groups = 8 / std::__gcd(c.heads, 8u);
+        p->grid = 8 * up(uint64_t{c.heads} * p->own_groups, 8) * up(own_tiles, p->own_groups);
+        return p->grid < kMaxGrid ? DF11_OK : DF11_E_UNSUPPORTED;
     }
-    p->own_grid = up(uint64_t{c.heads} * p->own_groups, 8) *
-                  ((own_tiles + p->own_groups - 1) / p->own_groups) * p->own_parts;
-    const uint64_t joins = p->whole ? 0 : (tokens * heads + 3) / 4;
-    return std::max(p->front_grid + p->own_grid, joins) < kMaxGrid ? DF11_OK : DF11_E_UNSUPPORTED;
+    // Shares: at least so many parts that items as long as each other can fill the GPU,
+    // and for own tokens, whose lengths differ, more while they cost little memory.
+    const uint64_t space = std::min<uint64_t>(uint64_t{b.width} * c.page_size, INT32_MAX);
+    const uint64_t own = std::max<uint64_t>(1, up(space, kTile));
+    const auto parts = [](uint64_t n, uint64_t items, uint64_t least) {
+        return std::min<uint64_t>({n, kMaxParts, std::max<uint64_t>(least, kSlots / items + 2)});
+    };
+    const uint64_t part_bytes = tokens * heads * (4ull * c.dim + 8);
+    p->row_tiles = tiles;
+    p->front_tiles = up(b.prefix_len, kTile);
+    p->front_parts = parts(p->front_tiles, tiles * c.heads, 1);
+    p->own_parts = parts(own, own_tiles * c.heads, std::min<uint64_t>(64, (64u << 20) / part_bytes));
+    const uint64_t all = c.heads * (tiles * (p->front_tiles + kStart) + own_tiles * (own + kStart));
+    p->grid = kSlots;
+    p->joins = tokens * heads;
+    if (all >> 32 || up(p->joins, 4) >= kMaxGrid) return DF11_E_UNSUPPORTED;
+    p->bytes = (p->front_parts + p->own_parts) * part_bytes + 4 * up(2 + b.sequences, 4) * 4;
+    return DF11_OK;
 }
 
 template <class C, uint32_t D>
-int launch(const AttendArgs &a, uint64_t grid, hipStream_t stream) {
-    hipLaunchKernelGGL((attend_kernel<C, D>), dim3(grid), dim3(kThreads), 0, stream, a);
+int launch(const AttendArgs &a, const Plan &p, hipStream_t stream) {
+    const dim3 grid(p.grid), block(kThreads);
+    if (p.whole) {
+        hipLaunchKernelGGL((attend_whole_kernel<C, D>), grid, block, 0, stream, a);
+        return launched();
+    }
+    hipLaunchKernelGGL((attend_shares_kernel<C, D>), grid, block, 0, stream, a);
     if (const int rc = launched()) return rc;
-    if (a.whole) return DF11_OK;
-    const uint32_t wgs = (a.batch.rows * a.heads + 3) / 4;
-    hipLaunchKernelGGL((attend_join_kernel<C, D>), dim3(wgs), dim3(kThreads), 0, stream, a);
+    if (p.joins <= kFewJoins)
+        hipLaunchKernelGGL((attend_join_kernel<C, D, 4>), dim3(p.joins), block, 0, stream, a);
+    else
+        hipLaunchKernelGGL((attend_join_kernel<C, D, 1>), dim3(up(p.joins, 4)), block, 0, stream, a);
     return launched();
 }
 
@@ -663,22 +916,20 @@ int df11_prefix_attention(const void *q, uint64_t q_stride, uint64_t tokens, uin
     if (!rc && p.bytes && (!workspace || misaligned(workspace, 16))) rc = DF11_E_INVALID_ARG;
     if (!rc && workspace_bytes < p.bytes) rc = DF11_E_BUFFER_TOO_SMALL;
     if (rc) return rc;
-    const uint64_t values = (p.front_parts + p.own_parts) * tokens * cols;
+    const uint64_t parts = p.front_parts + p.own_parts;
+    auto *part_o = static_cast<float *>(workspace);
+    auto *part_ml = reinterpret_cast<float2 *>(part_o + parts * tokens * cols);
     const AttendArgs a{static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(cache->k),
                        static_cast<const uint16_t *>(cache->v), static_cast<uint16_t *>(out), lse,
-                       static_cast<float *>(workspace),
-                       reinterpret_cast<float2 *>(static_cast<float *>(workspace) + values),
-                       q_stride, out_stride, cache->k_stride, cache->v_stride,
+                       part_o, part_ml, q_stride, out_stride, cache->k_stride, cache->v_stride,
                        device_batch(*batch, tokens), scale * kLog2e, cache->pages,
                        static_cast<uint32_t>(__builtin_ctz(cache->page_size)), heads, cache->heads,
-                       heads / cache->heads, p.front_tiles, p.front_parts, p.front_step,
-                       static_cast<uint32_t>(p.front_grid), p.own_tiles, p.own_parts, p.own_groups,
-                       p.whole};
-    const uint64_t grid = p.front_grid + p.own_grid;
+                       heads / cache->heads, p.own_tiles, p.own_groups, p.row_tiles, p.front_tiles,
+                       p.front_parts, p.own_parts,
+                       reinterpret_cast<uint32_t *>(part_ml + parts * tokens * heads)};
     if (cache->dtype == DF11_BF16)
-        return cache->dim == 128 ? launch<BF16, 128>(a, grid, stream)
-                                 : launch<BF16, 64>(a, grid, stream);
-    return cache->dim == 128 ? launch<F16, 128>(a, grid, stream) : launch<F16, 64>(a, grid, stream);
+        return cache->dim == 128 ? launch<BF16, 128>(a, p, stream) : launch<BF16, 64>(a, p, stream);
+    return cache->dim == 128 ? launch<F16, 128>(a, p, stream) : launch<F16, 64>(a, p, stream);
 }
 
 }  // extern "C"

@@ -89,7 +89,7 @@ def test_append_refusals(change, rc):
     (dict(prefix_table=None), INVALID), (dict(prefix_table=A + 2), INVALID), (dict(prefix_len=129), INVALID),
     (dict(out=None), INVALID), (dict(out=2 * A, out_stride=2048), INVALID), (dict(lse=A + 2), INVALID),
     (dict(ws=None), INVALID), (dict(ws=A + 8), INVALID), (dict(ws_bytes=16), SMALL),
-    (dict(tokens=1 << 23, sequences=1 << 22), UNSUPPORTED), (dict(sequences=1 << 23), UNSUPPORTED),
+    (dict(tokens=1 << 23, sequences=1 << 22), UNSUPPORTED), (dict(sequences=1 << 23, width=1 << 16, table_stride=1 << 16), UNSUPPORTED),
     (dict(NOTHING, prefix_table=None, prefix_len=0), 0),
 ])
 def test_attention_refusals(change, rc):
@@ -105,12 +105,10 @@ def test_workspace_sizes():
         return ops.lib().df11_prefix_attention_workspace_bytes(tokens, q_heads, cache, batch, into)
 
     assert size(0, 8) == 0 and n.value == 0
-    assert size(5, 8) == 0 and n.value % (5 * 8 * (128 * 4 + 8)) == 0 and n.value > 0
+    assert size(5, 8) == 0 and n.value >= 2 * 5 * 8 * (128 * 4 + 8)  # the prefix' and the own tokens' results
     assert size(5, 8, k=None, start=None, table=None, prefix_table=None) == 0  # sizes alone count
     assert size(5, 8, into=None) == INVALID and size(5, 7) == INVALID and size(5, 8, dim=80) == INVALID
-    assert size(4096, 32, heads=8) == 0 and n.value == 0 or n.value > 0
-    # what a call of fewer rows needs is not more than what the largest needs
-    assert size(64, 8, sequences=64) == 0
+    assert size(4096, 32, heads=8, sequences=2) == 0 and n.value == 0  # enough rows to fill the GPU
 
 
 def test_constants_and_structs_are_the_headers():
