@@ -24,6 +24,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import struct
 from typing import NamedTuple, Optional
 
 import torch
@@ -47,17 +48,10 @@ DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _lib = None
 
 
-class _Cache(ctypes.Structure):  # df11_kv_cache
-    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v")] + [
-        (n, ctypes.c_uint32) for n in ("dtype", "pages", "heads", "page_size", "dim")] + [
-        (n, ctypes.c_uint64) for n in ("k_stride", "v_stride")]
-
-
-class _Batch(ctypes.Structure):  # df11_kv_batch
-    _fields_ = [(n, ctypes.c_void_p) for n in ("start", "length", "table")] + [
-        ("sequences", ctypes.c_uint32), ("width", ctypes.c_uint32),
-        ("table_stride", ctypes.c_uint64), ("prefix_table", ctypes.c_void_p),
-        ("prefix_pages", ctypes.c_uint32), ("prefix_len", ctypes.c_uint32)]
+# df11_kv_cache: k, v, dtype, pages, heads, page_size, dim, k_stride, v_stride;
+# df11_kv_batch: start, length, table, sequences, width, table_stride, prefix_table,
+# prefix_pages, prefix_len
+_CACHE, _BATCH = struct.Struct("@QQIIIIIQQ"), struct.Struct("@QQQIIQQII")
 
 
 def lib():
@@ -82,12 +76,11 @@ def lib():
             "df11_lora_backward_workspace_bytes": [*shapes, size],
             "df11_lora_backward": [*adapters, vp, u64, u32, vp, u64, vp, u64, vp, vp, vp, u64, vp],
         }
-        cache, batch = ctypes.POINTER(_Cache), ctypes.POINTER(_Batch)
         sig |= {
-            "df11_kv_append": [vp, u64, vp, u64, vp, u64, u32, u64, u32, vp, u32, u32, cache, batch,
-                               vp, u64, vp],
-            "df11_prefix_attention_workspace_bytes": [u64, u32, cache, batch, size],
-            "df11_prefix_attention": [vp, u64, u64, u32, f32, cache, batch, vp, u64, vp, vp, u64, vp],
+            "df11_kv_append": [vp, u64, vp, u64, vp, u64, u32, u64, u32, vp, u32, u32, vp, vp, vp,
+                               u64, vp],
+            "df11_prefix_attention_workspace_bytes": [u64, u32, vp, vp, size],
+            "df11_prefix_attention": [vp, u64, u64, u32, f32, vp, vp, vp, u64, vp, vp, u64, vp],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -440,50 +433,125 @@ def lora_backward(x, a, b, scale, adapter, dy, dx_base=None, dx=None, da=None, d
 
 
 # ------------------------------------------------- a paged cache of keys and values
-def _kv_cache(cache, device):
-    """df11_kv_cache of a KVCache on this GPU."""
-    k, v = cache
-    if k.dim() != 4 or k.dtype not in (torch.bfloat16, torch.float16):
+# These calls have eleven tensors each, whose checks take longer than the kernels of a
+# single token: what the tensors look like (not where they lie) is checked once and
+# remembered.
+def _look(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype, t.get_device())
+
+
+def _is_contiguous(shape, stride):
+    want = 1
+    for n, s in zip(reversed(shape), reversed(stride)):
+        if n != 1 and s != want:
+            return False
+        want *= n
+    return True
+
+
+def _as(look, shape, dtype, index, what):
+    """_want for what a tensor looks like."""
+    if look is not None and (look[0] != shape or look[2] != dtype or look[3] != index or
+                             not (0 in shape or _is_contiguous(look[0], look[1]))):
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on "
+                         f"GPU {index}, not {look[2]} {tuple(look[0])} with strides {look[1]} on "
+                         f"{look[3]}")
+
+
+def _as_rows(look, dtypes, index, what, shape=None):
+    """_rows for what a tensor looks like."""
+    size, stride, dtype, where = look
+    if len(size) != 2 or dtype not in dtypes or where != index or (
+            shape is not None and size != shape):
+        raise ValueError(f"{what} must be a 2-d tensor of {' or '.join(map(str, dtypes))}"
+                         f"{'' if shape is None else ' and shape ' + str(tuple(shape))} on "
+                         f"GPU {index}, not {dtype} {tuple(size)} on {where}")
+    if size[1] > 1 and stride[1] != 1:
+        raise ValueError(f"{what} must have contiguous rows")
+    return stride[0] if size[0] > 1 else size[1]
+
+
+def _cache_sizes(k, v, index):
+    """What follows the addresses in df11_kv_cache."""
+    shape, stride, dtype, where = k
+    if len(shape) != 4 or dtype not in (torch.bfloat16, torch.float16):
         raise ValueError("cache.k must be (pages, kv_heads, page_size, head_dim), bfloat16 or "
-                         f"float16, not {k.dtype} {tuple(k.shape)}")
-    if v.shape != k.shape or v.dtype != k.dtype:
-        raise ValueError(f"cache.v must be as cache.k: {k.dtype} {tuple(k.shape)}, not {v.dtype} "
-                         f"{tuple(v.shape)}")
-    pages, heads, page, dim = k.shape
-    for t, what in ((k, "cache.k"), (v, "cache.v")):
-        if t.device != device:
-            raise ValueError(f"{what} must be on {device}, not {t.device}")
-        if t.stride()[1:] != (page * dim, dim, 1) and pages and not t[0].is_contiguous():
+                         f"float16, not {dtype} {tuple(shape)}")
+    if v[0] != shape or v[2] != dtype:
+        raise ValueError(f"cache.v must be as cache.k: {dtype} {tuple(shape)}, not {v[2]} "
+                         f"{tuple(v[0])}")
+    for (_, s, _, where), what in ((k, "cache.k"), (v, "cache.v")):
+        if where != index:
+            raise ValueError(f"{what} must be on GPU {index}, not {where}")
+        if not _is_contiguous(shape[1:], s[1:]):
             raise ValueError(f"each page of {what} must be contiguous")
-    return _Cache(k.data_ptr(), v.data_ptr(), DTYPES[k.dtype], pages, heads, page, dim,
-                  k.stride(0), v.stride(0))
+    return DTYPES[dtype], *shape, stride[0], v[1][0]
 
 
-def _kv_batch(batch, device):
-    """df11_kv_batch of a KVBatch on this GPU."""
-    start, length, table, prefix_table, prefix_len = batch
-    n = length.shape[0] if length.dim() == 1 else -1
-    _want(length, (n,), torch.int32, device, "batch.length")
-    _want(start, (n + 1,), torch.int32, device, "batch.start")
-    stride = _rows(table, (torch.int32,), device, "batch.table")
-    if table.shape[0] != n:
+def _batch_sizes(start, length, table, prefix_table, index):
+    """(sequences, width, table_stride) and pages of the prefix."""
+    n = length[0][0] if len(length[0]) == 1 else -1
+    _as(length, (n,), torch.int32, index, "batch.length")
+    _as(start, (n + 1,), torch.int32, index, "batch.start")
+    stride = _as_rows(table, (torch.int32,), index, "batch.table")
+    if table[0][0] != n:
         raise ValueError(f"batch.table must have a row for each of {n} sequences")
     pages = 0
     if prefix_table is not None:
-        pages = prefix_table.numel()
-        _want(prefix_table, (pages,), torch.int32, device, "batch.prefix_table")
+        pages = prefix_table[0].numel()
+        _as(prefix_table, (pages,), torch.int32, index, "batch.prefix_table")
+    return (n, table[0][1], stride), pages
+
+
+def _heads(columns, dim, what):
+    """Heads of `dim` values in the rows of a 2-d tensor."""
+    heads, rest = divmod(columns, dim)
+    if rest or not heads:
+        raise ValueError(f"{what}'s rows must be heads of {dim} values, not {columns}")
+    return heads
+
+
+def _on_gpu(t, what):
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{what} must be on a GPU, not {t.device}")
+    return index
+
+
+def _raw_stream(stream, index):
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index)
+    return codec._handle(stream, torch.device("cuda", index))
+
+
+def _pack(cache, batch, c, b, prefix_pages):
+    """The two structs; `c` and `b` as _cache_sizes and _batch_sizes give them."""
+    start, length, table, prefix_table, prefix_len = batch
     if not 0 <= prefix_len < 2 ** 31:
         raise ValueError(f"batch.prefix_len must be from 0 to 2^31 - 1, not {prefix_len}")
-    return _Batch(start.data_ptr(), length.data_ptr(), table.data_ptr(), n, table.shape[1], stride,
-                  _ptr(prefix_table), pages, prefix_len)
+    return (_CACHE.pack(cache[0].data_ptr(), cache[1].data_ptr(), *c),
+            _BATCH.pack(start.data_ptr(), length.data_ptr(), table.data_ptr(), *b,
+                        0 if prefix_table is None else prefix_table.data_ptr(), prefix_pages,
+                        prefix_len))
 
 
-def _heads(t, dim, what):
-    """Heads of `dim` values in the rows of a 2-d tensor."""
-    heads, rest = divmod(t.shape[1], dim)
-    if rest or not heads:
-        raise ValueError(f"{what}'s rows must be heads of {dim} values, not {t.shape[1]}")
-    return heads
+@functools.lru_cache(maxsize=1024)
+def _append_sizes(index, q, k, v, inv_freq, q_out, cache_k, cache_v, *batch):
+    c = _cache_sizes(cache_k, cache_v, index)
+    b, prefix_pages = _batch_sizes(*batch, index)
+    q_stride = _as_rows(q, DTYPES, index, "q")
+    tokens, heads = q[0][0], _heads(q[0][1], c[4], "q")
+    shape = (tokens, c[2] * c[4])
+    k_stride = _as_rows(k, (q[2],), index, "k", shape)
+    v_stride = _as_rows(v, (q[2],), index, "v", shape)
+    rotary = 0
+    if inv_freq is not None:
+        rotary = 2 * inv_freq[0].numel()
+        _as(inv_freq, (rotary // 2,), torch.float32, index, "inv_freq")
+    out_stride = q[0][1]
+    if q_out is not None:
+        out_stride = _as_rows(q_out, (cache_k[2],), index, "q_out", q[0])
+    return c, b, prefix_pages, q_stride, k_stride, v_stride, DTYPES[q[2]], tokens, heads, rotary, out_stride
 
 
 def kv_append(q, k, v, inv_freq, cache: KVCache, batch: KVBatch, interleaved: bool = False,
@@ -501,40 +569,49 @@ def kv_append(q, k, v, inv_freq, cache: KVCache, batch: KVBatch, interleaved: bo
     as they are in q_out; a row without a place in its sequence's pages, or whose
     page is not one of the cache, is not appended.  Two rows must not share a
     token of a page."""
-    device = _gpu(q, "q")
-    c, b = _kv_cache(cache, device), _kv_batch(batch, device)
-    tokens = q.shape[0]
-    q_stride = _rows(q, DTYPES, device, "q")
-    heads = _heads(q, c.dim, "q")
-    shape = (tokens, c.heads * c.dim)
-    k_stride = _rows(k, (q.dtype,), device, "k", shape)
-    v_stride = _rows(v, (q.dtype,), device, "v", shape)
-    rotary = 0
-    if inv_freq is not None:
-        rotary = 2 * inv_freq.numel()
-        _want(inv_freq, (rotary // 2,), torch.float32, device, "inv_freq")
+    index = _on_gpu(q, "q")
+    start, length, table, prefix_table, _ = batch
+    c, b, prefix_pages, q_stride, k_stride, v_stride, dtype, tokens, heads, rotary, out_stride = (
+        _append_sizes(index, _look(q), _look(k), _look(v), _look(inv_freq), _look(q_out),
+                      _look(cache[0]), _look(cache[1]), _look(start), _look(length), _look(table),
+                      _look(prefix_table)))
     if q_out is None:
-        q_out = _new(q.shape, cache.k.dtype, device, stream)
-    out_stride = _rows(q_out, (cache.k.dtype,), device, "q_out", q.shape)
+        q_out = _new(q.shape, cache[0].dtype, q.device, stream)
+    pc, pb = _pack(cache, batch, c, b, prefix_pages)
     codec._check(lib().df11_kv_append(
-        q.data_ptr(), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, DTYPES[q.dtype],
-        tokens, heads, _ptr(inv_freq), rotary, bool(interleaved), c, b, q_out.data_ptr(),
-        out_stride, _handle(stream, device)), "df11_kv_append")
+        q.data_ptr(), q_stride, k.data_ptr(), k_stride, v.data_ptr(), v_stride, dtype, tokens,
+        heads, _ptr(inv_freq), rotary, bool(interleaved), pc, pb, q_out.data_ptr(), out_stride,
+        _raw_stream(stream, index)), "df11_kv_append")
     return q_out
 
 
-def _attention_bytes(tokens, heads, c, b):
+@functools.lru_cache(maxsize=1024)
+def _attention_bytes(tokens, heads, c, b, prefix_pages, prefix_len):
     n = ctypes.c_uint64()
-    codec._check(lib().df11_prefix_attention_workspace_bytes(tokens, heads, c, b, ctypes.byref(n)),
-                 "df11_prefix_attention_workspace_bytes")
+    codec._check(lib().df11_prefix_attention_workspace_bytes(
+        tokens, heads, _CACHE.pack(0, 0, *c), _BATCH.pack(0, 0, 0, *b, 0, prefix_pages, prefix_len),
+        ctypes.byref(n)), "df11_prefix_attention_workspace_bytes")
     return int(n.value)
 
 
 def prefix_attention_workspace_bytes(tokens: int, heads: int, cache: KVCache,
                                      batch: KVBatch) -> int:
     """For this many rows of q; of cache and batch only the sizes count."""
-    device = cache.k.device
-    return _attention_bytes(tokens, heads, _kv_cache(cache, device), _kv_batch(batch, device))
+    index = _on_gpu(cache.k, "cache.k")
+    c = _cache_sizes(_look(cache.k), _look(cache.v), index)
+    return _attention_bytes(tokens, heads, c, *_batch_sizes(*map(_look, batch[:4]), index),
+                            batch.prefix_len)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_sizes(index, q, out, lse, cache_k, cache_v, *batch):
+    c = _cache_sizes(cache_k, cache_v, index)
+    b, prefix_pages = _batch_sizes(*batch, index)
+    q_stride = _as_rows(q, (cache_k[2],), index, "q")
+    tokens, heads = q[0][0], _heads(q[0][1], c[4], "q")
+    out_stride = q[0][1] if out is None else _as_rows(out, (q[2],), index, "out", q[0])
+    _as(lse, (tokens, heads), torch.float32, index, "lse")
+    return c, b, prefix_pages, q_stride, tokens, heads, out_stride
 
 
 def prefix_attention(q, cache: KVCache, batch: KVBatch, scale: Optional[float] = None, out=None,
@@ -550,23 +627,23 @@ def prefix_attention(q, cache: KVCache, batch: KVBatch, scale: Optional[float] =
     ``need_lse`` new) is the log of the sum of the exponentials.  Rows behind the
     last sequence's are left as they are in both.  A row that sees nothing has out
     0 and lse -inf; one that sees a page which is not of the cache has NaN."""
-    device = _gpu(q, "q")
-    c, b = _kv_cache(cache, device), _kv_batch(batch, device)
-    q_stride = _rows(q, (cache.k.dtype,), device, "q")
-    heads, tokens = _heads(q, c.dim, "q"), q.shape[0]
+    index = _on_gpu(q, "q")
+    start, length, table, prefix_table, prefix_len = batch
+    c, b, prefix_pages, q_stride, tokens, heads, out_stride = _attention_sizes(
+        index, _look(q), _look(out), _look(lse), _look(cache[0]), _look(cache[1]), _look(start),
+        _look(length), _look(table), _look(prefix_table))
     if out is None:
-        out = _new(q.shape, q.dtype, device, stream)
-    out_stride = _rows(out, (q.dtype,), device, "out", q.shape)
+        out = _new(q.shape, q.dtype, q.device, stream)
     if lse is None and need_lse:
-        lse = _new((tokens, heads), torch.float32, device, stream)
-    _want(lse, (tokens, heads), torch.float32, device, "lse")
+        lse = _new((tokens, heads), torch.float32, q.device, stream)
+    pc, pb = _pack(cache, batch, c, b, prefix_pages)
     if workspace is None:
-        ws_bytes = _attention_bytes(tokens, heads, c, b)
-        workspace = _new((ws_bytes,), torch.uint8, device, stream) if ws_bytes else None
+        ws_bytes = _attention_bytes(tokens, heads, c, b, prefix_pages, prefix_len)
+        workspace = _new((ws_bytes,), torch.uint8, q.device, stream) if ws_bytes else None
     else:
-        workspace, ws_bytes = _workspace(workspace, None, None, device, stream)
+        workspace, ws_bytes = _workspace(workspace, None, None, q.device, stream)
     codec._check(lib().df11_prefix_attention(
-        q.data_ptr(), q_stride, tokens, heads, c.dim ** -0.5 if scale is None else scale, c, b,
+        q.data_ptr(), q_stride, tokens, heads, c[4] ** -0.5 if scale is None else scale, pc, pb,
         out.data_ptr(), out_stride, _ptr(lse), _ptr(workspace), ws_bytes,
-        _handle(stream, device)), "df11_prefix_attention")
+        _raw_stream(stream, index)), "df11_prefix_attention")
     return Attention(out, lse)

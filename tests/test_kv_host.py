@@ -18,12 +18,24 @@ BATCH = dict(start=A, length=A, table=A, sequences=3, width=4, table_stride=4, p
              prefix_len=128)
 
 
+class Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v")] + [
+        (n, ctypes.c_uint32) for n in ("dtype", "pages", "heads", "page_size", "dim")] + [
+        (n, ctypes.c_uint64) for n in ("k_stride", "v_stride")]
+
+
+class Batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("start", "length", "table")] + [
+        ("sequences", ctypes.c_uint32), ("width", ctypes.c_uint32), ("table_stride", ctypes.c_uint64),
+        ("prefix_table", ctypes.c_void_p), ("prefix_pages", ctypes.c_uint32), ("prefix_len", ctypes.c_uint32)]
+
+
 def structs(change):
     """The two structs, and what of `change` is neither's."""
     rest = dict(change)
-    cache = ops._Cache(**{k: rest.pop(k, v) for k, v in CACHE.items()})
-    batch = ops._Batch(**{k: rest.pop(k, v) for k, v in BATCH.items()})
-    return cache, batch, rest
+    cache = Cache(**{k: rest.pop(k, v) for k, v in CACHE.items()})
+    batch = Batch(**{k: rest.pop(k, v) for k, v in BATCH.items()})
+    return bytes(cache), bytes(batch), rest
 
 
 def append(**change):
@@ -115,10 +127,11 @@ def test_constants_and_structs_are_the_headers():
     header = open(HEADER).read()
     for name, value in (("DF11_MIN_PAGE", ops.MIN_PAGE), ("DF11_MAX_PAGE", ops.MAX_PAGE)):
         assert re.search(rf"#define {name} (\d+)", header).group(1) == str(value)
-    for name, struct in (("df11_kv_cache", ops._Cache), ("df11_kv_batch", ops._Batch)):
+    for name, struct, packed in (("df11_kv_cache", Cache, ops._CACHE), ("df11_kv_batch", Batch, ops._BATCH)):
         body = re.findall(r"typedef struct \{([^}]*)\} " + name, header)[0]
-        fields = re.findall(r"\w+(?=\s*[,;])", body)
-        assert fields == [f for f, _ in struct._fields_]
+        assert re.findall(r"\w+(?=\s*[,;])", body) == [f for f, _ in struct._fields_]
+        values = range(1, len(struct._fields_) + 1)
+        assert packed.pack(*values) == bytes(struct(*values))
 
 
 def cpu_case():
@@ -134,20 +147,51 @@ def test_tensors_that_do_not_fit():
                  lambda: ops.kv_append(q, q[:, :128], q[:, :128], None, cache, batch)):
         with pytest.raises(ValueError, match="must be on a GPU"):
             call()
-    cpu = torch.device("cpu")
-    assert ops._kv_cache(cache, cpu).page_size == 16 and ops._kv_batch(batch, cpu).width == 3
+    def sizes(cache):
+        return ops._cache_sizes(ops._look(cache.k), ops._look(cache.v), -1)
+
+    def batch_sizes(**change):
+        return ops._batch_sizes(*map(ops._look, batch._replace(**change)[:4]), -1)
+
+    assert sizes(cache) == (1, 4, 2, 16, 64, 2048, 2048) and batch_sizes() == ((1, 3, 3), 0)
     k = cache.k
     for bad in (k.float(), k[0], k.transpose(1, 2), k[..., :32]):
         with pytest.raises(ValueError):
-            ops._kv_cache(ops.KVCache(bad, bad), cpu)
+            sizes(ops.KVCache(bad, bad))
     for bad in (k[:3], k.half(), k.transpose(2, 3)):
         with pytest.raises(ValueError, match="cache.v"):
-            ops._kv_cache(ops.KVCache(k, bad), cpu)
+            sizes(ops.KVCache(k, bad))
     for change in (dict(start=batch.start[:1]), dict(start=batch.start.long()), dict(length=batch.length[0]),
-                   dict(table=batch.table[0]), dict(table=batch.table.long()), dict(table=torch.zeros((2, 3)).int()),
-                   dict(table=batch.table.T), dict(prefix_table=batch.table.long()[0]), dict(prefix_len=-1),
-                   dict(prefix_len=2 ** 31), dict(prefix_table=batch.table)):
+                   dict(start=torch.zeros(4, dtype=torch.int32)[::2]), dict(table=batch.table[0]),
+                   dict(table=batch.table.long()), dict(table=torch.zeros((2, 3)).int()),
+                   dict(table=batch.table.T), dict(prefix_table=batch.table.long()[0]),
+                   dict(prefix_table=batch.table)):
         with pytest.raises(ValueError):
-            ops._kv_batch(batch._replace(**change), cpu)
+            batch_sizes(**change)
+    for length in (-1, 2 ** 31):
+        with pytest.raises(ValueError, match="prefix_len"):
+            ops._pack(cache, batch._replace(prefix_len=length), (1, 4, 2, 16, 64, 2048, 2048), (1, 3, 3), 0)
     with pytest.raises(ValueError, match="heads of 64"):
-        ops._heads(q[:, :100], 64, "q")
+        ops._heads(100, 64, "q")
+
+
+def sizes_of(**change):
+    """What kv_append makes of CPU tensors that would fit but for `change`."""
+    cache, batch = cpu_case()
+    q = torch.zeros((1, 256))
+    a = dict(index=-1, q=q, k=q[:, :128], v=q[:, :128], inv_freq=torch.zeros(32), q_out=None, cache_k=cache.k,
+             cache_v=cache.v, start=batch.start, length=batch.length, table=batch.table, prefix_table=None)
+    a = a | change
+    return ops._append_sizes(a.pop("index"), *map(ops._look, a.values()))
+
+
+def test_rows_that_do_not_fit():
+    q = torch.zeros((4, 256))
+    assert sizes_of()[3:] == (256, 128, 128, 0, 1, 4, 64, 256)
+    assert sizes_of(q=q[:1], k=q[:1, :128], v=q[:1, 128:], q_out=q[:1].half().bfloat16())[3:] == (
+        256, 128, 128, 0, 1, 4, 64, 256)
+    for change in (dict(q=q[0]), dict(q=q[:1, :100]), dict(q=q.T), dict(q=q[:1].double()), dict(k=q[:2, :128]),
+                   dict(k=q[:1, :64]), dict(v=q[:1, :128].half()), dict(v=q[:1, ::2]), dict(inv_freq=q[0].double()),
+                   dict(inv_freq=q[:2]), dict(q_out=q[:1]), dict(q_out=q[:1, :128].bfloat16()), dict(index=0)):
+        with pytest.raises(ValueError):
+            sizes_of(**change)
