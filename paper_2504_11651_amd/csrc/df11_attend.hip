@@ -21,6 +21,7 @@
 #include "df11_kv_common.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace {
 
@@ -115,11 +116,12 @@ __device__ inline Sequence sequence(const Batch &b, uint32_t s) {
     return {b.first(s), to, max(b.length[s], 0) - static_cast<int32_t>(to) + 1};
 }
 
-__device__ inline uint32_t swizzle64(uint32_t t) { return 2 * ((t >> 1) & 3) | ((t >> 3) & 1); }
-__device__ inline uint32_t swizzle128(uint32_t t) { return 2 * (t & 7) | ((t >> 3) & 1); }
+// Four neighbouring tokens 64 bytes apart, which the transposed reads take at once, and
+// each four 16 bytes further: no two lanes meet at a bank (counted: none; with the tokens
+// 16 or 32 bytes apart a third to a half of LDS' cycles are conflicts).
 template <uint32_t D>
 __device__ inline uint32_t swizzle(uint32_t t) {
-    return D == 64 ? swizzle64(t) : swizzle128(t);
+    return D == 64 ? (t & 2) * 2 | ((t >> 2) & 3) : (t & 3) * 4 | ((t >> 2) & 3);
 }
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -173,9 +175,9 @@ struct Worker {
     acc16 o[P::kBlocks];
     float m = -INFINITY, base = 0.0f, l = 0.0f;  // base: m where it is a number
 
-    __device__ Worker(const AttendArgs &args, uint32_t kvh_, bool split)
-        : a(args), at(threadIdx.x & 63, split ? threadIdx.x >> 1 & 32 : 0), lane(threadIdx.x & 63),
-          wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), kvh(kvh_) {
+    __device__ Worker(const AttendArgs &args, uint32_t thread, uint32_t kvh_, bool split)
+        : a(args), at(thread & 63, split ? thread >> 1 & 32 : 0), lane(thread & 63),
+          wave(__builtin_amdgcn_readfirstlane(thread >> 6)), kvh(kvh_) {
         head_off = (uint64_t{kvh} * D) << a.page_shift;
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; i++) {
@@ -210,25 +212,26 @@ struct Worker {
         v += 16 * wave * P::kRowBytes;
 #pragma unroll
         for (uint32_t i = 0; i < kLoads; i++) {
-            __builtin_amdgcn_global_load_lds((mem_void *)(kp + from[i]), (lds_void *)(k + i * 1024),
-                                             16, 0, 0);
-            __builtin_amdgcn_global_load_lds((mem_void *)(vp + from[i]), (lds_void *)(v + i * 1024),
-                                             16, 0, 0);
+            // 32 bits beside a base in scalar registers; widened before the loop it would be
+            // an addition of 64 bits a load
+            uint32_t off = from[i];
+            asm volatile("" : "+v"(off));
+            __builtin_amdgcn_global_load_lds((mem_void *)(kp + off), (lds_void *)(k + i * 1024), 16,
+                                             0, 0);
+            __builtin_amdgcn_global_load_lds((mem_void *)(vp + off), (lds_void *)(v + i * 1024), 16,
+                                             0, 0);
         }
         return !__any(numbers >= a.pages);
     }
-    // Waits for them, and clears the values of tokens behind the range: they meet a
-    // p of 0, and what memory holds there may be an infinity.
-    __device__ void landed(const Range &r, uint32_t tile, uint8_t *v) const {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (__builtin_expect(tile + kTile <= r.end, 1)) return;
-        uint32_t mine = lane;
-        asm volatile("" : "+v"(mine));  // nothing of this rare loop is kept in registers
-#pragma unroll
+    __device__ static void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+    // Clears the values of this wave's tokens behind the range: they meet a p of 0, and
+    // what memory holds there may be an infinity.
+    __device__ void clear(const Range &r, uint32_t tile, uint8_t *v) const {
+#pragma nounroll
         for (uint32_t i = 0; i < kLoads; i++) {
             constexpr uint32_t kLanes = 64 / kEach;
-            if (tile + 16 * wave + i * kEach + mine / kLanes >= r.end)
-                *reinterpret_cast<uint4 *>(v + 16 * wave * P::kRowBytes + i * 1024 + mine * 16) =
+            if (tile + 16 * wave + i * kEach + lane / kLanes >= r.end)
+                *reinterpret_cast<uint4 *>(v + 16 * wave * P::kRowBytes + i * 1024 + lane * 16) =
                     uint4{0, 0, 0, 0};
         }
     }
@@ -252,6 +255,15 @@ struct Worker {
             for (uint32_t b = 0; b < kCount; b++)
                 s[b] = Mat<C>::product(
                     *reinterpret_cast<const s8 *>(k + at.k[i] + b * 32 * P::kRowBytes), q[i], s[b]);
+        if constexpr (kCount == 2) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+            for (uint32_t i = 0; i < P::kSteps - 3; i++) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
+        }
     }
     // The softmax' step: p of them, in the order in which they meet the values.
     template <uint32_t kCount>
@@ -290,7 +302,9 @@ struct Worker {
     __device__ void tokens(const uint8_t *k, const uint8_t *v) {
         acc16 s[kCount];
         s8 p[2 * kCount];
+        __builtin_amdgcn_s_setprio(1);
         scores<kCount>(k, s);
+        __builtin_amdgcn_s_setprio(0);
         weigh<kCount>(s, p);
         products<kCount>(v, p);
     }
@@ -372,7 +386,11 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
     using P = Places<D>;
     // up to 64 rows: waves 2 i and 2 i + 1 take rows 32 i.. and share the tokens of a tile
     const bool split = rows <= 64;
-    W w(a, kvh, split);
+    // (its places are made anew for each tile of rows: kept over a loop around this they
+    // are spilled, and a spilled register is a round trip to memory)
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    W w(a, thread, kvh, split);
     const uint32_t half = w.lane >> 5, n = w.lane & 31;
     const uint32_t mine = 32 * (split ? w.wave >> 1 : w.wave);
     const bool busy = mine < rows;
@@ -398,33 +416,41 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
         // (page numbers behind the last tile: its own once more)
         bool fine = w.load(r, r.begin, w.pages(r, r.begin), k0, v0), odd = false;
         uint32_t next = w.pages(r, r.begin + kTile), t = r.begin;
-        w.landed(r, t, v0);
+        w.landed();
         __syncthreads();
-        // one tile is looked at while the next one is loaded
-        const auto step = [&](uint8_t *k, uint8_t *v, uint8_t *to_k, uint8_t *to_v) {
-            lost = lost || !fine;
-            const bool more = t + kTile < r.end;
-            if (more) fine = w.load(r, t + kTile, next, to_k, to_v);
-            next = w.pages(r, t + 2 * kTile);
-            if (busy) {
-                if (split)
-                    w.template tokens<1>(k, v);
-                else
-                    w.template tokens<2>(k, v);
+        // One tile is looked at while the next one is loaded.  (A loop for each kind of wave:
+        // where they meet in one, O is copied around in every turn.)
+        const auto loop = [&](auto count) {
+            const auto step = [&](uint8_t *k, uint8_t *v, uint8_t *to_k, uint8_t *to_v) {
+                lost = lost || !fine;
+                const bool more = t + kTile < r.end;
+                if (more) fine = w.load(r, t + kTile, next, to_k, to_v);
+                next = w.pages(r, t + 2 * kTile);
+                if constexpr (decltype(count)::value) w.template tokens<decltype(count)::value>(k, v);
+                t += kTile;
+                odd = !odd;
+                w.landed();
+                __syncthreads();
+            };
+            while (t < plain) {
+                step(k0, v0, k1, v1);
+                if (t >= plain) break;
+                step(k1, v1, k0, v0);
             }
-            t += kTile;
-            odd = !odd;
-            if (more) w.landed(r, t, to_v);
-            __syncthreads();
         };
-        while (t < plain) {
-            step(k0, v0, k1, v1);
-            if (t >= plain) break;
-            step(k1, v1, k0, v0);
-        }
+        if (!busy)
+            loop(std::integral_constant<uint32_t, 0>{});
+        else if (split)
+            loop(std::integral_constant<uint32_t, 1>{});
+        else
+            loop(std::integral_constant<uint32_t, 2>{});
         while (t < r.end) {
+            uint8_t *k = odd ? k1 : k0, *v = odd ? v1 : v0;
+            if (t + kTile > r.end) {
+                w.clear(r, t, v);
+                __syncthreads();
+            }
             if (busy) {
-                const uint8_t *k = odd ? k1 : k0, *v = odd ? v1 : v0;
                 const int32_t first = split ? 32 * (w.wave & 1) : 0;
 #pragma nounroll
                 for (uint32_t j = 0; j < (split ? 1 : 2); j++)
@@ -437,7 +463,7 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
             if (t >= r.end) break;
             fine = w.load(r, t, next, k0, v0);
             next = w.pages(r, t + kTile);
-            w.landed(r, t, v0);
+            w.landed();
             __syncthreads();
             odd = false;
         }
@@ -473,7 +499,7 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
     __syncthreads();
     constexpr uint32_t kPieces = D / 8;  // of a row: 8 values each
 #pragma nounroll
-    for (uint32_t i = threadIdx.x; i < rows * kPieces; i += kThreads) {
+    for (uint32_t i = thread; i < rows * kPieces; i += kThreads) {
         const uint32_t r = i / kPieces, piece = i % kPieces;
         const uint32_t src = split ? 2 * (r / 32) : r / 32, nn = r % 32;
         const float2 ml = stats[src * 32 + nn];
