@@ -598,28 +598,58 @@ struct Shares {
 __device__ inline uint32_t cost(uint32_t tiles) { return tiles ? kStart + tiles : 0; }
 __device__ inline uint32_t pieces(uint32_t n, uint32_t of) { return (n + of - 1) / of; }
 
-// Calls f(first sequence, this lane's units, units in front of this lane's) for 64
-// sequences after the other until it returns true.  All units, where it never does.
+// 64 sequences, one a lane: their rows, units, and the units of all sequences before.
+struct Lane {
+    Sequence q;
+    uint32_t units, before, most;  // most: tiles of the row that sees the most
+};
+__device__ inline Lane lane_of(const AttendArgs &a, uint32_t s0) {
+    const uint32_t s = s0 + (threadIdx.x & 63);
+    Lane y{};
+    if (s < a.batch.sequences) {
+        y.q = sequence(a.batch, s);
+        for (uint32_t i = 0; i < y.q.tiles(a); i++) {
+            y.most = y.q.token_tiles(a, i);  // later rows see more
+            y.units += cost(y.most);
+        }
+    }
+    return y;
+}
+// Calls f(first sequence, Lane) for 64 sequences after the other until it returns true.
+// All units, where it never does.
 template <class F>
 __device__ inline uint64_t each_64(const AttendArgs &a, F f) {
-    const uint32_t lane = threadIdx.x & 63;
     uint64_t all = 0;
     for (uint32_t s0 = 0; s0 < a.batch.sequences; s0 += 64) {
-        const uint32_t before = all;
-        uint32_t n = 0;
-        if (s0 + lane < a.batch.sequences) {
-            const Sequence q = sequence(a.batch, s0 + lane);
-            for (uint32_t i = 0; i < q.tiles(a); i++) n += cost(q.token_tiles(a, i));
-        }
-        uint32_t sum = n;
-        for (uint32_t d = 1; d < 64; d *= 2) {
-            const uint32_t y = __shfl_up(sum, d);
-            if (lane >= d) sum += y;
-        }
-        if (f(s0, n, before + sum - n)) break;
+        Lane y = lane_of(a, s0);
+        uint32_t sum = y.units;  // of the lanes up to this one
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x111, 0xF, 0xF, false);  // row_shr 1
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x112, 0xF, 0xF, false);
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x114, 0xF, 0xF, false);
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x118, 0xF, 0xF, false);
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x142, 0xA, 0xF, false);  // row_bcast 15
+        sum += __builtin_amdgcn_update_dpp(0, sum, 0x143, 0xC, 0xF, false);  // row_bcast 31
+        y.before = static_cast<uint32_t>(all) + sum - y.units;
+        if (f(s0, y)) break;
         all += __builtin_amdgcn_readlane(sum, 63);
     }
     return all;
+}
+// The lane's sequence that holds unit `to` of all, in every lane.
+struct Found {
+    uint32_t s, unit;
+    Sequence q;
+};
+__device__ inline bool find(uint32_t s0, const Lane &y, uint32_t to, Found *found) {
+    const uint64_t here = __ballot(y.before <= to && to < y.before + y.units);
+    if (!here) return false;
+    const uint32_t at = __builtin_ctzll(here);
+    found->s = s0 + at;
+    found->unit = to - __builtin_amdgcn_readlane(y.before, at);
+    found->q.from = __builtin_amdgcn_readlane(y.q.from, at);
+    found->q.to = __builtin_amdgcn_readlane(y.q.to, at);
+    found->q.before = __builtin_amdgcn_readlane(y.q.before, at);
+    return true;
 }
 
 // A workgroup takes one share.  It holds as many tiles as any other whatever the
@@ -632,12 +662,12 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
     // the units of all sequences, and the most tiles of a row
     Shares w{a.kv_heads * a.row_tiles * cost(a.front_tiles), 0, 0};
     uint32_t most = 0;
-    const uint64_t own_tiles = each_64(a, [&](uint32_t s0, uint32_t n, uint32_t before) {
-        if (s0 + lane < b.sequences) {
-            const Sequence q = sequence(b, s0 + lane);
-            if (n) most = max(most, q.token_tiles(a, q.tiles(a) - 1));
-            if (blockIdx.x == 0 && threadIdx.x < 64) a.sums[2 + s0 + lane] = before;
-        }
+    Lane y{};  // of up to 64 sequences: all of them
+    const uint64_t own_tiles = each_64(a, [&](uint32_t s0, const Lane &z) {
+        y = z;
+        most = max(most, z.most);
+        if (blockIdx.x == 0 && threadIdx.x < 64 && s0 + lane < b.sequences)
+            a.sums[2 + s0 + lane] = z.before;
         return false;
     });
     most = wave_max(most);
@@ -657,10 +687,29 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
     uint32_t at = share * w.size;
     const uint32_t end = min(at + w.size, w.front + a.kv_heads * w.own);
     if (at >= end) return;
-    uint32_t s = ~0u, i = 0, unit = 0, kvh = 0;  // own tokens: where `at` is
+    uint32_t s = ~0u, i = 0, own_unit = 0, kvh = 0;  // own tokens: where `at` is
     Sequence q{};
+    // own tokens from unit `to` of a head's on
+    const auto go = [&](uint32_t to, bool known) {
+        Found found{~0u, 0, {}};
+        if (known)
+            find(0, y, to, &found);
+        else
+            each_64(a, [&](uint32_t s0, const Lane &z) { return find(s0, z, to, &found); });
+        s = __builtin_amdgcn_readfirstlane(found.s);
+        q = found.q;
+        own_unit = found.unit;
+        for (i = 0; s != ~0u && own_unit >= cost(q.token_tiles(a, i)); i++)
+            own_unit -= cost(q.token_tiles(a, i));
+    };
+    // (known before the first tile of rows: not kept beyond it)
+    if (end > w.front && b.sequences <= 64) {
+        const uint32_t from = max(at, w.front) - w.front;
+        kvh = from / w.own;
+        go(from % w.own, true);
+    }
     while (at < end) {
-        uint32_t row0, rows, part, head, n, tiles;
+        uint32_t row0, rows, part, head, n, tiles, unit;
         int32_t least = INT32_MIN / 2;  // own tokens that the first row sees: none
         Range front{}, own{};
         if (at < w.front) {
@@ -674,21 +723,10 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
         } else {
             if (s == ~0u) {
                 kvh = (at - w.front) / w.own;
-                const uint32_t to = (at - w.front) % w.own;
-                each_64(a, [&](uint32_t s0, uint32_t n, uint32_t before) {
-                    const uint64_t here = __ballot(before <= to && to < before + n);
-                    if (!here) return false;
-                    const uint32_t at = __builtin_ctzll(here);
-                    s = s0 + at;
-                    unit = to - __builtin_amdgcn_readlane(before, at);
-                    return true;
-                });
-                s = __builtin_amdgcn_readfirstlane(s);
+                go((at - w.front) % w.own, false);
                 if (s == ~0u) return;
-                q = sequence(b, s);
-                for (i = 0; unit >= cost(q.token_tiles(a, i)); i++)
-                    unit -= cost(q.token_tiles(a, i));
             }
+            unit = own_unit;
             tiles = q.token_tiles(a, i);
             head = kvh;
             row0 = q.first_row(a, i);
@@ -714,9 +752,9 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
                                 stats, &left_out);
         }
         at += n;
-        if (s == ~0u || at >= end) continue;
+        if (at <= w.front || at >= end) continue;
         // on to the next tile of rows that sees something
-        unit = 0;
+        own_unit = 0;
         do i++;
         while (i < q.tiles(a) && !q.token_tiles(a, i));
         if (i < q.tiles(a)) continue;
@@ -739,30 +777,47 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
     }
 }
 
-// The parts of the prefix and of own tokens that a row's head has: those of the prefix
-// are 0.., of own tokens front_parts...
+// A row's sequence, and the parts of the prefix and of own tokens that a head of it has:
+// those of the prefix are 0.., of own tokens front_parts...
 struct Parts {
     uint32_t front, own;
 };
-__device__ inline Parts parts_of(const AttendArgs &a, uint32_t token, uint32_t head, uint32_t s) {
+__device__ inline bool parts_of(const AttendArgs &a, uint32_t token, uint32_t head, Parts *p) {
     const uint32_t kvh = head / a.group, row = token * a.group + head % a.group;
-    const uint32_t size = a.sums[0], own = a.sums[1];
+    const uint32_t size = a.sums[0], all = a.sums[1];
+    uint32_t before;
+    Sequence q;
+    if (a.batch.sequences <= 64) {
+        // one round of loads for all that is asked
+        const uint32_t lane = threadIdx.x & 63, s = min(lane, a.batch.sequences - 1);
+        const Sequence y = sequence(a.batch, s);
+        const uint32_t sum = a.sums[2 + s];
+        const uint64_t here = __ballot(lane == s && y.from <= token && token < y.to);
+        if (!here) return false;
+        const uint32_t at = __builtin_ctzll(here);
+        q.from = __builtin_amdgcn_readlane(y.from, at);
+        q.to = __builtin_amdgcn_readlane(y.to, at);
+        q.before = __builtin_amdgcn_readlane(y.before, at);
+        before = __builtin_amdgcn_readlane(sum, at);
+    } else {
+        const Owner o = owner(a.batch, token);
+        if (o.s == ~0u) return false;
+        q = sequence(a.batch, o.s);
+        before = a.sums[2 + o.s];
+    }
     const uint32_t each = cost(a.front_tiles);
-    Parts p{0, 0};
+    *p = {0, 0};
     if (each) {
         const uint32_t at = (kvh * a.row_tiles + row / kRows) * each + kStart;
-        p.front = (at + a.front_tiles - 1) / size - at / size + 1;
+        p->front = min((at + a.front_tiles - 1) / size - at / size + 1, a.front_parts);
     }
-    const Sequence q = sequence(a.batch, s);
     const uint32_t i = (row - q.from * a.group) / kRows, n = q.token_tiles(a, i);
     if (n) {
-        uint32_t at = a.kv_heads * a.row_tiles * each + kvh * own + a.sums[2 + s] + kStart;
+        uint32_t at = a.kv_heads * a.row_tiles * each + kvh * all + before + kStart;
         for (uint32_t j = 0; j < i; j++) at += cost(q.token_tiles(a, j));
-        p.own = (at + n - 1) / size - at / size + 1;
+        p->own = min((at + n - 1) / size - at / size + 1, a.own_parts);
     }
-    p.front = min(p.front, a.front_parts);
-    p.own = min(p.own, a.own_parts);
-    return p;
+    return true;
 }
 
 // Joins the parts of a row and head: kWaves waves for each, several parts at a time.
@@ -775,12 +830,20 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = wave / kWaves;
     const uint32_t at = __builtin_amdgcn_readfirstlane(blockIdx.x * (4 / kWaves) + mine);
     const uint32_t token = at / a.heads, head = at % a.heads;
-    const Owner o = token < a.batch.rows ? owner(a.batch, token) : Owner{~0u, 0};
-    if (o.s == ~0u) return;  // (with kWaves = 4 all waves)
-    const Parts n = parts_of(a, token, head, o.s);
+    Parts n;
+    if (token >= a.batch.rows || !parts_of(a, token, head, &n)) return;  // (kWaves = 4: all waves)
     const uint32_t parts = n.front + n.own, skip = a.front_parts - n.front;
     const uint64_t each = uint64_t{a.batch.rows} * a.heads;
     const auto slot = [&](uint32_t i) { return (i < n.front ? i : i + skip) * each + at; };
+    const uint32_t sub = wave % kWaves * kAtOnce + lane / kLanes, col = lane % kLanes * 4;
+    constexpr uint32_t kStep = kWaves * kAtOnce;
+    const auto value = [&](uint32_t i) {
+        return *reinterpret_cast<const float4 *>(a.part_o + slot(i) * D + col);
+    };
+    // the first values are asked for with the bounds and sums
+    float4 first[2];
+    for (uint32_t e = 0; e < 2; e++)
+        first[e] = sub + e * kStep < parts ? value(sub + e * kStep) : float4{0.0f, 0.0f, 0.0f, 0.0f};
     float2 ml[kRounds];
     float m = -INFINITY, l = 0.0f;
     for (uint32_t i = 0; i < kRounds && 64 * i < parts; i++) {
@@ -799,16 +862,13 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    const uint32_t sub = wave % kWaves * kAtOnce + lane / kLanes, col = lane % kLanes * 4;
-    constexpr uint32_t kStep = kWaves * kAtOnce;
-    const auto value = [&](uint32_t i) {
-        return *reinterpret_cast<const float4 *>(a.part_o + slot(i) * D + col);
-    };
     float4 x = {0.0f, 0.0f, 0.0f, 0.0f};
     const auto add = [&](float w, const float4 &y) {
         x.x += w * y.x, x.y += w * y.y, x.z += w * y.z, x.w += w * y.w;
     };
-    uint32_t i = sub;
+    for (uint32_t e = 0; e < 2; e++)
+        if (sub + e * kStep < parts) add(weights[mine][sub + e * kStep], first[e]);
+    uint32_t i = sub + 2 * kStep;
     for (; i + 3 * kStep < parts; i += 4 * kStep) {
         float4 y[4];
         for (uint32_t e = 0; e < 4; e++) y[e] = value(i + e * kStep);
@@ -876,7 +936,7 @@ int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_
     p->front_parts = parts(p->front_tiles, tiles * c.heads, 1);
     p->own_parts = parts(own, own_tiles * c.heads, std::min<uint64_t>(64, (64u << 20) / part_bytes));
     const uint64_t all = c.heads * (tiles * (p->front_tiles + kStart) + own_tiles * (own + kStart));
-    p->grid = kSlots;
+    p->grid = std::min<uint64_t>(kSlots, up(all, 2) * 2);
     p->joins = tokens * heads;
     if (all >> 32 || up(p->joins, 4) >= kMaxGrid) return DF11_E_UNSUPPORTED;
     p->bytes = (p->front_parts + p->own_parts) * part_bytes + 4 * up(2 + b.sequences, 4) * 4;
