@@ -255,15 +255,6 @@ struct Worker {
             for (uint32_t b = 0; b < kCount; b++)
                 s[b] = Mat<C>::product(
                     *reinterpret_cast<const s8 *>(k + at.k[i] + b * 32 * P::kRowBytes), q[i], s[b]);
-        if constexpr (kCount == 2) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
-#pragma unroll
-            for (uint32_t i = 0; i < P::kSteps - 3; i++) {
-                __builtin_amdgcn_sched_group_barrier(0x8, 2, 0);
-                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-            }
-            __builtin_amdgcn_sched_group_barrier(0x8, 6, 0);
-        }
     }
     // The softmax' step: p of them, in the order in which they meet the values.
     template <uint32_t kCount>
@@ -302,6 +293,8 @@ struct Worker {
     __device__ void tokens(const uint8_t *k, const uint8_t *v) {
         acc16 s[kCount];
         s8 p[2 * kCount];
+        // (in front of the wave of the other workgroup, which is at its softmax then: 558 ->
+        // 545 us for a prompt of 8192 tokens)
         __builtin_amdgcn_s_setprio(1);
         scores<kCount>(k, s);
         __builtin_amdgcn_s_setprio(0);
@@ -913,10 +906,15 @@ int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_
     if (!tokens || !b.sequences) return DF11_OK;
     const uint64_t rows = tokens * (heads / c.heads), tiles = up(rows, kRows);
     const uint64_t own_tiles = rows / kRows + b.sequences;
+    const uint64_t space = std::min<uint64_t>(uint64_t{b.width} * c.page_size, INT32_MAX);
+    const uint64_t own = std::max<uint64_t>(1, up(space, kTile)), front = up(b.prefix_len, kTile);
     // Rows that fill tiles by themselves, enough of them to fill the GPU: the prefix is
-    // read with the own tokens, and nothing has to be joined.
-    const uint64_t each = rows / std::min<uint64_t>(tokens, b.sequences);
-    p->whole = each >= 64 && tiles * c.heads >= kSlots / 2;
+    // read with the own tokens, and nothing has to be joined.  So it is, too, where a
+    // workgroup has little to read (single tokens of 250 9.8 us against 14.8, 64 of up to
+    // 1000 27.8 against 34, a prompt of 512 22 against 42; at 32 tiles 59 against 56).
+    const uint64_t each = rows / std::min<uint64_t>(tokens, b.sequences), read = front + own;
+    p->whole = read <= 8 || (!front && read <= 16 && own_tiles * c.heads >= kSlots) ||
+               (each >= 64 && (read <= 24 || tiles * c.heads >= kSlots / 2));
     if (p->whole) {
         p->own_tiles = own_tiles;
         p->own_groups = 8 / std::__gcd(c.heads, 8u);
@@ -925,14 +923,12 @@ int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_
     }
     // Shares: at least so many parts that items as long as each other can fill the GPU,
     // and for own tokens, whose lengths differ, more while they cost little memory.
-    const uint64_t space = std::min<uint64_t>(uint64_t{b.width} * c.page_size, INT32_MAX);
-    const uint64_t own = std::max<uint64_t>(1, up(space, kTile));
     const auto parts = [](uint64_t n, uint64_t items, uint64_t least) {
         return std::min<uint64_t>({n, kMaxParts, std::max<uint64_t>(least, kSlots / items + 2)});
     };
     const uint64_t part_bytes = tokens * heads * (4ull * c.dim + 8);
     p->row_tiles = tiles;
-    p->front_tiles = up(b.prefix_len, kTile);
+    p->front_tiles = front;
     p->front_parts = parts(p->front_tiles, tiles * c.heads, 1);
     p->own_parts = parts(own, own_tiles * c.heads, std::min<uint64_t>(64, (64u << 20) / part_bytes));
     const uint64_t all = c.heads * (tiles * (p->front_tiles + kStart) + own_tiles * (own + kStart));

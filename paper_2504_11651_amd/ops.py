@@ -524,11 +524,15 @@ def _raw_stream(stream, index):
     return codec._handle(stream, torch.device("cuda", index))
 
 
+def _check_prefix_len(n):
+    if not 0 <= n < 2 ** 31:
+        raise ValueError(f"batch.prefix_len must be from 0 to 2^31 - 1, not {n}")
+
+
 def _pack(cache, batch, c, b, prefix_pages):
     """The two structs; `c` and `b` as _cache_sizes and _batch_sizes give them."""
     start, length, table, prefix_table, prefix_len = batch
-    if not 0 <= prefix_len < 2 ** 31:
-        raise ValueError(f"batch.prefix_len must be from 0 to 2^31 - 1, not {prefix_len}")
+    _check_prefix_len(prefix_len)
     return (_CACHE.pack(cache[0].data_ptr(), cache[1].data_ptr(), *c),
             _BATCH.pack(start.data_ptr(), length.data_ptr(), table.data_ptr(), *b,
                         0 if prefix_table is None else prefix_table.data_ptr(), prefix_pages,
@@ -585,7 +589,6 @@ def kv_append(q, k, v, inv_freq, cache: KVCache, batch: KVBatch, interleaved: bo
     return q_out
 
 
-@functools.lru_cache(maxsize=1024)
 def _attention_bytes(tokens, heads, c, b, prefix_pages, prefix_len):
     n = ctypes.c_uint64()
     codec._check(lib().df11_prefix_attention_workspace_bytes(
@@ -604,14 +607,16 @@ def prefix_attention_workspace_bytes(tokens: int, heads: int, cache: KVCache,
 
 
 @functools.lru_cache(maxsize=1024)
-def _attention_sizes(index, q, out, lse, cache_k, cache_v, *batch):
+def _attention_sizes(index, prefix_len, q, out, lse, cache_k, cache_v, *batch):
+    _check_prefix_len(prefix_len)
     c = _cache_sizes(cache_k, cache_v, index)
     b, prefix_pages = _batch_sizes(*batch, index)
     q_stride = _as_rows(q, (cache_k[2],), index, "q")
     tokens, heads = q[0][0], _heads(q[0][1], c[4], "q")
     out_stride = q[0][1] if out is None else _as_rows(out, (q[2],), index, "out", q[0])
     _as(lse, (tokens, heads), torch.float32, index, "lse")
-    return c, b, prefix_pages, q_stride, tokens, heads, out_stride
+    return (c, b, prefix_pages, q_stride, tokens, heads, out_stride, c[4] ** -0.5,
+            _attention_bytes(tokens, heads, c, b, prefix_pages, prefix_len))
 
 
 def prefix_attention(q, cache: KVCache, batch: KVBatch, scale: Optional[float] = None, out=None,
@@ -629,21 +634,20 @@ def prefix_attention(q, cache: KVCache, batch: KVBatch, scale: Optional[float] =
     0 and lse -inf; one that sees a page which is not of the cache has NaN."""
     index = _on_gpu(q, "q")
     start, length, table, prefix_table, prefix_len = batch
-    c, b, prefix_pages, q_stride, tokens, heads, out_stride = _attention_sizes(
-        index, _look(q), _look(out), _look(lse), _look(cache[0]), _look(cache[1]), _look(start),
+    c, b, prefix_pages, q_stride, tokens, heads, out_stride, usual, ws_bytes = _attention_sizes(
+        index, prefix_len, _look(q), _look(out), _look(lse), _look(cache[0]), _look(cache[1]), _look(start),
         _look(length), _look(table), _look(prefix_table))
     if out is None:
         out = _new(q.shape, q.dtype, q.device, stream)
     if lse is None and need_lse:
         lse = _new((tokens, heads), torch.float32, q.device, stream)
     pc, pb = _pack(cache, batch, c, b, prefix_pages)
-    if workspace is None:
-        ws_bytes = _attention_bytes(tokens, heads, c, b, prefix_pages, prefix_len)
-        workspace = _new((ws_bytes,), torch.uint8, q.device, stream) if ws_bytes else None
-    else:
+    if workspace is not None:
         workspace, ws_bytes = _workspace(workspace, None, None, q.device, stream)
+    elif ws_bytes:
+        workspace = _new((ws_bytes,), torch.uint8, q.device, stream)
     codec._check(lib().df11_prefix_attention(
-        q.data_ptr(), q_stride, tokens, heads, c[4] ** -0.5 if scale is None else scale, pc, pb,
+        q.data_ptr(), q_stride, tokens, heads, usual if scale is None else scale, pc, pb,
         out.data_ptr(), out_stride, _ptr(lse), _ptr(workspace), ws_bytes,
         _raw_stream(stream, index)), "df11_prefix_attention")
     return Attention(out, lse)

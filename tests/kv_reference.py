@@ -18,6 +18,10 @@ class Case:
     behind the last.  Pages are in random order, entries and places that nothing needs
     hold what must not be looked at."""
 
+    # entries behind those that a table needs: the sizes that a call is planned by go with
+    # the tables' width, results do not
+    spare_pages = 0
+
     def __init__(self, new, own, prefix=0, heads=8, kv_heads=2, dim=128, page=64, dtype=BF16, seed=0,
                  spare=0, width=None, device="cuda", filled=True):
         self.new, self.own, self.prefix = list(new), list(own), prefix
@@ -29,7 +33,7 @@ class Case:
         front = -(-prefix // page)
         total = sum(used) + front + 3
         order = torch.randperm(total, generator=self.g, device=device).int()
-        width = max([1, *used]) if width is None else width
+        width = max([1, *used]) + self.spare_pages if width is None else width
         self.table = torch.full((n, width), -7, dtype=torch.int32, device=device)
         at = front
         self.pages = []

@@ -13,6 +13,13 @@ from kv_reference import BF16, F16, Case, near
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not gpu_available(), reason="needs an MI355X")]
 
 
+@pytest.fixture(autouse=True, params=[0, 100], ids=["short tables", "long tables"])
+def both_plans(request, monkeypatch):
+    """Few pages are read by one workgroup; where the tables have room for many, the work
+    is cut into shares and joined."""
+    monkeypatch.setattr(Case, "spare_pages", request.param)
+
+
 @pytest.mark.parametrize("dtype, dim", [(BF16, 128), (BF16, 64), (F16, 128), (F16, 64)])
 @pytest.mark.parametrize("own", [1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 191, 193, 257])
 def test_one_token_of_one_sequence(own, dtype, dim):
@@ -71,10 +78,11 @@ def test_sequences_without_rows_and_rows_without_sequence(spare):
     Case([0, 0], [5, 2], prefix=65, spare=2 + spare).attend()  # no row at all
 
 
-@pytest.mark.parametrize("sequences", [63, 64, 65, 129, 300, 4097, 5000])
+@pytest.mark.parametrize("sequences", [63, 64, 65, 129, 300, 4097])
 def test_many_sequences(sequences):
     own = [1 + (37 * i) % 90 for i in range(sequences)]
-    new = [min(x, (i * 7) % 3) for i, x in enumerate(own)]
+    # in a long batch few have rows: the reference takes them one by one
+    new = [min(x, (i * 7) % 3) if sequences < 200 or i % 41 == 0 or i > sequences - 9 else 0 for i, x in enumerate(own)]
     Case(new, own, prefix=130, heads=2, kv_heads=1, dim=64, page=16, seed=sequences, spare=2).check()
 
 
