@@ -253,7 +253,8 @@ int df11_kv_append(const void *q, uint64_t q_stride, const void *k, uint64_t k_s
  *   q, out     tokens x heads * dim of the cache's type, strides in elements, rows
  *              16-byte aligned; out may be q itself (with its stride);
  *   lse        tokens x heads floats, may be null;
- *   heads      a multiple of cache.heads; tokens * heads < 2^31; scale > 0.
+ *   heads      a multiple of cache.heads; tokens * heads < 2^31; scale a normal
+ *              number above 0.
  * The rows of all sequences read the prefix together, once.  Products are summed in
  * 32 bits on the matrix cores, the softmax is held in 32 bits; exp(s_j - m) is
  * rounded to the cache's type where it meets v.

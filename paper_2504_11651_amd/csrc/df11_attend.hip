@@ -197,10 +197,9 @@ struct Worker {
         const uint32_t at = min(tile + 16 * (lane & 3), r.end - 1) >> a.page_shift;
         return at < r.width ? static_cast<uint32_t>(r.table[at]) : ~0u;
     }
-    // Loads this wave's 16 tokens of a tile into LDS, past the registers.  True: the
-    // tile's tokens lie on pages of the cache; where they do not, those of another page
-    // are loaded in their place.
-    __device__ bool load(const Range &r, uint32_t tile, uint32_t numbers, uint8_t *k,
+    // Loads this wave's 16 tokens of a tile into LDS, past the registers.  Bit i: tokens
+    // 16 i.. of the tile lie on no page of the cache; another's are loaded in their place.
+    __device__ uint32_t load(const Range &r, uint32_t tile, uint32_t numbers, uint8_t *k,
                          uint8_t *v) const {
         uint32_t page = __builtin_amdgcn_readlane(numbers, wave);
         if (page >= a.pages) page = 0;
@@ -221,7 +220,7 @@ struct Worker {
             __builtin_amdgcn_global_load_lds((mem_void *)(vp + off), (lds_void *)(v + i * 1024), 16,
                                              0, 0);
         }
-        return !__any(numbers >= a.pages);
+        return __ballot(numbers >= a.pages) & 15;
     }
     __device__ static void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
     // Clears the values of this wave's tokens behind the range: they meet a p of 0, and
@@ -302,10 +301,12 @@ struct Worker {
         products<kCount>(v, p);
     }
 
-    // 32 tokens of which the lane's row sees the first `seen`, or of a page outside the
-    // cache (not `fine`).  A value that is an infinity or a NaN must not meet the p of 0 of
-    // a row that does not see it: those are left out, and true comes back if there are any.
-    __device__ bool tokens_of_some(const uint8_t *k, const uint8_t *v, int32_t seen, bool fine) {
+    // 32 tokens of which the lane's row sees the first `seen`; bit i of `lost`: tokens 16 i..
+    // are of no page of the cache.  A value that is an infinity or a NaN must not meet the
+    // p of 0 of a row that does not see it: those are left out, and true comes back if there
+    // are any.
+    __device__ bool tokens_of_some(const uint8_t *k, const uint8_t *v, int32_t seen,
+                                   uint32_t lost) {
         acc16 s[1];
         s8 p[2];
         scores<1>(k, s);
@@ -313,7 +314,7 @@ struct Worker {
 #pragma unroll
         for (uint32_t e = 0; e < 16; e++) {
             const int32_t t = 8 * (e / 4) + e % 4;
-            s[0][e] = t >= seen ? -INFINITY : fine ? s[0][e] : NAN;
+            s[0][e] = t >= seen ? -INFINITY : lost >> (e / 8) & 1 ? NAN : s[0][e];
         }
         weigh<1>(s, p);
         u4 bad = {0, 0, 0, 0};
@@ -322,10 +323,10 @@ struct Worker {
 #pragma unroll
             for (uint32_t b = 0; b < P::kBlocks; b++) {
                 const s8 x = read_v(v + i * 16 * P::kRowBytes, at.v[b][0], at.v[b][1]);
-                const u4 lost = not_finite(x);
-                bad |= lost;
+                const u4 out = not_finite(x);
+                bad |= out;
                 // 0 for 1, all bits for 0
-                const us8 keep = __builtin_bit_cast(us8, lost) - static_cast<unsigned short>(1);
+                const us8 keep = __builtin_bit_cast(us8, out) - static_cast<unsigned short>(1);
                 o[b] = Mat<C>::product(x & __builtin_bit_cast(s8, keep), p[i], o[b]);
             }
         return __any((bad[0] | bad[1] | bad[2] | bad[3]) != 0);
@@ -407,7 +408,8 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
         const int32_t sees = i ? min(places + later, end) : end;
         const uint32_t plain = least & ~(kTile - 1);  // tiles before it: no row is masked
         // (page numbers behind the last tile: its own once more)
-        bool fine = w.load(r, r.begin, w.pages(r, r.begin), k0, v0), odd = false;
+        uint32_t none = w.load(r, r.begin, w.pages(r, r.begin), k0, v0);
+        bool odd = false;
         uint32_t next = w.pages(r, r.begin + kTile), t = r.begin;
         w.landed();
         __syncthreads();
@@ -415,9 +417,9 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
         // where they meet in one, O is copied around in every turn.)
         const auto loop = [&](auto count) {
             const auto step = [&](uint8_t *k, uint8_t *v, uint8_t *to_k, uint8_t *to_v) {
-                lost = lost || !fine;
+                lost = lost || none;
                 const bool more = t + kTile < r.end;
-                if (more) fine = w.load(r, t + kTile, next, to_k, to_v);
+                if (more) none = w.load(r, t + kTile, next, to_k, to_v);
                 next = w.pages(r, t + 2 * kTile);
                 if constexpr (decltype(count)::value) w.template tokens<decltype(count)::value>(k, v);
                 t += kTile;
@@ -444,17 +446,18 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
                 __syncthreads();
             }
             if (busy) {
-                const int32_t first = split ? 32 * (w.wave & 1) : 0;
+                const uint32_t first = split ? w.wave & 1 : 0;
 #pragma nounroll
                 for (uint32_t j = 0; j < (split ? 1 : 2); j++)
                     if (w.tokens_of_some(k + 32 * j * P::kRowBytes, v + 32 * j * P::kRowBytes,
-                                         sees - static_cast<int32_t>(t + 32 * j) - first, fine))
+                                         sees - static_cast<int32_t>(t + 32 * (first + j)),
+                                         none >> 2 * (first + j)))
                         *left_out = 1;
             }
             t += kTile;
             __syncthreads();
             if (t >= r.end) break;
-            fine = w.load(r, t, next, k0, v0);
+            none = w.load(r, t, next, k0, v0);
             next = w.pages(r, t + kTile);
             w.landed();
             __syncthreads();
@@ -984,7 +987,8 @@ int df11_prefix_attention(const void *q, uint64_t q_stride, uint64_t tokens, uin
     if (!rc) rc = check_batch(batch);
     if (!rc) rc = plan_of(tokens, heads, *cache, *batch, &p);
     if (rc) return rc;
-    if (!(scale > 0.0f) || !(scale * kLog2e < INFINITY)) return DF11_E_INVALID_ARG;
+    // (a c below the normal numbers would be taken for 0)
+    if (!(scale >= 1.17549435e-38f) || !(scale * kLog2e < INFINITY)) return DF11_E_INVALID_ARG;
     if (!tokens || !batch->sequences) return DF11_OK;
     if (batch->prefix_len &&
         (!batch->prefix_table || misaligned(batch->prefix_table, 4) ||

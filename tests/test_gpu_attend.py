@@ -38,7 +38,7 @@ def test_page_sizes(page):
 
 
 @pytest.mark.parametrize("heads, kv_heads", [(1, 1), (3, 3), (3, 1), (7, 1), (12, 4), (28, 4), (40, 8), (33, 11),
-                                             (64, 8), (64, 1), (66, 1), (142, 2), (16, 16)])
+                                             (64, 8), (64, 1), (66, 1), (142, 2), (200, 1), (16, 16)])
 def test_head_layouts(heads, kv_heads):
     Case([1, 3, 2, 1], [70, 3, 200, 1], prefix=150, heads=heads, kv_heads=kv_heads, seed=heads).check()
     Case([1] * 40, [1 + 7 * i for i in range(40)], prefix=70, heads=heads, kv_heads=kv_heads, dim=64, dtype=F16,
@@ -196,6 +196,20 @@ def test_pages_outside_the_cache(new, own, prefix, heads, kv_heads, page, wrong)
     assert got.out.isnan().all() and got.lse.isnan().all()
 
 
+@pytest.mark.parametrize("hurt", [0, 1, 2, 3, 4, 5, 6])
+def test_pages_outside_the_cache_among_rows_of_a_tile(hurt):
+    """One head, so that a hundred rows share their tiles: those in front of the page have
+    all of their result."""
+    c = Case([100, 7], [100, 107], heads=2, kv_heads=2, page=16, seed=hurt)
+    clean = c.attend()
+    c.table[0, hurt] = -1
+    got = c.attend()
+    for name in ("out", "lse"):
+        a, b = getattr(got, name), getattr(clean, name)
+        assert torch.equal(a[:16 * hurt], b[:16 * hurt]) and a[16 * hurt:100].isnan().all(), name
+        assert torch.equal(a[100:], b[100:]), name
+
+
 def test_places_past_the_tables_width():
     c = Case([4, 1], [130, 20], prefix=10, page=16, width=8, seed=8)
     got = c.attend()
@@ -274,6 +288,17 @@ def test_in_place(new, own):
     assert torch.equal(c.q[:rows], want.out[:rows]) and torch.equal(c.q[rows:], q[rows:])
 
 
+def test_pages_that_sequences_share():
+    """A sequence forked from another: the same pages in two tables, and the prefix' pages
+    in a table of their own, each as if it had a copy."""
+    c = Case([2, 2, 1], [300, 300, 90], prefix=130, seed=17)
+    c.table[1] = c.table[0]
+    c.pages[1], c.sets[2] = c.pages[0], c.sets[1]
+    c.table[2, :2] = c.prefix_table[:2]
+    c.sets[3] = [x[:90] for x in c.sets[0]]
+    c.check()
+
+
 def test_far_pages():
     """Pages whose offsets pass 2^32 elements."""
     page, stride = 64, 1 << 31
@@ -296,6 +321,22 @@ def test_the_same_bits_every_time():
         for _ in range(5):
             again = c.attend()
             assert torch.equal(again.out, first.out) and torch.equal(again.lse, first.lse)
+
+
+def test_two_streams_at_once():
+    """Two batches under way together, with a workspace each."""
+    cases = [Case([1, 2, 1], [900, 200, 3000], prefix=900 + i, seed=18 + i) for i in range(2)]
+    want = [c.attend() for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i, c in enumerate(cases):
+            got[i].append(ops.prefix_attention(c.q, c.cache, c.batch, need_lse=True, stream=streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for x in got[i]:
+            assert torch.equal(x.out, want[i].out) and torch.equal(x.lse, want[i].lse)
 
 
 def test_a_workspace_given_and_on_a_stream():

@@ -14,7 +14,7 @@ from test_ops_host import A, INVALID, SMALL, UNSUPPORTED
 HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "df11_ops.h")
 CACHE = dict(k=A, v=A, dtype=1, pages=10, heads=2, page_size=64, dim=128, k_stride=2 * 64 * 128,
              v_stride=2 * 64 * 128)
-BATCH = dict(start=A, length=A, table=A, sequences=3, width=4, table_stride=4, prefix_table=A, prefix_pages=2,
+BATCH = dict(start=A, length=A, table=A, sequences=3, width=100, table_stride=100, prefix_table=A, prefix_pages=2,
              prefix_len=128)
 
 
@@ -69,7 +69,7 @@ NOTHING = dict(tokens=0)  # what is right with it launches nothing
     (dict(v_stride=2 * 64 * 128 + 4), INVALID), (dict(k_stride=1 << 41), INVALID),
     (dict(heads=1 << 20, page_size=1024, k_stride=1 << 38, v_stride=1 << 38), INVALID),
     (dict(start=None), INVALID), (dict(length=None), INVALID), (dict(table=None), INVALID),
-    (dict(start=A + 2), INVALID), (dict(table_stride=3), INVALID), (dict(sequences=(1 << 24) + 1), INVALID),
+    (dict(start=A + 2), INVALID), (dict(table_stride=99), INVALID), (dict(sequences=(1 << 24) + 1), INVALID),
     (dict(prefix_len=2 ** 31), INVALID), (dict(q=None), INVALID), (dict(q=A + 8), INVALID),
     (dict(q_stride=1023), INVALID), (dict(q_stride=1028 - 3), INVALID), (dict(q_stride=512), INVALID),
     (dict(out_stride=512), INVALID), (dict(out_stride=1028), INVALID), (dict(q_heads=0), INVALID),
@@ -97,6 +97,7 @@ def test_append_refusals(change, rc):
 
 @pytest.mark.parametrize("change, rc", [
     (dict(q_heads=7), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
+    (dict(scale=1e-40), INVALID), (dict(NOTHING, scale=2.0 ** -126), 0),
     (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=3e38), INVALID),
     (dict(prefix_table=None), INVALID), (dict(prefix_table=A + 2), INVALID), (dict(prefix_len=129), INVALID),
     (dict(out=None), INVALID), (dict(out=2 * A, out_stride=2048), INVALID), (dict(lse=A + 2), INVALID),
