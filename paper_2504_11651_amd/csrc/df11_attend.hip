@@ -820,7 +820,7 @@ __device__ inline bool parts_of(const AttendArgs &a, uint32_t token, uint32_t he
 template <class C, uint32_t D, uint32_t kWaves>
 __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
     constexpr uint32_t kLanes = D / 4, kAtOnce = 64 / kLanes;  // lanes of a part
-    constexpr uint32_t kRounds = 2 * kMaxParts / 64;
+    __shared__ float2 stats[4 / kWaves][2 * kMaxParts];
     __shared__ float weights[4 / kWaves][2 * kMaxParts];
     __shared__ float4 sums[4][kLanes];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = wave / kWaves;
@@ -836,23 +836,24 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
     const auto value = [&](uint32_t i) {
         return *reinterpret_cast<const float4 *>(a.part_o + slot(i) * D + col);
     };
-    // the first values are asked for with the bounds and sums
-    float4 first[2];
-    for (uint32_t e = 0; e < 2; e++)
-        first[e] = sub + e * kStep < parts ? value(sub + e * kStep) : float4{0.0f, 0.0f, 0.0f, 0.0f};
-    float2 ml[kRounds];
+    // The first values are asked for with the bounds and sums.  (Loops that are not
+    // unrolled: a kernel begins with no code in the instruction cache, and what it runs once
+    // costs about a microsecond a kilobyte.)
+    const float4 none = {0.0f, 0.0f, 0.0f, 0.0f}, first = sub < parts ? value(sub) : none;
     float m = -INFINITY, l = 0.0f;
-    for (uint32_t i = 0; i < kRounds && 64 * i < parts; i++) {
-        const uint32_t p = 64 * i + lane;
-        ml[i] = p < parts ? a.part_ml[slot(p)] : float2{-INFINITY, 0.0f};
-        m = fmaxf(m, ml[i].x);
+#pragma nounroll
+    for (uint32_t i = lane; i < parts; i += 64) {
+        const float2 ml = a.part_ml[slot(i)];
+        stats[mine][i] = ml;  // kWaves = 4: each wave writes the same
+        m = fmaxf(m, ml.x);
     }
     m = wave_max(m);
     const float base = m == -INFINITY ? 0.0f : m;
-    for (uint32_t i = 0; i < kRounds && 64 * i < parts; i++) {
-        const float w = __builtin_amdgcn_exp2f(ml[i].x - base);
-        l += w * ml[i].y;
-        weights[mine][64 * i + lane] = w;  // kWaves = 4: each wave writes the same
+#pragma nounroll
+    for (uint32_t i = lane; i < parts; i += 64) {  // (its own)
+        const float w = __builtin_amdgcn_exp2f(stats[mine][i].x - base);
+        l += w * stats[mine][i].y;
+        weights[mine][i] = w;
     }
     l = wave_sum(l);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -862,14 +863,14 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
     const auto add = [&](float w, const float4 &y) {
         x.x += w * y.x, x.y += w * y.y, x.z += w * y.z, x.w += w * y.w;
     };
-    for (uint32_t e = 0; e < 2; e++)
-        if (sub + e * kStep < parts) add(weights[mine][sub + e * kStep], first[e]);
-    uint32_t i = sub + 2 * kStep;
+    if (sub < parts) add(weights[mine][sub], first);
+    uint32_t i = sub + kStep;
     for (; i + 3 * kStep < parts; i += 4 * kStep) {
         float4 y[4];
         for (uint32_t e = 0; e < 4; e++) y[e] = value(i + e * kStep);
         for (uint32_t e = 0; e < 4; e++) add(weights[mine][i + e * kStep], y[e]);
     }
+#pragma nounroll
     for (; i < parts; i += kStep) add(weights[mine][i], value(i));
     for (uint32_t d = kLanes; d < 64; d *= 2) {
         x.x += __shfl_xor(x.x, d), x.y += __shfl_xor(x.y, d);
