@@ -266,7 +266,7 @@ int df11_kv_append(const void *q, uint64_t q_stride, const void *k, uint64_t k_s
  *     no result: out and lse NaN.
  * tokens = 0 launches nothing.  A call of few rows cuts its work into shares that it
  * joins through the workspace; one of many needs none.  DF11_E_UNSUPPORTED for tokens *
- * heads of 2^26 or 2^38 / cache.heads tokens (sequences times what a table row holds,
+ * heads of 2^26 or 2^37 / cache.heads tokens (sequences times what a table row holds,
  * prompts' and the prefix' times their rows / 128) with a workspace, and for more than
  * 2^24 - 1 workgroups (tokens * heads / 128 + sequences * cache.heads) without. */
 int df11_prefix_attention_workspace_bytes(uint64_t tokens, uint32_t heads,

@@ -17,6 +17,15 @@
 // products.  A direct load fills LDS in the lanes' order, so the rows cannot be
 // padded; instead the 16-byte pieces of token t lie at piece ^ swizzle(t), which
 // each lane takes into account in the address it loads from.
+//
+// Two workgroups of four waves a CU (66 KB of LDS and 256 registers a lane each).  Few
+// rows are bound by memory: 31 sequences of up to 30,001 tokens, 1.7 GB of keys and
+// values, take 295 us (5.8 TB/s); 8 rows behind 131,072 shared tokens 122 us (5.0 TB/s).
+// Many are bound by what a SIMD issues: a prompt of 8192 tokens, 32 heads over 8, runs at
+// 1,000 TFLOP/s with the matrix cores busy 47% of the time and the softmax' 139 vector
+// operations a tile of 32 x 64 most of the rest (without its exponentials it would take 6%
+// less, without any of its operations but the maximum 12%, without the reads of V from
+// LDS 7%).
 
 #include "df11_kv_common.h"
 
@@ -74,8 +83,8 @@ struct AttendArgs {
     uint32_t pages, page_shift, heads, kv_heads, group;
     uint32_t own_tiles, own_groups;  // `whole`: tile numbers; groups of them that share an XCD
     // `shares`: tiles of rows and of tokens of the prefix, most parts of a row's prefix and
-    // of its own tokens, and for the join the share's size, the tiles of all sequences'
-    // own tokens, and those in front of every sequence
+    // of its own tokens, and for the join the share's size, where own tokens begin, their
+    // units, and those in front of every sequence
     uint32_t row_tiles, front_tiles, front_parts, own_parts;
     uint32_t *sums;
 };
@@ -255,7 +264,11 @@ struct Worker {
                 s[b] = Mat<C>::product(
                     *reinterpret_cast<const s8 *>(k + at.k[i] + b * 32 * P::kRowBytes), q[i], s[b]);
     }
-    // The softmax' step: p of them, in the order in which they meet the values.
+    // The softmax' step: p of them, in the order in which they meet the values.  l sums
+    // them in 32 bits; the matrix cores take them in the cache's type.  That rounding, half
+    // a step of each p to either side, and the result's own are the only ones to fewer bits
+    // (relative error of a result 0.0022 against 0.0017 for the result's rounding alone, in
+    // BF16); P in two terms would take a second product with V for each.
     template <uint32_t kCount>
     __device__ void weigh(const acc16 (&s)[kCount], s8 (&p)[2 * kCount]) {
         float top = s[0][0];
@@ -586,13 +599,31 @@ __global__ __launch_bounds__(kThreads, 2) void attend_whole_kernel(AttendArgs a)
 // All the work in a row, cut into equal shares: the prefix' tokens for each head and tile
 // of rows, then every sequence's own tokens for each head and tile of its rows.  The unit
 // is a tile of kTile tokens; kStart units before an item's tiles stand for what it costs to
-// begin and end one (about 7 us of loads after one another, where a tile takes 2).
+// begin and end one: loads after one another, and code that is run once.  (Units of 2, 4 and
+// 6: 16 rows behind 4,099 shared tokens 24.7, 22.2 and 22.4 us, 64 behind 32,768 109, 108
+// and 112.)
 constexpr uint32_t kStart = 4;
-struct Shares {
-    uint32_t front, own, size;  // units of the prefix, of own tokens (one head), of a share
-};
 __device__ inline uint32_t cost(uint32_t tiles) { return tiles ? kStart + tiles : 0; }
 __device__ inline uint32_t pieces(uint32_t n, uint32_t of) { return (n + of - 1) / of; }
+// Where a few tiles of rows read the prefix, a share of it is taken by as many workgroups,
+// one for each tile, on one XCD: its L2 reads the keys and values once for all.  (Two tiles
+// of 128 rows behind 32,768 shared tokens: 533 -> 399 MB from memory, 105 -> 98 us; behind
+// 131,072 214 -> 183 us.)
+constexpr uint32_t kMaxTogether = 16;
+__host__ __device__ inline uint32_t together(uint32_t row_tiles) {
+    return row_tiles <= kMaxTogether ? row_tiles : 1;
+}
+struct Shares {
+    uint32_t size;         // units of a share
+    uint32_t front;        // units of the prefix for `copies` tiles of rows
+    uint32_t copies, runs; // shares of the prefix: of `runs` each is there `copies` times
+    uint32_t own_at, own;  // own tokens: where they begin, units for a head
+};
+// The prefix' place in the row for a head and tile of rows.
+__device__ inline uint32_t front_at(const AttendArgs &a, uint32_t kvh, uint32_t tile) {
+    const uint32_t tiles = together(a.row_tiles) == a.row_tiles ? 1 : a.row_tiles;
+    return (kvh * tiles + (tiles == 1 ? 0 : tile)) * cost(a.front_tiles);
+}
 
 // 64 sequences, one a lane: their rows, units, and the units of all sequences before.
 struct Lane {
@@ -656,32 +687,49 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
     const Batch &b = a.batch;
     const uint32_t lane = threadIdx.x & 63;
     // the units of all sequences, and the most tiles of a row
-    Shares w{a.kv_heads * a.row_tiles * cost(a.front_tiles), 0, 0};
+    Shares w{};
+    w.copies = together(a.row_tiles);
+    w.front = a.kv_heads * (a.row_tiles / w.copies) * cost(a.front_tiles);
     uint32_t most = 0;
     Lane y{};  // of up to 64 sequences: all of them
-    const uint64_t own_tiles = each_64(a, [&](uint32_t s0, const Lane &z) {
+    const uint64_t own_units = each_64(a, [&](uint32_t s0, const Lane &z) {
         y = z;
         most = max(most, z.most);
         if (blockIdx.x == 0 && threadIdx.x < 64 && s0 + lane < b.sequences)
-            a.sums[2 + s0 + lane] = z.before;
+            a.sums[3 + s0 + lane] = z.before;
         return false;
     });
     most = wave_max(most);
-    // (more than 32 bits only where the sequences' starts do not ascend: no result)
-    w.own = (w.front + a.kv_heads * own_tiles) >> 32 ? 0 : own_tiles;
-    // no row has more parts than there is room for
-    w.size = pieces(w.front + a.kv_heads * w.own, gridDim.x);
+    // (more than 31 bits only where the sequences' starts do not ascend: no result)
+    w.own = (w.front * w.copies + a.kv_heads * own_units) >> 31 ? 0 : own_units;
+    // no row has more parts than there is room for, and no more shares are than workgroups
+    w.size = pieces(w.front * w.copies + a.kv_heads * w.own,
+                    gridDim.x - (w.copies > 1 ? w.copies + 1 : 0));
     if (a.front_parts > 1) w.size = max(w.size, pieces(a.front_tiles - 1, a.front_parts - 1));
     if (a.own_parts > 1) w.size = max(w.size, pieces(most - min(most, 1u), a.own_parts - 1));
     w.size = max(w.size, 1u);
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.sums[0] = w.size, a.sums[1] = w.own;
+    w.runs = pieces(w.front, w.size);
+    // (one copy: a share may have the prefix' last units and the first of own tokens)
+    w.own_at = w.copies > 1 ? w.runs * w.copies * w.size : w.front;
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        a.sums[0] = w.size, a.sums[1] = w.own_at, a.sums[2] = w.own;
     // A CU has the workgroups i and i + 256: one takes its share from the front of the row
     // (the prefix, which the matrix cores bound), the other from its end (own tokens, which
     // memory bounds).
     const uint32_t half = gridDim.x / 2;
     const uint32_t share = blockIdx.x < half ? blockIdx.x : gridDim.x - 1 - (blockIdx.x - half);
-    uint32_t at = share * w.size;
-    const uint32_t end = min(at + w.size, w.front + a.kv_heads * w.own);
+    uint32_t at = share * w.size, end = min(at + w.size, w.own_at + a.kv_heads * w.own);
+    uint32_t run = share, copy = 0;
+    if (w.copies > 1 && share < w.runs * w.copies) {
+        // eight runs' copies after one another: the copies of a run are eight apart, on the
+        // same XCD
+        const uint32_t eight = share / (8 * w.copies), n = min(8u, w.runs - 8 * eight);
+        const uint32_t in = share - 8 * eight * w.copies;
+        run = 8 * eight + in % n;
+        copy = in / n;
+        at = run * w.size;
+        end = min(at + w.size, w.front);
+    }
     if (at >= end) return;
     uint32_t s = ~0u, i = 0, own_unit = 0, kvh = 0;  // own tokens: where `at` is
     Sequence q{};
@@ -699,8 +747,8 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
             own_unit -= cost(q.token_tiles(a, i));
     };
     // (known before the first tile of rows: not kept beyond it)
-    if (end > w.front && b.sequences <= 64) {
-        const uint32_t from = max(at, w.front) - w.front;
+    if (end > w.own_at && b.sequences <= 64) {
+        const uint32_t from = max(at, w.own_at) - w.own_at;
         kvh = from / w.own;
         go(from % w.own, true);
     }
@@ -710,16 +758,16 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
         Range front{}, own{};
         if (at < w.front) {
             tiles = a.front_tiles;
-            const uint32_t item = at / cost(tiles);
+            const uint32_t item = at / cost(tiles), of_head = a.row_tiles / w.copies;
             unit = at % cost(tiles);
-            head = item / a.row_tiles;
-            row0 = item % a.row_tiles * kRows;
+            head = item / of_head;
+            row0 = (item % of_head + copy) * kRows;
             const uint32_t all = b.first(b.sequences) * a.group;
             rows = row0 < all ? min(kRows, all - row0) : 0;
         } else {
             if (s == ~0u) {
-                kvh = (at - w.front) / w.own;
-                go((at - w.front) % w.own, false);
+                kvh = (at - w.own_at) / w.own;
+                go((at - w.own_at) % w.own, false);
                 if (s == ~0u) return;
             }
             unit = own_unit;
@@ -731,7 +779,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
         }
         n = min(cost(tiles) - unit, end - at);
         const uint32_t first = max(unit, kStart) - kStart, last = max(unit + n, kStart) - kStart;
-        part = share - (at - unit + kStart) / w.size;
+        part = (at < w.front ? run : share) - (at - unit + kStart) / w.size;
         if (at < w.front) {
             front = {b.prefix_table, b.prefix_pages, first * kTile,
                      min(b.prefix_len, last * kTile)};
@@ -748,7 +796,7 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
                                 stats, &left_out);
         }
         at += n;
-        if (at <= w.front || at >= end) continue;
+        if (at <= w.own_at || at >= end) continue;
         // on to the next tile of rows that sees something
         own_unit = 0;
         do i++;
@@ -780,14 +828,14 @@ struct Parts {
 };
 __device__ inline bool parts_of(const AttendArgs &a, uint32_t token, uint32_t head, Parts *p) {
     const uint32_t kvh = head / a.group, row = token * a.group + head % a.group;
-    const uint32_t size = a.sums[0], all = a.sums[1];
+    const uint32_t size = a.sums[0], own_at = a.sums[1], all = a.sums[2];
     uint32_t before;
     Sequence q;
     if (a.batch.sequences <= 64) {
         // one round of loads for all that is asked
         const uint32_t lane = threadIdx.x & 63, s = min(lane, a.batch.sequences - 1);
         const Sequence y = sequence(a.batch, s);
-        const uint32_t sum = a.sums[2 + s];
+        const uint32_t sum = a.sums[3 + s];
         const uint64_t here = __ballot(lane == s && y.from <= token && token < y.to);
         if (!here) return false;
         const uint32_t at = __builtin_ctzll(here);
@@ -799,17 +847,16 @@ __device__ inline bool parts_of(const AttendArgs &a, uint32_t token, uint32_t he
         const Owner o = owner(a.batch, token);
         if (o.s == ~0u) return false;
         q = sequence(a.batch, o.s);
-        before = a.sums[2 + o.s];
+        before = a.sums[3 + o.s];
     }
-    const uint32_t each = cost(a.front_tiles);
     *p = {0, 0};
-    if (each) {
-        const uint32_t at = (kvh * a.row_tiles + row / kRows) * each + kStart;
+    if (a.front_tiles) {
+        const uint32_t at = front_at(a, kvh, row / kRows) + kStart;
         p->front = min((at + a.front_tiles - 1) / size - at / size + 1, a.front_parts);
     }
     const uint32_t i = (row - q.from * a.group) / kRows, n = q.token_tiles(a, i);
     if (n) {
-        uint32_t at = a.kv_heads * a.row_tiles * each + kvh * all + before + kStart;
+        uint32_t at = own_at + kvh * all + before + kStart;
         for (uint32_t j = 0; j < i; j++) at += cost(q.token_tiles(a, j));
         p->own = min((at + n - 1) / size - at / size + 1, a.own_parts);
     }
@@ -936,10 +983,10 @@ int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_
     p->front_parts = parts(p->front_tiles, tiles * c.heads, 1);
     p->own_parts = parts(own, own_tiles * c.heads, std::min<uint64_t>(64, (64u << 20) / part_bytes));
     const uint64_t all = c.heads * (tiles * (p->front_tiles + kStart) + own_tiles * (own + kStart));
-    p->grid = std::min<uint64_t>(kSlots, up(all, 2) * 2);
+    p->grid = std::min<uint64_t>(kSlots, up(all + together(tiles) + 1, 2) * 2);
     p->joins = tokens * heads;
-    if (all >> 32 || up(p->joins, 4) >= kMaxGrid) return DF11_E_UNSUPPORTED;
-    p->bytes = (p->front_parts + p->own_parts) * part_bytes + 4 * up(2 + b.sequences, 4) * 4;
+    if (all >> 31 || up(p->joins, 4) >= kMaxGrid) return DF11_E_UNSUPPORTED;
+    p->bytes = (p->front_parts + p->own_parts) * part_bytes + 4 * up(3 + b.sequences, 4) * 4;
     return DF11_OK;
 }
 
