@@ -162,8 +162,8 @@ struct Places {
 #pragma unroll
             for (uint32_t e = 0; e < 2; e++) {
                 const uint32_t piece = 4 * b + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-                v[b][e] = (first + tok + 8 * e) * kRowBytes + ((piece ^ swizzle<D>(tok + 8 * e)) << 4) +
-                          (i & 1) * 8;
+                const uint32_t t = tok + 8 * e;
+                v[b][e] = (first + t) * kRowBytes + ((piece ^ swizzle<D>(t)) << 4) + (i & 1) * 8;
             }
     }
 };
@@ -349,7 +349,8 @@ struct Worker {
     typedef unsigned short us8 __attribute__((ext_vector_type(8)));
     __device__ static u4 not_finite(s8 x) {
         const us8 t = __builtin_bit_cast(us8, x) & static_cast<unsigned short>(0x7FFF);
-        return __builtin_bit_cast(u4, (t + static_cast<unsigned short>(0x8000 - Mat<C>::kInf)) >> 15);
+        constexpr unsigned short kCarry = 0x8000 - Mat<C>::kInf;
+        return __builtin_bit_cast(u4, (t + kCarry) >> 15);
     }
     template <uint32_t kCount>
     __device__ void products(const uint8_t *v, const s8 (&p)[2 * kCount]) {
@@ -372,7 +373,8 @@ __device__ void add_left_out(const AttendArgs &a, const Range &r, uint32_t from,
         if (i >= r.width) return;  // the row has no result
         const uint32_t page = r.table[i];
         if (page >= a.pages) return;
-        const uint64_t in = (uint64_t{kvh * D} << a.page_shift) + (t & ((1u << a.page_shift) - 1)) * D;
+        const uint64_t in =
+            (uint64_t{kvh * D} << a.page_shift) + (t & ((1u << a.page_shift) - 1)) * D;
         const uint4 y = load16(a.v + page * a.page_v + in + 8 * piece);
         for (uint32_t e = 0; e < 8; e++) {
             const float z = C::get(y, e);
@@ -429,12 +431,13 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
         // One tile is looked at while the next one is loaded.  (A loop for each kind of wave:
         // where they meet in one, O is copied around in every turn.)
         const auto loop = [&](auto count) {
+            constexpr uint32_t kCount = decltype(count)::value;
             const auto step = [&](uint8_t *k, uint8_t *v, uint8_t *to_k, uint8_t *to_v) {
                 lost = lost || none;
                 const bool more = t + kTile < r.end;
                 if (more) none = w.load(r, t + kTile, next, to_k, to_v);
                 next = w.pages(r, t + 2 * kTile);
-                if constexpr (decltype(count)::value) w.template tokens<decltype(count)::value>(k, v);
+                if constexpr (kCount) w.template tokens<kCount>(k, v);
                 t += kTile;
                 odd = !odd;
                 w.landed();
@@ -481,7 +484,8 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
     // piece ^ n.  Waves that shared tokens bring theirs to the larger bound first.
     float l = w.l + __shfl_xor(w.l, 32), m = w.m;
     if (lost || places + later > static_cast<int32_t>(room(a.batch, a.page_shift))) l = NAN;
-    float *slice = reinterpret_cast<float *>(w.wave == 0 ? k0 : w.wave == 1 ? v0 : w.wave == 2 ? k1 : v1);
+    float *slice =
+        reinterpret_cast<float *>(w.wave == 0 ? k0 : w.wave == 1 ? v0 : w.wave == 2 ? k1 : v1);
     if (split) {
         if (half == 0) stats[w.wave * 32 + n] = float2{m, l};
         __syncthreads();
@@ -981,7 +985,8 @@ int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_
     p->row_tiles = tiles;
     p->front_tiles = front;
     p->front_parts = parts(p->front_tiles, tiles * c.heads, 1);
-    p->own_parts = parts(own, own_tiles * c.heads, std::min<uint64_t>(64, (64u << 20) / part_bytes));
+    p->own_parts =
+        parts(own, own_tiles * c.heads, std::min<uint64_t>(64, (64u << 20) / part_bytes));
     const uint64_t all = c.heads * (tiles * (p->front_tiles + kStart) + own_tiles * (own + kStart));
     p->grid = std::min<uint64_t>(kSlots, up(all + together(tiles) + 1, 2) * 2);
     p->joins = tokens * heads;
@@ -1002,7 +1007,8 @@ int launch(const AttendArgs &a, const Plan &p, hipStream_t stream) {
     if (p.joins <= kFewJoins)
         hipLaunchKernelGGL((attend_join_kernel<C, D, 4>), dim3(p.joins), block, 0, stream, a);
     else
-        hipLaunchKernelGGL((attend_join_kernel<C, D, 1>), dim3(up(p.joins, 4)), block, 0, stream, a);
+        hipLaunchKernelGGL((attend_join_kernel<C, D, 1>), dim3(up(p.joins, 4)), block, 0, stream,
+                           a);
     return launched();
 }
 

@@ -80,9 +80,9 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
         const uint32_t at = apart ? u * 8 : u * 16;
         const uint32_t next = apart ? at + a.rotary / 2 : at + 8;
         const uint32_t head = is_q ? h : is_k ? h - a.heads : h - a.heads - a.kv_heads;
-        const typename S::raw *src = static_cast<const typename S::raw *>(is_q ? a.q : is_k ? a.k : a.v) +
-                                     row * (is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride) +
-                                     head * D;
+        const uint64_t stride = is_q ? a.q_stride : is_k ? a.k_stride : a.v_stride;
+        const void *from = is_q ? a.q : is_k ? a.k : a.v;
+        const auto *src = static_cast<const typename S::raw *>(from) + row * stride + head * D;
         uint16_t *dst = is_q ? a.q_out + row * a.out_stride + head * D
                              : (is_k ? a.cache_k + page * a.page_k : a.cache_v + page * a.page_v) +
                                    (uint64_t{head * D} << a.page_shift) + in_page;
@@ -99,7 +99,8 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
         } else if (turns) {
             for (uint32_t e = 0; e < 8; e++) {
                 const float c = turn[0][u * 8 + e], s = turn[1][u * 8 + e];
-                float &p = e < 4 ? x[2 * e] : y[2 * e - 8], &q = e < 4 ? x[2 * e + 1] : y[2 * e - 7];
+                float &p = e < 4 ? x[2 * e] : y[2 * e - 8];
+                float &q = e < 4 ? x[2 * e + 1] : y[2 * e - 7];
                 const float p0 = p, q0 = q;
                 p = p0 * c - q0 * s;
                 q = q0 * c + p0 * s;
@@ -139,7 +140,8 @@ int df11_kv_append(const void *q, uint64_t q_stride, const void *k, uint64_t k_s
     if (rotary % 16 || rotary > cache->dim || (rotary && (!inv_freq || misaligned(inv_freq, 4))))
         return DF11_E_INVALID_ARG;
     if (!tokens || !batch->sequences) return DF11_OK;
-    const uint64_t q_cols = uint64_t{heads} * cache->dim, kv_cols = uint64_t{cache->heads} * cache->dim;
+    const uint64_t q_cols = uint64_t{heads} * cache->dim;
+    const uint64_t kv_cols = uint64_t{cache->heads} * cache->dim;
     const uint32_t size = elem_bytes(dtype);
     rc = check_strided(q, q_stride, q_cols, tokens, size);
     if (!rc) rc = check_strided(k, k_stride, kv_cols, tokens, size);

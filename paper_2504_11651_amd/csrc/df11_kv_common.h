@@ -95,8 +95,8 @@ inline int check_batch(const df11_kv_batch *b) {
 }
 
 inline Batch device_batch(const df11_kv_batch &b, uint64_t rows) {
-    return {b.start,     b.length, b.table,        b.prefix_table, b.sequences > 1 ? b.table_stride : 0,
-            b.sequences, b.width,  b.prefix_pages, b.prefix_len,   static_cast<uint32_t>(rows)};
+    return {b.start, b.length, b.table, b.prefix_table, b.sequences > 1 ? b.table_stride : 0,
+            b.sequences, b.width, b.prefix_pages, b.prefix_len, static_cast<uint32_t>(rows)};
 }
 
 // Rows of `size`-byte elements that are loaded 16 bytes at a time.

@@ -123,7 +123,7 @@ class KVCache(NamedTuple):
 class KVBatch(NamedTuple):
     """The sequences that a call works on, and where their tokens lie."""
     start: torch.Tensor   # int32 (sequences + 1,): first row of each, ascending from 0, and the end
-    length: torch.Tensor  # int32 (sequences,): own tokens of each, the call's rows (its last) included
+    length: torch.Tensor  # int32 (sequences,): own tokens of each, with the call's rows, its last
     table: torch.Tensor   # int32 (sequences, width): pages of each sequence's own tokens
     prefix_table: Optional[torch.Tensor] = None  # int32 (n,): pages of the shared prefix
     prefix_len: int = 0                          # its tokens
@@ -515,6 +515,8 @@ def _on_gpu(t, what):
     index = t.get_device()
     if index < 0:
         raise ValueError(f"{what} must be on a GPU, not {t.device}")
+    if index != torch._C._cuda_getDevice():
+        raise ValueError(f"{what} must be on the current GPU, not {t.device}")
     return index
 
 
@@ -555,7 +557,8 @@ def _append_sizes(index, q, k, v, inv_freq, q_out, cache_k, cache_v, *batch):
     out_stride = q[0][1]
     if q_out is not None:
         out_stride = _as_rows(q_out, (cache_k[2],), index, "q_out", q[0])
-    return c, b, prefix_pages, q_stride, k_stride, v_stride, DTYPES[q[2]], tokens, heads, rotary, out_stride
+    return (c, b, prefix_pages, q_stride, k_stride, v_stride, DTYPES[q[2]], tokens, heads, rotary,
+            out_stride)
 
 
 def kv_append(q, k, v, inv_freq, cache: KVCache, batch: KVBatch, interleaved: bool = False,
@@ -635,8 +638,8 @@ def prefix_attention(q, cache: KVCache, batch: KVBatch, scale: Optional[float] =
     index = _on_gpu(q, "q")
     start, length, table, prefix_table, prefix_len = batch
     c, b, prefix_pages, q_stride, tokens, heads, out_stride, usual, ws_bytes = _attention_sizes(
-        index, prefix_len, _look(q), _look(out), _look(lse), _look(cache[0]), _look(cache[1]), _look(start),
-        _look(length), _look(table), _look(prefix_table))
+        index, prefix_len, _look(q), _look(out), _look(lse), _look(cache[0]), _look(cache[1]),
+        _look(start), _look(length), _look(table), _look(prefix_table))
     if out is None:
         out = _new(q.shape, q.dtype, q.device, stream)
     if lse is None and need_lse:

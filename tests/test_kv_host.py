@@ -176,6 +176,20 @@ def test_tensors_that_do_not_fit():
         ops._heads(100, 64, "q")
 
 
+def test_another_gpu_than_the_current_one_is_refused(monkeypatch):
+    class Elsewhere:
+        device = "cuda:1"
+
+        def get_device(self):
+            return 1
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    with pytest.raises(ValueError, match="current GPU, not cuda:1"):
+        ops._on_gpu(Elsewhere(), "q")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    assert ops._on_gpu(Elsewhere(), "q") == 1
+
+
 def sizes_of(**change):
     """What kv_append makes of CPU tensors that would fit but for `change`."""
     cache, batch = cpu_case()
