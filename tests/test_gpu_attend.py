@@ -1,6 +1,7 @@
 """Attention to a shared prefix and to each sequence's own tokens over a paged cache,
 against its definition in 64 bits."""
 import math
+import random
 
 import pytest
 import torch
@@ -312,6 +313,24 @@ def test_far_pages():
     k.copy_(c.k), v.copy_(c.v)
     got = ops.prefix_attention(c.q, ops.KVCache(k, v), c.batch, need_lse=True)
     assert torch.equal(got.out, want.out) and torch.equal(got.lse, want.lse)
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_random_batches(seed):
+    """Sizes, layouts and lengths of all kinds together."""
+    rng = random.Random(seed)
+    group = rng.choice([1, 2, 3, 4, 5, 8, 13, 40])
+    kv_heads = rng.choice([1, 2, 3, 4, 8])
+    page = rng.choice([16, 32, 64, 128, 512])
+    new, own = [], []
+    for _ in range(rng.choice([1, 2, 3, 10, 40, 70])):
+        new.append(rng.choice([0, 1, 1, 1, 2, 5, rng.randint(1, 90)]))
+        own.append(new[-1] + rng.choice([0, 0, 1, rng.randint(0, 70), rng.randint(0, 900)]) - (rng.random() < 0.1) * 3)
+    c = Case(new, own, prefix=rng.choice([0, 0, 1, rng.randint(1, 200), rng.randint(1, 3000)]), heads=group * kv_heads,
+             kv_heads=kv_heads, dim=rng.choice([64, 128]), page=page, dtype=rng.choice([BF16, F16]), seed=seed,
+             spare=rng.choice([0, 1, 20]))
+    if sum(new):
+        c.check(scale=rng.choice([None, 0.02, 0.5]))
 
 
 def test_the_same_bits_every_time():
