@@ -171,7 +171,6 @@ struct Places {
 template <class C, uint32_t D>
 struct Worker {
     using P = Places<D>;
-    static constexpr uint32_t kBytes = kTile * 2 * D;  // of a tile of K or V
     static constexpr uint32_t kLoads = 2 * D / 64;     // 1 KB each: 16 tokens
     static constexpr uint32_t kEach = 16 / kLoads;     // tokens of one
 
