@@ -482,7 +482,8 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
     // Rows through LDS: a wave's 32 x D floats in a buffer, 16-byte pieces of row n at
     // piece ^ n.  Waves that shared tokens bring theirs to the larger bound first.
     float l = w.l + __shfl_xor(w.l, 32), m = w.m;
-    if (lost || places + later > static_cast<int32_t>(room(a.batch, a.page_shift))) l = NAN;
+    if (lost || (kWhole && places + later > static_cast<int32_t>(room(a.batch, a.page_shift))))
+        l = NAN;  // (of a share's rows the join knows: a row may have no share of own tokens)
     float *slice =
         reinterpret_cast<float *>(w.wave == 0 ? k0 : w.wave == 1 ? v0 : w.wave == 2 ? k1 : v1);
     if (split) {
@@ -825,9 +826,11 @@ __global__ __launch_bounds__(kThreads, 2) void attend_shares_kernel(AttendArgs a
 }
 
 // A row's sequence, and the parts of the prefix and of own tokens that a head of it has:
-// those of the prefix are 0.., of own tokens front_parts...
+// those of the prefix are 0.., of own tokens front_parts...  past: it sees places past the
+// table's width, whose tokens are in no part.
 struct Parts {
     uint32_t front, own;
+    bool past;
 };
 __device__ inline bool parts_of(const AttendArgs &a, uint32_t token, uint32_t head, Parts *p) {
     const uint32_t kvh = head / a.group, row = token * a.group + head % a.group;
@@ -852,7 +855,9 @@ __device__ inline bool parts_of(const AttendArgs &a, uint32_t token, uint32_t he
         q = sequence(a.batch, o.s);
         before = a.sums[3 + o.s];
     }
-    *p = {0, 0};
+    *p = {0, 0,
+          q.before + static_cast<int32_t>(token) >
+              static_cast<int32_t>(room(a.batch, a.page_shift))};
     if (a.front_tiles) {
         const uint32_t at = front_at(a, kvh, row / kRows) + kStart;
         p->front = min((at + a.front_tiles - 1) / size - at / size + 1, a.front_parts);
@@ -890,7 +895,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
     // unrolled: a kernel begins with no code in the instruction cache, and what it runs once
     // costs about a microsecond a kilobyte.)
     const float4 none = {0.0f, 0.0f, 0.0f, 0.0f}, first = sub < parts ? value(sub) : none;
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, l = n.past ? NAN : 0.0f;
 #pragma nounroll
     for (uint32_t i = lane; i < parts; i += 64) {
         const float2 ml = a.part_ml[slot(i)];
