@@ -257,7 +257,8 @@ int df11_kv_append(const void *q, uint64_t q_stride, const void *k, uint64_t k_s
  *              number above 0.
  * The rows of all sequences read the prefix together, once.  Products are summed in
  * 32 bits on the matrix cores, the softmax is held in 32 bits; exp(s_j - m) is
- * rounded to the cache's type where it meets v.
+ * rounded to the cache's type where it meets v (in DF11_F16 in steps that end at 2^-31 of
+ * the row's largest).
  *   - A row that sees nothing (no prefix and a negative place), or scores of -inf
  *     alone: out 0, lse -inf.
  *   - What lies behind a row's place (in pages, or later rows' keys and values) has

@@ -40,8 +40,8 @@ constexpr uint32_t kThreads = 256;
 constexpr uint32_t kTile = 64;   // tokens of a tile
 constexpr uint32_t kRows = 128;  // rows of a tile: 32 a wave
 constexpr uint32_t kMaxParts = 256;  // of the prefix, and of a sequence's own tokens
-// How far c s may rise above m before O is taken down: p stays below 2^8, far from
-// the largest fp16, and what is summed in 32 bits loses nothing.
+// How far c s may rise above the row's largest so far before O is taken down: what is
+// summed in 32 bits loses nothing by it.
 constexpr float kSlack = 8.0f;
 
 typedef float acc16 __attribute__((ext_vector_type(16)));
@@ -56,6 +56,7 @@ struct Mat;
 template <>
 struct Mat<BF16> {
     static constexpr uint32_t kInf = 0x7F80;  // the least that is not finite, without sign
+    static constexpr float kLift = 0.0f;      // how far m lies below the largest c s
     static __device__ acc16 product(s8 a, s8 b, acc16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a),
                                                        __builtin_bit_cast(b8, b), c, 0, 0, 0);
@@ -64,6 +65,11 @@ struct Mat<BF16> {
 template <>
 struct Mat<F16> {
     static constexpr uint32_t kInf = 0x7C00;
+    // p from 2^7 for the largest on, below 2^(7 + kSlack) = half the largest fp16.  Its
+    // steps end at 2^-24, which is 2^-31 of the largest then: thousands of tokens far below
+    // it still weigh what l counts of them.  (8192 tokens 15 powers of e below one: with m at
+    // the largest 2.6% of their share was lost, at 17.5 powers all of it.)
+    static constexpr float kLift = 7.0f;
     static __device__ acc16 product(s8 a, s8 b, acc16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a),
                                                       __builtin_bit_cast(h8, b), c, 0, 0, 0);
@@ -278,8 +284,8 @@ struct Worker {
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top),
                                                            __float_as_uint(top), false, false);
         top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.c;
-        if (__builtin_expect(__any(top > m + kSlack), 0)) {
-            const float rise = fmaxf(m, top);
+        if (__builtin_expect(__any(top > m + (kSlack + Mat<C>::kLift)), 0)) {
+            const float rise = fmaxf(m, top - Mat<C>::kLift);
             base = rise == -INFINITY ? 0.0f : rise;
             const float down = __builtin_amdgcn_exp2f(m - base);
             m = rise;
