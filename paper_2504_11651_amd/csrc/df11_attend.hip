@@ -1,10 +1,10 @@
 // Attention of a batch to a prefix that its sequences share and to their own
 // tokens, over a paged cache.
 //
-// One pass over keys and values: scores s of 64 tokens at a time, p = 2^(c s - m)
-// with m a running bound of the row's c s (c = scale log2 e), l += p, O += p v, and
-// l and O taken down by 2^(m - m') where the bound rises.  Parts of a row that
-// different workgroups took are joined with 2^(m_i - m).
+// One pass over keys and values: scores s of 64 tokens at a time, p = 2^(c (s - m))
+// with m a running bound of the row's s (c = scale log2 e), l += p, O += p v, and
+// l and O taken down by 2^(c (m - m')) where the bound rises.  Parts of a row that
+// different workgroups took are joined with 2^(c (m_i - m)).
 //
 // A tile is kRows rows of q (tokens x query heads that share a head of the cache)
 // against 64 tokens.  S^T = K Q^T on v_mfma_f32_32x32x16: a lane then holds 16
@@ -40,9 +40,13 @@ constexpr uint32_t kThreads = 256;
 constexpr uint32_t kTile = 64;   // tokens of a tile
 constexpr uint32_t kRows = 128;  // rows of a tile: 32 a wave
 constexpr uint32_t kMaxParts = 256;  // of the prefix, and of a sequence's own tokens
-// How far c s may rise above the row's largest so far before O is taken down: what is
-// summed in 32 bits loses nothing by it.
+// How far c s may rise above c m before O is taken down: what is summed in 32 bits loses
+// nothing by it.
 constexpr float kSlack = 8.0f;
+// From c s of this size on 32 bits hold it in steps too large for c s - c m, and p is taken
+// from s - m, which is exact where it counts (an operation more for each score).
+constexpr float kLarge = 1 << 20;
+constexpr float kMaxSlack = 1.0e38f;  // of s, whatever c is: -inf and it are -inf
 
 typedef float acc16 __attribute__((ext_vector_type(16)));
 typedef short s4 __attribute__((ext_vector_type(4)));
@@ -56,7 +60,7 @@ struct Mat;
 template <>
 struct Mat<BF16> {
     static constexpr uint32_t kInf = 0x7F80;  // the least that is not finite, without sign
-    static constexpr float kLift = 0.0f;      // how far m lies below the largest c s
+    static constexpr float kLift = 0.0f;      // p = 2^(c (s - m) + kLift)
     static __device__ acc16 product(s8 a, s8 b, acc16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a),
                                                        __builtin_bit_cast(b8, b), c, 0, 0, 0);
@@ -67,8 +71,8 @@ struct Mat<F16> {
     static constexpr uint32_t kInf = 0x7C00;
     // p from 2^7 for the largest on, below 2^(7 + kSlack) = half the largest fp16.  Its
     // steps end at 2^-24, which is 2^-31 of the largest then: thousands of tokens far below
-    // it still weigh what l counts of them.  (8192 tokens 15 powers of e below one: with m at
-    // the largest 2.6% of their share was lost, at 17.5 powers all of it.)
+    // it still weigh what l counts of them.  (8192 tokens 15 powers of e below one: from 1
+    // on 2.6% of their share was lost, at 17.5 powers all of it.)
     static constexpr float kLift = 7.0f;
     static __device__ acc16 product(s8 a, s8 b, acc16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a),
@@ -85,7 +89,8 @@ struct AttendArgs {
     float2 *part_ml; // parts x tokens x heads: m, l
     uint64_t q_stride, out_stride, page_k, page_v;
     Batch batch;
-    float c;  // scale log2 e
+    float c;      // scale log2 e
+    float slack;  // kSlack / c
     uint32_t pages, page_shift, heads, kv_heads, group;
     uint32_t own_tiles, own_groups;  // `whole`: tile numbers; groups of them that share an XCD
     // `shares`: tiles of rows and of tokens of the prefix, most parts of a row's prefix and
@@ -187,7 +192,9 @@ struct Worker {
     uint32_t from[kLoads];  // a lane's bytes from its 16 tokens' first
     s8 q[P::kSteps];
     acc16 o[P::kBlocks];
-    float m = -INFINITY, base = 0.0f, l = 0.0f;  // base: m where it is a number
+    float m = -INFINITY, l = 0.0f;
+    float base = 0.0f;   // c m - kLift where m is a number
+    bool large = false;  // in some lane of the wave
 
     __device__ Worker(const AttendArgs &args, uint32_t thread, uint32_t kvh_, bool split)
         : a(args), at(thread & 63, split ? thread >> 1 & 32 : 0), lane(thread & 63),
@@ -275,7 +282,7 @@ struct Worker {
     // (relative error of a result 0.0022 against 0.0017 for the result's rounding alone, in
     // BF16); P in two terms would take a second product with V for each.
     template <uint32_t kCount>
-    __device__ void weigh(const acc16 (&s)[kCount], s8 (&p)[2 * kCount]) {
+    __device__ void weigh(acc16 (&s)[kCount], s8 (&p)[2 * kCount]) {
         float top = s[0][0];
 #pragma unroll
         for (uint32_t b = 0; b < kCount; b++)
@@ -283,23 +290,33 @@ struct Worker {
             for (uint32_t e = 0; e < 16; e++) top = fmaxf(top, s[b][e]);
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top),
                                                            __float_as_uint(top), false, false);
-        top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.c;
-        if (__builtin_expect(__any(top > m + (kSlack + Mat<C>::kLift)), 0)) {
-            const float rise = fmaxf(m, top - Mat<C>::kLift);
-            base = rise == -INFINITY ? 0.0f : rise;
-            const float down = __builtin_amdgcn_exp2f(m - base);
+        top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+        if (__builtin_expect(__any(top > m + a.slack), 0)) {
+            const float rise = fmaxf(m, top), at = rise == -INFINITY ? 0.0f : rise;
+            const float down = __builtin_amdgcn_exp2f((m - at) * a.c);
             m = rise;
+            base = fmaf(at, a.c, -Mat<C>::kLift);
+            large = __any(fabsf(base) >= kLarge);
             l *= down;
 #pragma unroll
             for (auto &x : o)
 #pragma unroll
                 for (uint32_t e = 0; e < 16; e++) x[e] *= down;
         }
+        float shift = base;
+        if (__builtin_expect(large, 0)) {
+            const float at = m == -INFINITY ? 0.0f : m;
+            shift = -Mat<C>::kLift;
+#pragma unroll
+            for (uint32_t b = 0; b < kCount; b++)
+#pragma unroll
+                for (uint32_t e = 0; e < 16; e++) s[b][e] -= at;
+        }
 #pragma unroll
         for (uint32_t b = 0; b < kCount; b++)
 #pragma unroll
             for (uint32_t e = 0; e < 16; e++) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(s[b][e], a.c, -base));
+                const float x = __builtin_amdgcn_exp2f(fmaf(s[b][e], a.c, -shift));
                 l += x;
                 p[2 * b + e / 8][e % 8] = static_cast<short>(C::store(x));
             }
@@ -497,8 +514,8 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
         __syncthreads();
         const float2 other = stats[(w.wave ^ 1) * 32 + n];
         const float both = fmaxf(m, other.x), base = both == -INFINITY ? 0.0f : both;
-        const float down = __builtin_amdgcn_exp2f(m - base);
-        l = l * down + other.y * __builtin_amdgcn_exp2f(other.x - base);
+        const float down = __builtin_amdgcn_exp2f((m - base) * a.c);
+        l = l * down + other.y * __builtin_amdgcn_exp2f((other.x - base) * a.c);
         m = both;
 #pragma unroll
         for (auto &x : w.o)
@@ -558,7 +575,8 @@ __device__ __forceinline__ void attend(const AttendArgs &a, uint32_t kvh, uint32
                     uint4{word[0], word[1], word[2], word[3]});
             if (a.lse && piece == 0)
                 a.lse[uint64_t{tok} * a.heads + hd] =
-                    ml.y == 0.0f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
+                    ml.y == 0.0f ? -INFINITY
+                                 : fmaf(ml.x, a.c, log2f(ml.y) - Mat<C>::kLift) * kLn2;
         } else {
             const uint64_t slot = (uint64_t{part} * a.batch.rows + tok) * a.heads + hd;
             float *p = a.part_o + slot * D + 8 * piece;
@@ -912,7 +930,7 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
     const float base = m == -INFINITY ? 0.0f : m;
 #pragma nounroll
     for (uint32_t i = lane; i < parts; i += 64) {  // (its own)
-        const float w = __builtin_amdgcn_exp2f(stats[mine][i].x - base);
+        const float w = __builtin_amdgcn_exp2f((stats[mine][i].x - base) * a.c);
         l += w * stats[mine][i].y;
         weights[mine][i] = w;
     }
@@ -949,7 +967,8 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
             uint2{C::store(x.x * inv) | static_cast<uint32_t>(C::store(x.y * inv)) << 16,
                   C::store(x.z * inv) | static_cast<uint32_t>(C::store(x.w * inv)) << 16};
     }
-    if (a.lse && lane == 0) a.lse[at] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+    if (a.lse && lane == 0)
+        a.lse[at] = l == 0.0f ? -INFINITY : fmaf(m, a.c, log2f(l) - Mat<C>::kLift) * kLn2;
 }
 
 constexpr uint32_t kSlots = 512;  // workgroups that the GPU holds at once: two a CU
@@ -1072,7 +1091,8 @@ int df11_prefix_attention(const void *q, uint64_t q_stride, uint64_t tokens, uin
     const AttendArgs a{static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(cache->k),
                        static_cast<const uint16_t *>(cache->v), static_cast<uint16_t *>(out), lse,
                        part_o, part_ml, q_stride, out_stride, cache->k_stride, cache->v_stride,
-                       device_batch(*batch, tokens), scale * kLog2e, cache->pages,
+                       device_batch(*batch, tokens), scale * kLog2e,
+                       std::min(kSlack / (scale * kLog2e), kMaxSlack), cache->pages,
                        static_cast<uint32_t>(__builtin_ctz(cache->page_size)), heads, cache->heads,
                        heads / cache->heads, p.own_tiles, p.own_groups, p.row_tiles, p.front_tiles,
                        p.front_parts, p.own_parts,
