@@ -9,7 +9,8 @@ namespace {
 using namespace df11ops;
 
 constexpr uint32_t kThreads = 256;
-constexpr double kTurns = 0.15915494309189533577;  // 1 / (2 pi)
+// 1 / (2 pi) as the sum of two
+constexpr double kTurns = 0.15915494309189533577, kTurnsRest = -9.839338337591243e-18;
 
 struct AppendArgs {
     const void *q, *k, *v;
@@ -53,11 +54,14 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
     if (o.s == ~0u) return;
     const int64_t place = int64_t{a.batch.length[o.s]} - (o.end - row);
     if (threadIdx.x < a.rotary / 2) {
-        // 24 bits times 31: exact in 53 for every position below 2^29, and good to
-        // 10^-9 of a turn beyond; what 32 bits then round is a fraction of a turn
-        double t = static_cast<double>(place + a.batch.prefix_len) *
-                   static_cast<double>(a.inv_freq[threadIdx.x]) * kTurns;
-        t -= rint(t);
+        // Turns of one position with what 53 bits leave out of them; of p of them the whole
+        // ones go before anything is rounded (products of 53 bits were off by 10^-8 of a
+        // turn at 2^28 and ten times that at 2^32).  What 32 bits then round is a fraction
+        // of a turn
+        const double f = a.inv_freq[threadIdx.x];
+        const double p = static_cast<double>(place + a.batch.prefix_len);
+        const double each = f * kTurns, each_rest = fma(f, kTurns, -each) + f * kTurnsRest;
+        const double t = fma(p, each, -rint(p * each)) + p * each_rest;
         float s, c;
         sincospif(static_cast<float>(2.0 * t), &s, &c);
         turn[0][threadIdx.x] = c;
