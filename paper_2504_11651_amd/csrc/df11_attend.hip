@@ -43,9 +43,10 @@ constexpr uint32_t kMaxParts = 256;  // of the prefix, and of a sequence's own t
 // How far c s may rise above c m before O is taken down: what is summed in 32 bits loses
 // nothing by it.
 constexpr float kSlack = 8.0f;
-// From c s of this size on 32 bits hold it in steps too large for c s - c m, and p is taken
-// from s - m, which is exact where it counts (an operation more for each score).
-constexpr float kLarge = 1 << 20;
+// From c m of this size on p is taken from s - m, which is exact where it counts, by an
+// operation more for each score.  Below, c m is off by half a step, 2^-15 at most, and so is
+// the weight of all that was summed under one bound: a 23rd of fp16's half step.
+constexpr float kLarge = 1024.0f;
 constexpr float kMaxSlack = 1.0e38f;  // of s, whatever c is: -inf and it are -inf
 
 typedef float acc16 __attribute__((ext_vector_type(16)));

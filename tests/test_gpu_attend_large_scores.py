@@ -84,3 +84,40 @@ def test_large_scores_of_a_prompt(dtype, q, size):
         kv[0][:] = 0
         kv[0][..., 0] = (steps * (size / 128))[:, None].to(dtype)
     check(c, q, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("prefix", [100, 1000, 5000])
+@pytest.mark.parametrize("q, k", [(0.0, 0.0), (16.0, 44.0), (30.0, 180.0), (200.0, 240.0), (1000.0, 300.0),
+                                  (1000.0, 720.0), (-1000.0, 720.0), (1000.0, 1600.0)])
+def test_weights_of_near_scores_in_parts_of_a_row(q, k, prefix, dtype):
+    """One token of the prefix and one of its own outweigh a row's others, by scores q k + d
+    that lie within 3 of each other: their weights go by the difference, however large they
+    are.  Scores and d are exact; each p is off by half a step and by 2^-15 at most where c s
+    is below 2^10 (half a step of it), the result by half a step."""
+    n = 17
+    c = Case([1] * n, [1 + 5 * i for i in range(n)], prefix=prefix, dtype=dtype, seed=7)
+    c.q[:] = 0
+    q, k = (float(torch.tensor(x).to(dtype)) for x in (q, k))
+    c.q[:, ::c.dim], c.q[:, 1::c.dim] = q, 1
+    d = (torch.arange(n, device="cuda") - 8) * 0.375
+    for i, kv in enumerate(c.sets):
+        kv[0][:], kv[1][:] = 0, 0
+        kv[0][..., 1] = -200  # the others
+        kv[0][..., 0] = k
+        at = kv[0].shape[0] // 2
+        kv[0][at, :, 1] = 0 if not i else d[i - 1].to(dtype)
+        if not i:
+            kv[1][at] = 1
+    for pages, kv in zip([c.prefix_table.long(), *c.pages], c.sets):
+        i = torch.arange(kv[0].shape[0], device="cuda")
+        c.k[pages[i // c.page], :, i % c.page] = kv[0]
+        c.v[pages[i // c.page], :, i % c.page] = kv[1]
+    score = q * k
+    assert score == float(torch.tensor(score).float()) and float((torch.tensor(score) + 0.375).float()) == score + 0.375
+    got = c.attend(scale=1.0)
+    want = 1 / (1 + d.double().exp())
+    tol = want * (3 * half_step(dtype) + 2 ** -14 + 2 ** -20)
+    near(got.out, want[:, None].expand(got.out.shape), tol[:, None].expand(got.out.shape), "out")
+    lse = score + (1 + d.double().exp()).log()
+    near(got.lse, lse[:, None].expand(got.lse.shape), (lse.abs() * 2 ** -21 + 2 ** -21)[:, None].expand(got.lse.shape), "lse")
