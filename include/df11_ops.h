@@ -255,21 +255,31 @@ int df11_kv_append(const void *q, uint64_t q_stride, const void *k, uint64_t k_s
  *   lse        tokens x heads floats, may be null;
  *   heads      a multiple of cache.heads; tokens * heads < 2^31; scale a normal
  *              number above 0.
- * The rows of all sequences read the prefix together, once.  Products are summed in
- * 32 bits on the matrix cores, the softmax is held in 32 bits; exp(s_j - m) is
- * rounded to the cache's type where it meets v (in DF11_F16 in steps that end at 2^-31 of
- * the row's largest).
+ * Products are summed in 32 bits on the matrix cores, the softmax is held in 32 bits;
+ * exp(s_j - m) is rounded to the cache's type where it meets v (in DF11_F16 in steps that
+ * end at 2^-31 of the row's largest).
  *   - A row that sees nothing (no prefix and a negative place), or scores of -inf
  *     alone: out 0, lse -inf.
  *   - What lies behind a row's place (in pages, or later rows' keys and values) has
  *     no effect on it, NaN and infinities included.
  *   - A row that sees a place past the table's width or a page outside the cache has
  *     no result: out and lse NaN.
- * tokens = 0 launches nothing.  A call of few rows cuts its work into shares that it
- * joins through the workspace; one of many needs none.  DF11_E_UNSUPPORTED for tokens *
- * heads of 2^26 or 2^37 / cache.heads tokens (sequences times what a table row holds,
- * prompts' and the prefix' times their rows / 128) with a workspace, and for more than
- * 2^24 - 1 workgroups (tokens * heads / 128 + sequences * cache.heads) without. */
+ * How the work is laid out goes by the call's sizes, the table's width among them, since
+ * lengths lie in device memory:
+ *   - in shares that are joined through the workspace: the rows of all sequences read the
+ *     prefix together, once for 128 rows of a head of the cache;
+ *   - in one kernel without a workspace, where a workgroup reads the prefix and the own
+ *     tokens of 128 rows of one sequence by itself: for sequences of 64 rows of a head of
+ *     the cache or more on average whose tiles fill half the GPU, and for short contexts
+ *     (prefix and the table's width 512 places; 1,024 or 1,536 where rows are many).
+ * So a table much wider than its sequences costs up to twice the time where they are short
+ * (a prompt of 512 tokens 41 us for 22), and prompts and single tokens behind long contexts
+ * are faster in a call each (four tokens of 30,000 beside a prompt of 1024 tokens, 32 heads
+ * over 8: 515 us in one call, 135 in two).
+ * tokens = 0 launches nothing.  DF11_E_UNSUPPORTED for tokens * heads of 2^26 or 2^37 /
+ * cache.heads tokens (sequences times what a table row holds, prompts' and the prefix'
+ * times their rows / 128) with a workspace, and for more than 2^24 - 1 workgroups (tokens *
+ * heads / 128 + sequences * cache.heads) without. */
 int df11_prefix_attention_workspace_bytes(uint64_t tokens, uint32_t heads,
                                           const df11_kv_cache *cache, const df11_kv_batch *batch,
                                           uint64_t *bytes);

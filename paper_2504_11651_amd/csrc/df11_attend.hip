@@ -20,9 +20,9 @@
 //
 // Two workgroups of four waves a CU (66 KB of LDS and 256 registers a lane each).  Few
 // rows are bound by memory: 31 sequences of up to 30,001 tokens, 1.7 GB of keys and
-// values, take 295 us (5.8 TB/s); 8 rows behind 131,072 shared tokens 122 us (5.0 TB/s).
+// values, take 292 us (5.9 TB/s); 8 rows behind 131,072 shared tokens 112 to 123 us.
 // Many are bound by what a SIMD issues: a prompt of 8192 tokens, 32 heads over 8, runs at
-// 1,000 TFLOP/s with the matrix cores busy 47% of the time and the softmax' 139 vector
+// 950 to 1,010 TFLOP/s (by the card) with the matrix cores busy 47% of the time and the softmax' 139 vector
 // operations a tile of 32 x 64 most of the rest (without its exponentials it would take 6%
 // less, without any of its operations but the maximum 12%, without the reads of V from
 // LDS 7%).
@@ -44,8 +44,9 @@ constexpr uint32_t kMaxParts = 256;  // of the prefix, and of a sequence's own t
 // nothing by it.
 constexpr float kSlack = 8.0f;
 // From c m of this size on p is taken from s - m, which is exact where it counts, by an
-// operation more for each score.  Below, c m is off by half a step, 2^-15 at most, and so is
-// the weight of all that was summed under one bound: a 23rd of fp16's half step.
+// operation more for each score (a prompt of 8192 tokens 549 -> 553 us).  Below, c m is off
+// by half a step, 2^-15 at most, and so is the weight of all that was summed under one
+// bound: a 23rd of fp16's half step.
 constexpr float kLarge = 1024.0f;
 constexpr float kMaxSlack = 1.0e38f;  // of s, whatever c is: -inf and it are -inf
 
@@ -635,9 +636,9 @@ constexpr uint32_t kStart = 4;
 __device__ inline uint32_t cost(uint32_t tiles) { return tiles ? kStart + tiles : 0; }
 __device__ inline uint32_t pieces(uint32_t n, uint32_t of) { return (n + of - 1) / of; }
 // Where a few tiles of rows read the prefix, a share of it is taken by as many workgroups,
-// one for each tile, on one XCD: its L2 reads the keys and values once for all.  (Two tiles
-// of 128 rows behind 32,768 shared tokens: 533 -> 399 MB from memory, 105 -> 98 us; behind
-// 131,072 214 -> 183 us.)
+// one for each tile, on one XCD: its L2 reads the keys and values once for all.  (Behind
+// 32,768 shared tokens: two tiles of 128 rows 533 -> 399 MB from memory and 84 -> 81 us, 8 tiles
+// 208 -> 203, 16 379 -> 373; 32 and 64 tiles are bound by their products, and no faster.)
 constexpr uint32_t kMaxTogether = 16;
 __host__ __device__ inline uint32_t together(uint32_t row_tiles) {
     return row_tiles <= kMaxTogether ? row_tiles : 1;
@@ -973,6 +974,9 @@ __global__ __launch_bounds__(kThreads) void attend_join_kernel(AttendArgs a) {
 }
 
 constexpr uint32_t kSlots = 512;  // workgroups that the GPU holds at once: two a CU
+// Up to so many rows and heads four waves join one (32 of them 17.9 us a call against 18.7
+// with one wave each, 512 24.1 against 25.4), beyond one wave does (4096 50.6 us against
+// 54.2 with four, 16,384 159 against 178).
 constexpr uint32_t kFewJoins = 1024;
 
 struct Plan {
@@ -993,10 +997,14 @@ int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_
     const uint64_t own_tiles = rows / kRows + b.sequences;
     const uint64_t space = std::min<uint64_t>(uint64_t{b.width} * c.page_size, INT32_MAX);
     const uint64_t own = std::max<uint64_t>(1, up(space, kTile)), front = up(b.prefix_len, kTile);
-    // Rows that fill tiles by themselves, enough of them to fill the GPU: the prefix is
-    // read with the own tokens, and nothing has to be joined.  So it is, too, where a
-    // workgroup has little to read (single tokens of 250 9.8 us against 14.8, 64 of up to
-    // 1000 27.8 against 34, a prompt of 512 22 against 42; at 32 tiles 59 against 56).
+    // Rows that fill tiles by themselves, enough of them to fill half the GPU: the prefix
+    // is read with the own tokens, and nothing has to be joined (32 heads over 8 behind 6,000
+    // tokens: 250 rows, 64 tiles, 157 us against 64 in shares, 750 169 against 152, 1000,
+    // 256 tiles, 176 against 193, 2000 256 against 429).  So it is, too, where a workgroup
+    // has little to read (single tokens of 250 9.2 us against 13.0, 64 of up to 1000 27.5
+    // against 33.8, a prompt of 512 21.9 against 41.3; at 32 tiles 59 against 56).  Lengths
+    // are not known here: the tables' width stands for them, and the mean of the rows for
+    // each sequence's.
     const uint64_t each = rows / std::min<uint64_t>(tokens, b.sequences), read = front + own;
     p->whole = read <= 8 || (!front && read <= 16 && own_tiles * c.heads >= kSlots) ||
                (each >= 64 && (read <= 24 || tiles * c.heads >= kSlots / 2));
@@ -1007,7 +1015,9 @@ int plan_of(uint64_t tokens, uint32_t heads, const df11_kv_cache &c, const df11_
         return p->grid < kMaxGrid ? DF11_OK : DF11_E_UNSUPPORTED;
     }
     // Shares: at least so many parts that items as long as each other can fill the GPU,
-    // and for own tokens, whose lengths differ, more while they cost little memory.
+    // and for own tokens, whose lengths differ, up to 64 while they take no more than 64 MB
+    // (8 sequences of up to 30,001 tokens 87 us against 96 without, 2 37 against 41; with up
+    // to 256 the same).
     const auto parts = [](uint64_t n, uint64_t items, uint64_t least) {
         return std::min<uint64_t>({n, kMaxParts, std::max<uint64_t>(least, kSlots / items + 2)});
     };

@@ -44,7 +44,7 @@ __device__ inline void store8(uint16_t *p, const float (&x)[8]) {
 // A workgroup appends one row.  The angles' cosines and sines are made once for all
 // heads and lie in LDS; a thread then takes 16 values at a time that turn together:
 // eight and the eight half the rotary part further, or 16 neighbours.  Many rows are bound
-// by memory (8191 of 32 + 2 x 8 heads of 128, fp32 to BF16: 56 us, 5.4 TB/s), few by the
+// by memory (8191 of 32 + 2 x 8 heads of 128, fp32 to BF16: 57 us, 5.3 TB/s), few by the
 // loads after one another (64 rows of 64 + 2 x 8 heads 4.4 us, one row 2.8).
 template <class S, class C, uint32_t D>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {

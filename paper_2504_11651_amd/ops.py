@@ -627,8 +627,11 @@ def prefix_attention(q, cache: KVCache, batch: KVBatch, scale: Optional[float] =
     """Attention of q's rows (tokens, heads * head_dim, the cache's type, rows
     contiguous, as ``kv_append`` gives them) to the prefix that the batch's
     sequences share and to their own sequence's tokens up to themselves, which the
-    cache already holds: the prefix is read once for all rows.  Consecutive
-    heads / kv_heads query heads share a head of the cache.
+    cache already holds.  Consecutive heads / kv_heads query heads share a head of the
+    cache.  Single and guessed tokens read the prefix together, prompts each for
+    themselves; which it is goes by the sizes (rows for each sequence on average, the
+    table's width), not by the lengths: prompts and single tokens of long contexts are
+    faster in two calls, short contexts with a table not much wider than they are.
 
     scale: of the products q k before the softmax (None: head_dim ** -0.5).
     ``out`` may be q itself; ``lse`` (float32 (tokens, heads), given or with
