@@ -22,10 +22,10 @@
 // rows are bound by memory: 31 sequences of up to 30,001 tokens, 1.7 GB of keys and
 // values, take 292 us (5.9 TB/s); 8 rows behind 131,072 shared tokens 112 to 123 us.
 // Many are bound by what a SIMD issues: a prompt of 8192 tokens, 32 heads over 8, runs at
-// 950 to 1,010 TFLOP/s (by the card) with the matrix cores busy 47% of the time and the softmax' 139 vector
-// operations a tile of 32 x 64 most of the rest (without its exponentials it would take 6%
-// less, without any of its operations but the maximum 12%, without the reads of V from
-// LDS 7%).
+// 950 to 1,010 TFLOP/s (by the card) with the matrix cores busy 47% of the time and the
+// softmax' 139 vector operations a tile of 32 x 64 most of the rest (without its
+// exponentials it would take 6% less, without any of its operations but the maximum 12%,
+// without the reads of V from LDS 7%).
 
 #include "df11_kv_common.h"
 
